@@ -459,7 +459,8 @@ int swam_sample_step(swam_ctx* ctx, const swam_model* model, const swam_latent_i
 enum {
   SWAM_T_ADALN = 0, SWAM_T_LNMOD, SWAM_T_GEMM_QKV, SWAM_T_ATTN, SWAM_T_GEMM_OUT,
   SWAM_T_GEMM_UP, SWAM_T_GEMM_DOWN, SWAM_T_SCORE, SWAM_T_REDUCE, SWAM_T_SELECT,
-  SWAM_T_PACK, SWAM_T_UNPACK, SWAM_T_COPY, SWAM_T_SAMPLE, SWAM_T_QK_POST, SWAM_T_COUNT
+  SWAM_T_PACK, SWAM_T_UNPACK, SWAM_T_COPY, SWAM_T_SAMPLE, SWAM_T_QK_POST, SWAM_T_QUANT, SWAM_T_GEMM_I8,
+  SWAM_T_CROSS, SWAM_T_COUNT
 };
 
 /* Bracket every launch (phase) of the classes in `mask` (bit i = class i)

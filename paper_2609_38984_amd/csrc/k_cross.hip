@@ -1,0 +1,476 @@
+// Attention of query tokens to the states of an encoder: another length than the
+// queries', grouped K/V heads, padding masks, prompts shared by sequences.
+//
+// The rows of a tile are (query token, head of the group) pairs of one sequence
+// and one K/V head, so that every head that reads a K/V head reads it from the
+// same tile.  bf16: S^T = K Q^T and O^T = V^T P^T on 32x32x16 MFMAs, one row per
+// lane (lane & 31) and the keys in the accumulator registers, as in the block's
+// self attention: row maxima and sums need one exchange, and P^T is the next
+// operand as it stands.  K and V tiles of 64 keys go global -> LDS by buffer
+// loads; a hidden key's lanes get an offset past the descriptor's end and store
+// zeros, so what padding holds never reaches a product.
+// Softmax in one pass with a running maximum (base 2, float32).
+#include "launchers.h"
+
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+namespace swam {
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+constexpr int CR_BK = 64;                      // keys per tile: one bit of a mask word each
+constexpr int CR_DWORD3 = 0x00020000;          // raw buffer descriptor, 32-bit data
+constexpr int CR_PAST_END = 0x7fffff00;        // an offset that no tile reaches
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// The sequence that holds tile t of `bq` rows (rows are tokens x group): lane b
+// looks at sequence b, a scan over the lanes finds the one.
+struct TileAt {
+  int a, rows;        // first token, token x group rows of the sequence
+  int r0;             // first row of the tile
+  int s0, s1;         // its keys
+};
+__device__ __forceinline__ bool tile_at(const CrossArgs& c, int group, int bq, int t, TileAt& o) {
+  const int lane = threadIdx.x & 63;
+  int a = 0, e = 0;
+  if (lane < c.n_seqs) {
+    e = c.cu_q ? min(max(c.cu_q[lane + 1], 0), c.n_q) : c.n_q;
+    a = c.cu_q ? min(max(c.cu_q[lane], 0), e) : 0;
+  }
+  const int nt = ((e - a) * group + bq - 1) / bq;
+  int upto = nt;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int v = __shfl_up(upto, s);
+    if (lane >= s) upto += v;
+  }
+  const uint64_t past = __ballot(upto > t);
+  if (past == 0) return false;
+  const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+  o.a = __builtin_amdgcn_readlane(a, b);
+  o.rows = (__builtin_amdgcn_readlane(e, b) - o.a) * group;
+  o.r0 = (t - (__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(nt, b))) * bq;
+  const int kb = c.kv_seq ? __builtin_amdgcn_readfirstlane(c.kv_seq[b]) : b;
+  o.s0 = o.s1 = 0;
+  if (kb >= 0 && kb < c.n_kv_seqs) {
+    o.s1 = c.cu_k ? min(max(__builtin_amdgcn_readfirstlane(c.cu_k[kb + 1]), 0), c.n_k) : c.n_k;
+    o.s0 = c.cu_k ? min(max(__builtin_amdgcn_readfirstlane(c.cu_k[kb]), 0), o.s1) : 0;
+  }
+  return true;
+}
+
+// tiles [t0, t1) of the keys of one of `splits` slices
+__device__ __forceinline__ void slice_of(int s0, int s1, int bk, int y, int splits, int& t0, int& t1) {
+  const int64_t n = (s1 - s0 + bk - 1) / bk;
+  t0 = (int)(n * y / splits);
+  t1 = (int)(n * (y + 1) / splits);
+}
+
+// partial results of slice y: [y][token][head][head_dim] sums, then [y][token][head][2]
+// (maximum, sum)
+struct Partial {
+  float* o;
+  float* ml;
+  int splits;
+};
+
+template <int D, int NW>
+__global__ void __launch_bounds__(NW * 64)
+cross_bf16(const CrossArgs c, int slots, const Partial part) {
+  constexpr int H2 = D / 64;                     // 128-byte halves of a head's row
+  constexpr int BQ = 32 * NW;
+  constexpr int TILE = CR_BK * 8 * H2;           // uint4 of a K or V tile
+  __shared__ uint4 kv[2][2][TILE];               // [stage][K | V][half][key][8 chunks]
+  const int group = c.heads / c.kv_heads;
+  const int nwg = gridDim.x, pid = blockIdx.x;
+  const int xcd = pid & 7, per = nwg >> 3, rem = nwg & 7;
+  const int id = xcd * per + min(xcd, rem) + (pid >> 3);
+  const int hk = id / slots;
+  TileAt ta;
+  if (!tile_at(c, group, BQ, id - hk * slots, ta)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, r31 = lane & 31;
+  const int rr = min(ta.r0 + wave * 32 + r31, ta.rows - 1);
+  const bool live = ta.r0 + wave * 32 + r31 < ta.rows;
+  const int64_t tok = ta.a + rr / group;
+  const int head = hk * group + rr % group;
+  bf16x8 qf[D / 16];
+  {
+    const bf16_t* qp = (const bf16_t*)c.q + tok * c.q_ld + head * D;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      qf[s] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 8 * (2 * s + g)));
+  }
+  int t0, t1;
+  slice_of(ta.s0, ta.s1, CR_BK, blockIdx.y, part.splits, t0, t1);
+
+  // visible keys of tile t, one bit each
+  auto mask_byte = [&](int t) -> int {
+    const int key = ta.s0 + t * CR_BK + lane;
+    return t < t1 && key < ta.s1 && (c.mask == nullptr || c.mask[key] != 0);
+  };
+  const int lrow = lane >> 3, kld = (int)c.k_ld, vld = (int)c.v_ld;
+  constexpr int SLABS = 8 * H2;                  // 8-row slabs of a tile
+  static_assert(SLABS % NW == 0, "every wave stages whole slabs");
+  auto issue = [&](int buf, int t, uint64_t vis) {
+    const int64_t row = ta.s0 + (int64_t)t * CR_BK;
+    const int rows = min(ta.s1 - (int)row, CR_BK);
+    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)((const bf16_t*)c.k + row * c.k_ld + hk * D), (short)0, ((rows - 1) * kld + D) * 2, CR_DWORD3);
+    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)((const bf16_t*)c.v + row * c.v_ld + hk * D), (short)0, ((rows - 1) * vld + D) * 2, CR_DWORD3);
+#pragma unroll
+    for (int j = 0; j < SLABS / NW; ++j) {
+      const int slab = wave * (SLABS / NW) + j, half = slab >> 3;
+      const int r = (slab & 7) * 8 + lrow, col = 64 * half + 8 * ((lane & 7) ^ lds_swz(r));
+      const bool see = (vis >> r) & 1;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(&kv[buf][0][slab * 64]), 16,
+                                               see ? (r * kld + col) * 2 : CR_PAST_END, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(&kv[buf][1][slab * 64]), 16,
+                                               see ? (r * vld + col) * 2 : CR_PAST_END, 0, 0, 0);
+    }
+  };
+  // V^T operand by transposed LDS reads: in each 16-lane group lane a addresses
+  // V[key0 + (a >> 2)][col0 + 4 (a & 3)] and lane i receives keys key0..key0+3 of
+  // column col0 + i, the order in which the P^T accumulators hold the keys
+  const int a16 = lane & 15, G = lane >> 4, rlo = 4 * g + (a16 >> 2);
+  int vofs[2][2];
+#pragma unroll
+  for (int ht = 0; ht < 2; ++ht)
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int r = rlo + 8 * hf, hd = 32 * ht + 16 * (G & 1) + 4 * (a16 & 3);
+      vofs[ht][hf] = r * 64 + 8 * ((hd >> 3) ^ lds_swz(r)) + (hd & 7);
+    }
+  int kofs[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) kofs[s] = r31 * 8 + ((2 * s + g) ^ lds_swz(r31));
+
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+  // the lowest finite value: a row whose keys so far are all hidden adds nothing
+  float m_run = -FLT_MAX, l_run = 0.0f;
+  const float sc = LOG2E * c.scale;
+
+  auto tile = [&](int buf, uint64_t vis, auto masked) {
+    const uint4* Kt = kv[buf][0];
+    auto scores = [&](f32x16 (&st)[2]) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[t][r] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, Kt[(s >> 2) * CR_BK * 8 + kofs[s & 3] + t * 32 * 8]);
+          st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[t], 0, 0, 0);
+        }
+        if constexpr (decltype(masked)::value) {
+          const uint32_t w = (uint32_t)(vis >> (32 * t)) >> (4 * g);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!((w >> (8 * (r >> 2) + (r & 3))) & 1u)) st[t][r] = -INFINITY;
+        }
+      }
+    };
+    bf16x8 pf[2][2];
+    float ps0, ps1;
+    auto probs = [&](const f32x16 (&st)[2]) {
+      ps0 = 0.0f; ps1 = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int mm = 0; mm < 8; mm += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(st[t][8 * u + mm], sc, -m_run));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(st[t][8 * u + mm + 1], sc, -m_run));
+            ps0 += p0; ps1 += p1;
+            // P in bf16, the other operand's type; the sum keeps float32
+            pf[t][u][mm] = (__bf16)p0; pf[t][u][mm + 1] = (__bf16)p1;
+          }
+    };
+    {
+      f32x16 st[2];
+      scores(st);
+      probs(st);
+    }
+    // the running maximum moves only when a row sum shows that some weight passed
+    // 2^8 (or is NaN): the scores are then formed again against the new one
+    if (__any(!(ps0 + ps1 <= 256.0f))) {
+      asm volatile("" ::: "memory");
+      f32x16 st[2];
+      scores(st);
+      float mx = st[0][0];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[t][r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(m_run, mx * sc);
+      const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= corr;
+      probs(st);
+    }
+    l_run += ps0 + ps1;
+    const unsigned short* vs = reinterpret_cast<const unsigned short*>(kv[buf][1]);
+#pragma unroll
+    for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int base = (ht >> 1) * CR_BK * 64 + (32 * t + 16 * u) * 64;
+          const v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1][0] + base));
+          const v4i16 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1][1] + base));
+          const uint2 w1 = __builtin_bit_cast(uint2, x1), w2 = __builtin_bit_cast(uint2, x2);
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(w1.x, w1.y, w2.x, w2.y));
+          o[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t][u], o[ht], 0, 0, 0);
+        }
+  };
+
+  // all waves of the workgroup form the same words; a tile without a visible key is
+  // neither loaded nor multiplied
+  uint64_t vis = __ballot(mask_byte(t0));
+  if (vis) issue(0, t0, vis);
+  int next = mask_byte(t0 + 1);
+  for (int t = t0; t < t1; ++t) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int buf = (t - t0) & 1;
+    const uint64_t ahead = __ballot(next);
+    if (ahead) issue(buf ^ 1, t + 1, ahead);
+    next = mask_byte(t + 2);
+    if (vis == ~0ull) tile(buf, vis, std::false_type{});
+    else if (vis) tile(buf, vis, std::true_type{});
+    vis = ahead;
+  }
+  float l = l_run + __shfl_xor(l_run, 32);
+  if (!live) return;
+  const int64_t row = tok * c.heads + head;
+  if (part.splits > 1) {
+    float* po = part.o + ((int64_t)blockIdx.y * c.n_q * c.heads + row) * D;
+#pragma unroll
+    for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<float4*>(po + 32 * ht + 8 * q4 + 4 * g) =
+            make_float4(o[ht][4 * q4], o[ht][4 * q4 + 1], o[ht][4 * q4 + 2], o[ht][4 * q4 + 3]);
+    if (g == 0) {
+      float* pm = part.ml + ((int64_t)blockIdx.y * c.n_q * c.heads + row) * 2;
+      pm[0] = m_run;
+      pm[1] = l;
+    }
+    return;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bf16_t* op = (bf16_t*)c.o + tok * c.o_ld + head * D;
+#pragma unroll
+  for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      uint2 w;
+      w.x = pack_bf16x2(o[ht][4 * q4] * inv, o[ht][4 * q4 + 1] * inv);
+      w.y = pack_bf16x2(o[ht][4 * q4 + 2] * inv, o[ht][4 * q4 + 3] * inv);
+      *(uint2*)(op + 32 * ht + 8 * q4 + 4 * g) = w;
+    }
+  if (c.lse != nullptr && g == 0) c.lse[row] = l == 0.0f ? -INFINITY : (m_run + log2f(l)) * LN2;
+}
+
+// float32: the same products on 32x32x2 MFMAs with operands straight from global
+// memory (an MFMA takes 64 cycles for 4 to 16 bytes per lane).  Four waves take
+// every fourth tile of 32 keys of the same 32 rows and meet in LDS.
+template <int D>
+__global__ void __launch_bounds__(256)
+cross_f32(const CrossArgs c, int slots, const Partial part) {
+  constexpr int LD = D + 4;
+  __shared__ float os[4][32][LD];
+  __shared__ float ms[4][32], ls[4][32];
+  const int group = c.heads / c.kv_heads;
+  const int hk = blockIdx.x / slots;
+  TileAt ta;
+  if (!tile_at(c, group, 32, blockIdx.x - hk * slots, ta)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, r31 = lane & 31;
+  const int rr = min(ta.r0 + r31, ta.rows - 1);
+  f32x4 qf[D / 8];
+  {
+    const float* qp = (const float*)c.q + (int64_t)(ta.a + rr / group) * c.q_ld + (hk * group + rr % group) * D;
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 4 * (2 * s + g));
+  }
+  int t0, t1;
+  slice_of(ta.s0, ta.s1, 32, blockIdx.y, part.splits, t0, t1);
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+  const float sc = LOG2E * c.scale;
+  float m = -FLT_MAX, l = 0.0f;
+  for (int t = t0 + wave; t < t1; t += 4) {
+    const int kb = ta.s0 + t * 32;
+    const int key = kb + r31;
+    const uint32_t vis = (uint32_t)__ballot(key < ta.s1 && (c.mask == nullptr || c.mask[min(key, ta.s1 - 1)] != 0));
+    if (vis == 0) continue;
+    const float* kp = (const float*)c.k + (int64_t)min(key, ta.s1 - 1) * c.k_ld + hk * D;
+    const float* vb = (const float*)c.v + hk * D + r31;
+    f32x16 st;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) {
+      const f32x4 kf = *reinterpret_cast<const f32x4*>(kp + 4 * (2 * s + g));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[s][e], st, 0, 0, 0);
+    }
+    const uint32_t w = vis >> (4 * g);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      st[r] = ((w >> (8 * (r >> 2) + (r & 3))) & 1u) ? st[r] * sc : -INFINITY;
+      mx = fmaxf(mx, st[r]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float m_new = fmaxf(m, mx), corr = exp2f(m - m_new);
+    m = m_new;
+    l *= corr;
+#pragma unroll
+    for (int h = 0; h < D / 32; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[h][r] *= corr;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int kr = 8 * (r >> 2) + 4 * g + (r & 3);
+      const bool see = (vis >> kr) & 1u;
+      const float p = exp2f(st[r] - m_new);
+      l += p;
+      const float* vp = vb + (int64_t)min(kb + kr, ta.s1 - 1) * c.v_ld;
+#pragma unroll
+      for (int h = 0; h < D / 32; ++h) {
+        const float v = vp[32 * h];
+        o[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(see ? v : 0.0f, p, o[h], 0, 0, 0);
+      }
+    }
+  }
+  l += __shfl_xor(l, 32);
+  if (g == 0) { ms[wave][r31] = m; ls[wave][r31] = l; }
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+      *reinterpret_cast<float4*>(&os[wave][r31][32 * t + 8 * q4 + 4 * g]) =
+          make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
+  __syncthreads();
+  const int q = tid >> 3;
+  if (ta.r0 + q >= ta.rows) return;
+  const int64_t tok = ta.a + (ta.r0 + q) / group;
+  const int head = hk * group + (ta.r0 + q) % group;
+  const int64_t row = tok * c.heads + head;
+  const float mt = fmaxf(fmaxf(ms[0][q], ms[1][q]), fmaxf(ms[2][q], ms[3][q]));
+  float f[4], lt = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = exp2f(ms[w][q] - mt);
+    lt = fmaf(ls[w][q], f[w], lt);
+  }
+  const bool whole = part.splits <= 1;
+  const float inv = !whole ? 1.0f : lt == 0.0f ? 0.0f : 1.0f / lt;
+  float* dst = whole ? (float*)c.o + tok * c.o_ld + head * D
+                     : part.o + ((int64_t)blockIdx.y * c.n_q * c.heads + row) * D;
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) {
+    const int col = 64 * h + (tid & 7) * 8;
+    float acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      acc[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) acc[e] = fmaf(os[w][q][col + e], f[w], acc[e]);
+      acc[e] *= inv;
+    }
+    store8(dst + col, acc);
+  }
+  if ((tid & 7) == 0) {
+    if (!whole) {
+      float* pm = part.ml + ((int64_t)blockIdx.y * c.n_q * c.heads + row) * 2;
+      pm[0] = mt;
+      pm[1] = lt;
+    } else if (c.lse != nullptr) {
+      c.lse[row] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * LN2;
+    }
+  }
+}
+
+// One wave per token and head adds up the slices in their order.  Rows outside
+// every sequence have none and are left as they are.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+cross_join(const CrossArgs c, const Partial part) {
+  const int64_t n = (int64_t)c.n_q * c.heads;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= n) return;
+  const int lane = threadIdx.x & 63;
+  const int tok = (int)(row / c.heads), head = (int)(row % c.heads);
+  bool in = c.cu_q == nullptr;
+  if (c.cu_q != nullptr && lane < c.n_seqs) in = tok >= c.cu_q[lane] && tok < c.cu_q[lane + 1];
+  if (!__any(in)) return;
+  float mt = -FLT_MAX;
+  for (int s = lane; s < part.splits; s += 64) mt = fmaxf(mt, part.ml[(s * n + row) * 2]);
+  mt = warp_max(mt);
+  float l = 0.0f, acc[D / 64] = {};
+  for (int s = 0; s < part.splits; ++s) {
+    const float* pm = part.ml + (s * n + row) * 2;
+    const float f = exp2f(pm[0] - mt);
+    l = fmaf(pm[1], f, l);
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(part.o[(s * n + row) * D + 64 * e + lane], f, acc[e]);
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e)
+    Elem<T>::store((T*)c.o + tok * c.o_ld + head * D + 64 * e + lane, acc[e] * inv);
+  if (c.lse != nullptr && lane == 0) c.lse[row] = l == 0.0f ? -INFINITY : (mt + log2f(l)) * LN2;
+}
+
+template <int D>
+static void run_cross(int dtype, const CrossArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
+  const int group = c.heads / c.kv_heads;
+  const int bq = dtype == 1 ? 128 : 32;
+  const int64_t rows = (int64_t)c.n_q * group;
+  const int slots = (int)((rows + (int64_t)(bq - 1) * c.n_seqs) / bq);
+  const int64_t wgs = (int64_t)slots * c.kv_heads;
+  const int64_t tiles = (c.n_k / c.n_kv_seqs + 63) / 64;
+  int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(wgs, 1), tiles / 4), 64));
+  splits = std::max<int64_t>(1, std::min<int64_t>(splits, ws_floats / std::max<int64_t>(1, (int64_t)c.n_q * c.heads * (D + 2))));
+  Partial p{ws, ws + splits * c.n_q * c.heads * D, (int)splits};
+  if (dtype == 1)
+    hipLaunchKernelGGL((cross_bf16<D, 4>), dim3((unsigned)wgs, (unsigned)splits), dim3(256), 0, st, c, slots, p);
+  else
+    hipLaunchKernelGGL((cross_f32<D>), dim3((unsigned)wgs, (unsigned)splits), dim3(256), 0, st, c, slots, p);
+  if (splits > 1) {
+    const unsigned n = (unsigned)(((int64_t)c.n_q * c.heads + 3) / 4);
+    if (dtype == 1) hipLaunchKernelGGL((cross_join<bf16_t, D>), dim3(n), dim3(256), 0, st, c, p);
+    else hipLaunchKernelGGL((cross_join<float, D>), dim3(n), dim3(256), 0, st, c, p);
+  }
+}
+
+hipError_t launch_cross(int dtype, const CrossArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
+  if (c.n_q <= 0) return hipSuccess;
+  if (c.head_dim == 64) run_cross<64>(dtype, c, ws, ws_floats, st);
+  else run_cross<128>(dtype, c, ws, ws_floats, st);
+  return hipGetLastError();
+}
+
+}  // namespace swam

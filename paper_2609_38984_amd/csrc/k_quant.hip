@@ -1,0 +1,280 @@
+// Rows to 8-bit codes with a scale each: the residual addition and RMS norm in
+// front of an 8-bit projection, and the plain quantiser of activations and
+// weights.
+//
+//   t = x + r;  y = t / sqrt(mean t^2 + eps) * gain * (1 + scale) + shift
+//   s = max|y| / 127;  code = round(y / s)
+// Two numbers of the whole row (the mean square and the largest magnitude) stand
+// between reading x and writing the codes.  The row stays on chip in float32
+// between them, so every byte moves once: memory bounds it (rows * d * (x + r +
+// sum + 1) bytes).
+#include "launchers.h"
+
+namespace swam {
+
+// Bits of |v|: as unsigned integers they order like the magnitudes, with
+// infinities and then NaN above every finite value, so one integer maximum
+// finds the largest magnitude and any non-finite value.
+__device__ __forceinline__ uint32_t mag_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+constexpr uint32_t INF_BITS = 0x7f800000u;
+
+__device__ __forceinline__ uint32_t warp_umax(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  return v;
+}
+
+// What a row's largest magnitude makes of it: the stored scale, and the factors
+// pre, inv with code = round((y pre) inv).  pre lifts rows whose 127 / max would
+// overflow.
+struct RowScale {
+  float s, pre, inv, top;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t bits) {
+  RowScale r;
+  r.top = __uint_as_float(bits);
+  r.pre = r.top < 0x1p-100f ? 0x1p100f : 1.0f;
+  r.inv = bits == 0u ? 0.0f : 127.0f / (r.top * r.pre);
+  r.s = r.top / 127.0f;
+  if (bits >= INF_BITS) {
+    r.s = __uint_as_float(0x7fc00000u);
+    r.pre = r.inv = 0.0f;
+  }
+  return r;
+}
+
+// The code of y.  EXACT: within 1e-4 of a border (the product above is off by at
+// most 2^-16 there) the side is decided on 254 |y| against (2 b + 1) max, both
+// exact in float64.
+template <bool EXACT>
+__device__ __forceinline__ int code_of(float y, const RowScale& r) {
+  if (r.inv == 0.0f) return 0;
+  const float f = (y * r.pre) * r.inv;
+  float c = rintf(f);
+  if constexpr (EXACT) {
+    if (fabsf(fabsf(f - c) - 0.5f) < 1e-4f) {
+      const float b = floorf(fabsf(f));
+      const double lhs = 254.0 * (double)fabsf(y), rhs = (2.0 * (double)b + 1.0) * (double)r.top;
+      const float even = ((int)b & 1) ? b + 1.0f : b;
+      const float m = lhs > rhs ? b + 1.0f : lhs < rhs ? b : even;
+      c = copysignf(m, y);
+    }
+  }
+  return (int)c;
+}
+
+// 1 / sqrt(mean square + eps); NaN for a sum that is NaN or overflowed, so that every
+// y and with it the scale is NaN; 0 for a row of zeros without eps
+__device__ __forceinline__ float inv_rms(float ss, int d, float eps) {
+  const float ms = ss / (float)d + eps;
+  return !(ss < INFINITY) ? __uint_as_float(0x7fc00000u) : ms > 0.0f ? 1.0f / sqrtf(ms) : 0.0f;
+}
+
+__device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
+  return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)d << 24);
+}
+
+// Sum / maximum over the NW waves that share a row; one wave needs no LDS.
+template <int NW>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  v = warp_sum(v);
+  if constexpr (NW > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v += red[w];
+  }
+  return v;
+}
+template <int NW>
+__device__ __forceinline__ uint32_t row_umax(uint32_t v, uint32_t* red) {
+  v = warp_umax(v);
+  if constexpr (NW > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v = max(v, red[w]);
+  }
+  return v;
+}
+
+// Aligned rows of up to NW * 64 * 8 * NV elements in registers: NW waves to a
+// row, lane t holding the 8-element vectors t, t + 64 NW, ...  NW = 1 puts four
+// rows on a workgroup and needs no barrier.
+template <typename T, bool NORM, int NW, int NV>
+__global__ void __launch_bounds__(256)
+quant_rows(const RowQuant a) {
+  constexpr int TPR = NW * 64, RPW = 4 / NW;
+  __shared__ float red[4];
+  __shared__ uint32_t redu[4];
+  const int64_t row = (int64_t)blockIdx.x * RPW + (NW == 4 ? 0 : threadIdx.x / TPR);
+  if (row >= a.rows) return;                    // whole waves
+  const int t = threadIdx.x % TPR, d = a.d;
+  const T* xp = (const T*)a.x + row * a.x_ld;
+  float v[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int e = (i * TPR + t) * 8;
+    if (e < d) {
+      load8(xp + e, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+    }
+  }
+  if constexpr (NORM) {
+    float ss = 0.0f;
+    if (a.res != nullptr) {
+      const T* rp = (const T*)a.res + row * a.res_ld;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int e = (i * TPR + t) * 8;
+        if (e < d) {
+          float r[8];
+          load8(rp + e, r);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] += r[j];
+        }
+      }
+    }
+    if (a.sum != nullptr) {
+      T* sp = (T*)a.sum + row * a.sum_ld;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int e = (i * TPR + t) * 8;
+        if (e < d) store8(sp + e, v[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+    ss = row_sum<NW>(ss, red);
+    const float r = inv_rms(ss, d, a.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = (i * TPR + t) * 8;
+      if (e < d) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] *= r;
+        if (a.gain != nullptr) {
+          float g[8];
+          load8((const T*)a.gain + e, g);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
+        }
+        if (a.shift != nullptr) {
+          float sc[8], sh[8];
+          load8(a.scale + e, sc);
+          load8(a.shift + e, sh);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j], 1.0f + sc[j], sh[j]);
+        }
+      }
+    }
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, mag_bits(v[i][j]));
+  const RowScale rs = row_scale(row_umax<NW>(top, redu));
+  int8_t* qp = a.q + row * a.q_ld;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int e = (i * TPR + t) * 8;
+    if (e < d) {
+      int c[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = code_of<!NORM>(v[i][j], rs);
+      *reinterpret_cast<uint2*>(qp + e) = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+    }
+  }
+  if (t == 0) a.q_scale[row] = rs.s;
+}
+
+// Any alignment and width: the row in LDS as float32, one row to a workgroup.
+template <typename T, bool NORM, int CAP>
+__global__ void __launch_bounds__(512)
+quant_rows_any(const RowQuant a) {
+  __shared__ float buf[CAP];
+  __shared__ float red[8];
+  __shared__ uint32_t redu[8];
+  const int64_t row = blockIdx.x;
+  const int d = a.d, t = threadIdx.x;
+  const T* xp = (const T*)a.x + row * a.x_ld;
+  float r = 1.0f;
+  if constexpr (NORM) {
+    float ss = 0.0f;
+    for (int e = t; e < d; e += 512) {
+      float v = Elem<T>::load(xp + e);
+      if (a.res != nullptr) v += Elem<T>::load((const T*)a.res + row * a.res_ld + e);
+      if (a.sum != nullptr) Elem<T>::store((T*)a.sum + row * a.sum_ld + e, v);
+      buf[e] = v;
+      ss = fmaf(v, v, ss);
+    }
+    ss = row_sum<8>(ss, red);
+    r = inv_rms(ss, d, a.eps);
+  }
+  uint32_t top = 0;
+  for (int e = t; e < d; e += 512) {            // every thread its own elements of buf
+    float v;
+    if constexpr (NORM) {
+      v = buf[e] * r;
+      if (a.gain != nullptr) v *= Elem<T>::load((const T*)a.gain + e);
+      if (a.shift != nullptr) v = fmaf(v, 1.0f + a.scale[e], a.shift[e]);
+    } else {
+      v = Elem<T>::load(xp + e);
+    }
+    buf[e] = v;
+    top = max(top, mag_bits(v));
+  }
+  const RowScale rs = row_scale(row_umax<8>(top, redu));
+  for (int e = t; e < d; e += 512) a.q[row * a.q_ld + e] = (int8_t)code_of<!NORM>(buf[e], rs);
+  if (t == 0) a.q_scale[row] = rs.s;
+}
+
+template <typename T, bool NORM>
+static void run_quant(const RowQuant& a, bool vec, hipStream_t st) {
+  const int vecs = (a.d + 7) / 8;
+#define SWAM_Q(NW_, NV_)                                                                         \
+  hipLaunchKernelGGL((quant_rows<T, NORM, NW_, NV_>), dim3((unsigned)((a.rows + 4 / NW_ - 1) / (4 / NW_))), \
+                     dim3(256), 0, st, a)
+  if (vec && vecs <= 256) {
+    if (vecs <= 64) SWAM_Q(1, 1);
+    else if (vecs <= 128) SWAM_Q(1, 2);
+    else if (vecs <= 192) SWAM_Q(1, 3);
+    else SWAM_Q(1, 4);
+  } else if (vec && vecs <= 1024) {
+    if (vecs <= 512) SWAM_Q(4, 2);
+    else SWAM_Q(4, 4);
+  } else if (a.d <= 8192) {
+    hipLaunchKernelGGL((quant_rows_any<T, NORM, 8192>), dim3((unsigned)a.rows), dim3(512), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((quant_rows_any<T, NORM, 32768>), dim3((unsigned)a.rows), dim3(512), 0, st, a);
+  }
+#undef SWAM_Q
+}
+
+hipError_t launch_quant_rows(int dtype, bool norm, const RowQuant& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  const int esz = dtype == 1 ? 2 : 4;
+  auto row16 = [&](const void* p, int64_t ld) {
+    return p == nullptr || (((uintptr_t)p | (uintptr_t)(ld * esz)) & 15) == 0;
+  };
+  const bool vec = a.d % 8 == 0 && row16(a.x, a.x_ld) && row16(a.res, a.res_ld) && row16(a.sum, a.sum_ld) &&
+                   row16(a.gain, 0) && (((uintptr_t)a.shift | (uintptr_t)a.scale) & 15) == 0 &&
+                   (((uintptr_t)a.q | (uintptr_t)a.q_ld) & 7) == 0;
+  if (dtype == 1) {
+    if (norm) run_quant<bf16_t, true>(a, vec, st);
+    else run_quant<bf16_t, false>(a, vec, st);
+  } else {
+    if (norm) run_quant<float, true>(a, vec, st);
+    else run_quant<float, false>(a, vec, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace swam

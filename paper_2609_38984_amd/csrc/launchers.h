@@ -240,4 +240,49 @@ hipError_t launch_copy(const void* src, void* dst, int64_t bytes, hipStream_t st
 hipError_t launch_copy_pruned(const void* x_full, void* y_full, const int32_t* pack_pos,
                               int64_t rows, int64_t row_bytes, hipStream_t st);
 
+// ---------------------------------------------------------------------------
+// 8-bit, encoder-conditioned block (swam_ops.h)
+// ---------------------------------------------------------------------------
+// rows to 8-bit codes (k_quant.hip); norm: with the residual addition, RMS norm,
+// gain and modulation in front
+struct RowQuant {
+  const void* x; int64_t x_ld;
+  const void* res; int64_t res_ld;     // norm only, may be NULL
+  const void* gain;                    // act [d] or NULL
+  const float *shift, *scale;          // [d] or both NULL
+  float eps;
+  int64_t rows; int d;
+  void* sum; int64_t sum_ld;           // may be NULL
+  int8_t* q; int64_t q_ld;
+  float* q_scale;
+};
+hipError_t launch_quant_rows(int dtype, bool norm, const RowQuant& a, hipStream_t st);
+
+// 8-bit product (k_gemm_i8.hip); epilogue: bias (may be NULL), then GELU or the
+// gated residual.  ws: workspace for the int32 partial sums of a split K.
+struct GemmI8 {
+  const int8_t* a; int64_t lda; const float* a_scale;
+  const int8_t* b; int64_t ldb; const float* b_scale;
+  const void* bias;
+  const void* res; int64_t ldr; const float* gate;
+  void* c; int64_t ldc;
+  int64_t M, N, K;
+  bool gelu;
+};
+hipError_t launch_gemm_i8(int dtype, const GemmI8& g, int32_t* ws, int64_t ws_words, hipStream_t st);
+
+// attention to an encoder's states (k_cross.hip); ws: workspace for the partial
+// results of split keys
+struct CrossArgs {
+  const void *q, *k, *v;
+  void* o;
+  float* lse;
+  const uint8_t* mask;
+  const int32_t *cu_q, *cu_k, *kv_seq;
+  int64_t q_ld, k_ld, v_ld, o_ld;
+  int n_seqs, n_kv_seqs, n_q, n_k, heads, kv_heads, head_dim;
+  float scale;
+};
+hipError_t launch_cross(int dtype, const CrossArgs& a, float* ws, int64_t ws_floats, hipStream_t st);
+
 }  // namespace swam

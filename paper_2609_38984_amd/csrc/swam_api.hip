@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "../../include/swam.h"
+#include "../../include/swam_ops.h"
 #include "launchers.h"
 
 #include <cmath>
@@ -294,6 +295,54 @@ bool bad_block(const swam_block_weights* w) {
     if (!q || !aligned16(q)) return true;
   return false;
 }
+
+// ---- arguments of the operators of swam_ops.h
+
+constexpr int64_t OPS_MAX_STRIDE = (1 << 22) - 1;
+
+// A call is checked before its context: what is wrong with it is reported (to
+// swam_last_error(NULL)) even where there is none, with bf16 for the missing dtype.
+int64_t ops_esz(const swam_ctx* c) { return c ? c->dv.esz : 2; }
+
+bool typed(const void* p, int64_t esz) { return ((uintptr_t)p & (uintptr_t)(esz - 1)) == 0; }
+
+// the bytes of `rows` rows of `width` elements, `ld` elements apart
+struct Span { uintptr_t lo, hi, pitch, width; };
+Span span(const void* p, int64_t ld, int64_t rows, int64_t width, int64_t esz) {
+  if (!p || rows <= 0) return Span{0, 0, 0, 0};
+  const uintptr_t lo = (uintptr_t)p;
+  return Span{lo, lo + (uintptr_t)(((rows - 1) * ld + width) * esz), (uintptr_t)(ld * esz), (uintptr_t)(width * esz)};
+}
+// whether two tensors share a byte; column ranges of one wider buffer need not
+bool meet(const Span& a, const Span& b) {
+  if (a.lo >= b.hi || b.lo >= a.hi) return false;
+  if (a.pitch != b.pitch || a.pitch == 0) return true;
+  const uintptr_t at = b.lo >= a.lo ? (b.lo - a.lo) % a.pitch : (a.pitch - (a.lo - b.lo) % a.pitch) % a.pitch;
+  return at < a.width || at + b.width > a.pitch;
+}
+
+int check_rows(swam_ctx* c, const void* x, int64_t x_stride, int64_t rows, int64_t d, const int8_t* q,
+               int64_t q_stride, const float* q_scale) {
+  if (rows < 0) return set_err(c, SWAM_E_INVALID, "rows < 0");
+  if (rows >= (1ll << 31)) return set_err(c, SWAM_E_SHAPE, "rows below 2^31");
+  if (d < 1 || d > SWAM_I8_MAX_WIDTH) return set_err(c, SWAM_E_SHAPE, "d must be in [1, SWAM_I8_MAX_WIDTH]");
+  if (rows > 0 && (!x || !q || !q_scale)) return set_err(c, SWAM_E_INVALID, "x, q, q_scale required");
+  if (x_stride < d || q_stride < d) return set_err(c, SWAM_E_INVALID, "a row stride is smaller than its row");
+  if (!typed(q_scale, 4)) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  return SWAM_OK;
+}
+
+// the context's device for the length of a call, then the caller's again
+struct OnDevice {
+  int prev = -1;
+  explicit OnDevice(swam_ctx* c) {
+    int cur = c->device;
+    if (hipGetDevice(&cur) == hipSuccess && cur != c->device && hipSetDevice(c->device) == hipSuccess) prev = cur;
+  }
+  ~OnDevice() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+};
 
 // one block in place on x [n_rows][d]; mod = this block's [6][d] modulation
 // pos_mode (rope only): 0 = dense layout, 1 = packed rows of the cached
@@ -1387,6 +1436,157 @@ int swam_timer_read_kind(swam_ctx* c, int32_t cls, int32_t kind, int64_t* launch
 
 int swam_timer_read(swam_ctx* c, int32_t cls, int64_t* launches, double* total_ms) {
   return swam_timer_read_kind(c, cls, SWAM_KIND_ANY, launches, total_ms);
+}
+
+// ------------------------------------------- 8-bit, encoder-conditioned block
+
+int swam_rms_norm_i8(swam_ctx* c, const void* x, int64_t x_stride, const void* residual,
+                     int64_t residual_stride, const void* gain, const float* shift,
+                     const float* scale, float eps, int64_t rows, int64_t d, void* sum_out,
+                     int64_t sum_stride, int8_t* q, int64_t q_stride, float* q_scale) {
+  if (int rc = check_rows(c, x, x_stride, rows, d, q, q_stride, q_scale)) return rc;
+  if (residual && residual_stride < d) return set_err(c, SWAM_E_INVALID, "residual row stride < d");
+  if (sum_out && sum_stride < d) return set_err(c, SWAM_E_INVALID, "sum_out row stride < d");
+  if (!shift != !scale) return set_err(c, SWAM_E_INVALID, "shift and scale come together");
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return set_err(c, SWAM_E_INVALID, "eps must be finite and >= 0");
+  const int64_t es = ops_esz(c);
+  if (!typed(x, es) || !typed(residual, es) || !typed(gain, es) || !typed(sum_out, es) || !typed(shift, 4) ||
+      !typed(scale, 4))
+    return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  const Span xs = span(x, x_stride, rows, d, es), rs = span(residual, residual_stride, rows, d, es);
+  const Span ss = span(sum_out, sum_stride, rows, d, es), qs = span(q, q_stride, rows, d, 1);
+  const Span cs = span(q_scale, 1, rows, 1, 4), gs = span(gain, d, 1, d, es);
+  const Span hs = span(shift, d, 1, d, 4), ls = span(scale, d, 1, d, 4);
+  const bool sum_x = sum_out == x && sum_stride == x_stride;
+  const bool sum_r = sum_out == residual && sum_stride == residual_stride;
+  if ((!sum_x && meet(ss, xs)) || (!sum_r && meet(ss, rs)))
+    return set_err(c, SWAM_E_INVALID, "sum_out overlaps x or residual (it may only be one of them)");
+  for (const Span& in : {xs, rs, gs, hs, ls, ss})
+    if (meet(qs, in) || meet(cs, in)) return set_err(c, SWAM_E_INVALID, "q or q_scale overlaps another tensor");
+  for (const Span& in : {gs, hs, ls})
+    if (meet(ss, in)) return set_err(c, SWAM_E_INVALID, "sum_out overlaps gain, shift or scale");
+  if (meet(qs, cs)) return set_err(c, SWAM_E_INVALID, "q overlaps q_scale");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (rows == 0) return SWAM_OK;
+  RowQuant a{x, x_stride, residual, residual_stride, gain, shift, scale, eps, rows, (int)d,
+             sum_out, sum_stride, q, q_stride, q_scale};
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_QUANT);
+  SWAM_HIP(c, launch_quant_rows(c->cfg.dtype, true, a, c->st), "rms_norm_i8");
+  return SWAM_OK;
+}
+
+int swam_quantize_i8(swam_ctx* c, const void* x, int64_t x_stride, int64_t rows, int64_t d,
+                     int8_t* q, int64_t q_stride, float* q_scale) {
+  if (int rc = check_rows(c, x, x_stride, rows, d, q, q_stride, q_scale)) return rc;
+  if (!typed(x, ops_esz(c))) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  const Span xs = span(x, x_stride, rows, d, ops_esz(c)), qs = span(q, q_stride, rows, d, 1);
+  const Span cs = span(q_scale, 1, rows, 1, 4);
+  if (meet(qs, xs) || meet(cs, xs) || meet(qs, cs))
+    return set_err(c, SWAM_E_INVALID, "q or q_scale overlaps another tensor");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (rows == 0) return SWAM_OK;
+  RowQuant a{};
+  a.x = x; a.x_ld = x_stride;
+  a.rows = rows; a.d = (int)d;
+  a.q = q; a.q_ld = q_stride; a.q_scale = q_scale;
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_QUANT);
+  SWAM_HIP(c, launch_quant_rows(c->cfg.dtype, false, a, c->st), "quantize_i8");
+  return SWAM_OK;
+}
+
+int swam_gemm_i8(swam_ctx* c, const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b,
+                 int64_t ldb, const float* b_scale, const void* bias, const void* residual,
+                 int64_t ldr, const float* gate, int32_t flags, void* out, int64_t ldc, int64_t m,
+                 int64_t n, int64_t k) {
+  if (m < 0 || n < 0) return set_err(c, SWAM_E_INVALID, "m and n must be >= 0");
+  if (k < 16 || k % 16 || k > SWAM_I8_MAX_K)
+    return set_err(c, SWAM_E_SHAPE, "k must be a multiple of 16 in [16, SWAM_I8_MAX_K]");
+  if (m >= (1ll << 30) || n >= (1ll << 30)) return set_err(c, SWAM_E_SHAPE, "m and n below 2^30");
+  if (flags & ~SWAM_GEMM_GELU) return set_err(c, SWAM_E_INVALID, "unknown flags");
+  if ((flags & SWAM_GEMM_GELU) && residual)
+    return set_err(c, SWAM_E_UNSUPPORTED, "GELU and a residual exclude each other");
+  if (gate && !residual) return set_err(c, SWAM_E_INVALID, "gate needs a residual");
+  const bool empty = m == 0 || n == 0;
+  if (!empty && (!a || !a_scale || !b || !b_scale || !out))
+    return set_err(c, SWAM_E_INVALID, "a, a_scale, b, b_scale, c required");
+  if (lda < k || ldb < k || ldc < n || (residual && ldr < n))
+    return set_err(c, SWAM_E_INVALID, "a row stride is smaller than its row");
+  if (lda > OPS_MAX_STRIDE || ldb > OPS_MAX_STRIDE)
+    return set_err(c, SWAM_E_SHAPE, "row strides of a and b below 2^22");
+  if (!aligned16(a) || !aligned16(b) || lda % 16 || ldb % 16)
+    return set_err(c, SWAM_E_INVALID, "a, b and their row strides must be 16-byte aligned");
+  const int64_t es = ops_esz(c);
+  if (!typed(a_scale, 4) || !typed(b_scale, 4) || !typed(gate, 4) || !typed(bias, es) ||
+      !typed(residual, es) || !typed(out, es))
+    return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  if (((m + 127) / 128) * ((n + 127) / 128) >= (1ll << 31))
+    return set_err(c, SWAM_E_SHAPE, "more than 2^31 output tiles");
+  const Span os = span(out, ldc, m, n, es);
+  for (const Span& in : {span(a, lda, m, k, 1), span(b, ldb, n, k, 1), span(a_scale, 1, m, 1, 4),
+                         span(b_scale, 1, n, 1, 4), span(bias, n, 1, n, es), span(gate, n, 1, n, 4)})
+    if (meet(os, in)) return set_err(c, SWAM_E_INVALID, "c overlaps an input");
+  if (!(residual == out && ldr == ldc) && meet(os, span(residual, ldr, m, n, es)))
+    return set_err(c, SWAM_E_INVALID, "c overlaps residual (it may only be it)");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (empty) return SWAM_OK;
+  GemmI8 g{a, lda, a_scale, b, ldb, b_scale, bias, residual, ldr, gate, out, ldc, m, n, k,
+           (flags & SWAM_GEMM_GELU) != 0};
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_GEMM_I8);
+  SWAM_HIP(c, launch_gemm_i8(c->cfg.dtype, g, c->ptr<int32_t>(c->lay.splitk), c->dv.splitk_floats, c->st),
+           "gemm_i8");
+  return SWAM_OK;
+}
+
+int swam_cross_attention(swam_ctx* c, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, const void* v, int64_t v_stride,
+                         const uint8_t* key_mask, const int32_t* cu_q, const int32_t* cu_k,
+                         const int32_t* kv_seq, int32_t n_seqs, int32_t n_kv_seqs, int64_t n_q,
+                         int64_t n_k, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                         float scale, void* o, int64_t o_stride, float* lse) {
+  if (head_dim != 64 && head_dim != 128) return set_err(c, SWAM_E_SHAPE, "head_dim must be 64 or 128");
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads)
+    return set_err(c, SWAM_E_INVALID, "n_heads must be a positive multiple of n_kv_heads");
+  if (n_seqs < 1 || n_seqs > SWAM_MAX_BATCH || n_kv_seqs < 1 || n_kv_seqs > SWAM_MAX_BATCH)
+    return set_err(c, SWAM_E_SHAPE, "1..64 query and key sequences");
+  if (!cu_q && n_seqs != 1) return set_err(c, SWAM_E_INVALID, "several query sequences need cu_q");
+  if (!cu_k && n_kv_seqs != 1) return set_err(c, SWAM_E_INVALID, "several key sequences need cu_k");
+  if (!kv_seq && n_kv_seqs != n_seqs)
+    return set_err(c, SWAM_E_INVALID, "without kv_seq there are as many key as query sequences");
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return set_err(c, SWAM_E_INVALID, "scale must be finite and > 0");
+  if (n_q < 0 || n_k < 0) return set_err(c, SWAM_E_INVALID, "n_q and n_k must be >= 0");
+  if (n_heads >= (1 << 16) || n_q * n_heads >= (1ll << 30) || n_k >= (1ll << 30))
+    return set_err(c, SWAM_E_SHAPE, "n_q * n_heads and n_k below 2^30");
+  if (n_q > 0 && (!q || !o)) return set_err(c, SWAM_E_INVALID, "q and o required");
+  if (n_k > 0 && (!k || !v)) return set_err(c, SWAM_E_INVALID, "k and v required");
+  const int64_t qw = (int64_t)n_heads * head_dim, kw = (int64_t)n_kv_heads * head_dim, es = ops_esz(c);
+  if (q_stride < qw || o_stride < qw || (n_k > 0 && (k_stride < kw || v_stride < kw)))
+    return set_err(c, SWAM_E_INVALID, "a row stride is smaller than its row");
+  if (std::max(std::max(q_stride, o_stride), std::max(k_stride, v_stride)) > OPS_MAX_STRIDE)
+    return set_err(c, SWAM_E_SHAPE, "row strides below 2^22");
+  if (!aligned16(q) || !aligned16(o) || !aligned16(k) || !aligned16(v) || q_stride * es % 16 ||
+      o_stride * es % 16 || (n_k > 0 && (k_stride * es % 16 || v_stride * es % 16)))
+    return set_err(c, SWAM_E_INVALID, "q, k, v, o and their rows must be 16-byte aligned");
+  if (!typed(lse, 4) || !typed(cu_q, 4) || !typed(cu_k, 4) || !typed(kv_seq, 4))
+    return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  const Span os = span(o, o_stride, n_q, qw, es), ls = span(lse, n_heads, n_q, n_heads, 4);
+  for (const Span& in : {span(q, q_stride, n_q, qw, es), span(k, k_stride, n_k, kw, es),
+                         span(v, v_stride, n_k, kw, es), span(key_mask, 1, n_k, 1, 1),
+                         span(cu_q, 1, n_seqs + 1, 1, 4), span(cu_k, 1, n_kv_seqs + 1, 1, 4),
+                         span(kv_seq, 1, n_seqs, 1, 4)})
+    if (meet(os, in) || meet(ls, in)) return set_err(c, SWAM_E_INVALID, "o or lse overlaps an input");
+  if (meet(os, ls)) return set_err(c, SWAM_E_INVALID, "o overlaps lse");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (n_q == 0) return SWAM_OK;
+  CrossArgs a{q, k, v, o, lse, key_mask, cu_q, cu_k, kv_seq, q_stride, k_stride, v_stride, o_stride,
+              n_seqs, n_kv_seqs, (int)n_q, (int)n_k, n_heads, n_kv_heads, head_dim, scale};
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_CROSS);
+  SWAM_HIP(c, launch_cross(c->cfg.dtype, a, c->ptr<float>(c->lay.splitk), c->dv.splitk_floats, c->st),
+           "cross_attention");
+  return SWAM_OK;
 }
 
 }  // extern "C"

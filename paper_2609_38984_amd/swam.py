@@ -22,7 +22,8 @@ FORCE_DENSE, FORCE_REFRESH = 1, 2
 KIND_DENSE, KIND_REFRESH, KIND_SPARSE = 0, 1, 2
 KIND_NONE, KIND_ANY = -1, -2   # timer slots outside any step / every slot
 TIMERS = ["ADALN", "LNMOD", "GEMM_QKV", "ATTN", "GEMM_OUT", "GEMM_UP", "GEMM_DOWN", "SCORE",
-          "REDUCE", "SELECT", "PACK", "UNPACK", "COPY", "SAMPLE", "QK_POST"]
+          "REDUCE", "SELECT", "PACK", "UNPACK", "COPY", "SAMPLE", "QK_POST", "QUANT", "GEMM_I8",
+          "CROSS"]
 T = {name: i for i, name in enumerate(TIMERS)}
 
 EXPORTS = ["swam_create", "swam_destroy", "swam_set_stream", "swam_plan", "swam_status_str",
@@ -33,6 +34,11 @@ EXPORTS = ["swam_create", "swam_destroy", "swam_set_stream", "swam_plan", "swam_
            "swam_timer_read_kind", "swam_embed", "swam_velocity",
            "swam_sample_update", "swam_sample_step", "swam_overlap", "swam_select_random",
            "swam_flow_sigmas", "swam_select_noalloc"]
+
+# include/swam_ops.h
+OP_EXPORTS = ["swam_rms_norm_i8", "swam_quantize_i8", "swam_gemm_i8", "swam_cross_attention"]
+I8_MAX_WIDTH, I8_MAX_K = 32768, 131056   # SWAM_I8_MAX_WIDTH, SWAM_I8_MAX_K
+GEMM_GELU = 1                            # SWAM_GEMM_GELU
 
 # the flow-schedule shift of the paper's backbones (App. B.2)
 SCHEDULE_SHIFT = 5.0
@@ -141,6 +147,11 @@ def load_library(path: str = LIB_PATH):
         "swam_sample_update": [P, I32, P, P, P, F, I32],
         "swam_sample_step": [P, C.POINTER(ModelStruct), C.POINTER(LatentIOStruct), P, P, P, P, P,
                              P, I32, F, I32, C.POINTER(I32)],
+        "swam_rms_norm_i8": [P, P, I64, P, I64, P, P, P, F, I64, I64, P, I64, P, I64, P],
+        "swam_quantize_i8": [P, P, I64, I64, I64, P, I64, P],
+        "swam_gemm_i8": [P, P, I64, P, P, I64, P, P, P, I64, P, I32, P, I64, I64, I64, I64],
+        "swam_cross_attention": [P, P, I64, P, I64, P, I64, P, P, P, P, I32, I32, I64, I64, I32, I32,
+                                 I32, F, P, I64, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -180,6 +191,25 @@ def _ptr(t, dtype=None, numel=None, name="tensor"):
     if numel is not None and t.numel() < numel:
         raise ValueError(f"{name} has {t.numel()} elements, needs {numel}")
     return t.data_ptr()
+
+
+def _rows(t, dtype, shape, name):
+    """Device pointer and row stride of a GPU tensor of `shape` whose rows are
+    contiguous (None -> NULL); the rows themselves may lie further apart."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    width = 1
+    for n, step in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and step != width:
+            raise ValueError(f"{name} must have contiguous rows")
+        width *= n
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else width
 
 
 class Model:
@@ -461,6 +491,85 @@ class Context:
             _ptr(temb, torch.float32, c.d_temb, "temb"), int(tau), float(dsigma), int(flags),
             C.byref(kind)))
         return kind.value
+
+    # -- 8-bit, encoder-conditioned block (include/swam_ops.h) -------------------------
+    def _here(self, **tensors):
+        """Every tensor lies on the context's device."""
+        for name, t in tensors.items():
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != self.stream.device:
+                raise ValueError(f"{name} is on {t.device}, the context on {self.stream.device}")
+
+    def rms_norm_i8(self, x, q, q_scale, residual=None, sum_out=None, gain=None, shift=None,
+                    scale=None, eps: float = 1e-6):
+        """q, q_scale = 8-bit codes of RMSnorm(x + residual) gain (1 + scale) + shift, a scale
+        per row.  x, residual, sum_out [rows][d] (sum_out receives x + residual and may be
+        either of them), gain [d] in the context's dtype; shift, scale float [d]; q int8
+        [rows][d]; q_scale float [rows]."""
+        self._here(x=x, q=q, q_scale=q_scale, residual=residual, sum_out=sum_out, gain=gain, shift=shift,
+                   scale=scale)
+        rows, d = x.shape
+        f32 = torch.float32
+        xp, xs = _rows(x, self.act_dtype, (rows, d), "x")
+        rp, rs = _rows(residual, self.act_dtype, (rows, d), "residual")
+        sp, ss = _rows(sum_out, self.act_dtype, (rows, d), "sum_out")
+        qp, qs = _rows(q, torch.int8, (rows, d), "q")
+        self._ok(self.lib.swam_rms_norm_i8(
+            self.h, xp, xs, rp, rs, _ptr(gain, self.act_dtype, d, "gain"), _ptr(shift, f32, d, "shift"),
+            _ptr(scale, f32, d, "scale"), float(eps), rows, d, sp, ss, qp, qs,
+            _ptr(q_scale, f32, rows, "q_scale")))
+
+    def quantize_i8(self, x, q, q_scale):
+        """q int8 [rows][d], q_scale float [rows] = 8-bit codes of the rows of x with a scale
+        each: activations per token, a weight [out][in] per output channel."""
+        self._here(x=x, q=q, q_scale=q_scale)
+        rows, d = x.shape
+        xp, xs = _rows(x, self.act_dtype, (rows, d), "x")
+        qp, qs = _rows(q, torch.int8, (rows, d), "q")
+        self._ok(self.lib.swam_quantize_i8(self.h, xp, xs, rows, d, qp, qs,
+                                           _ptr(q_scale, torch.float32, rows, "q_scale")))
+
+    def gemm_i8(self, a, a_scale, w, w_scale, c, bias=None, residual=None, gate=None, gelu: bool = False):
+        """c [m][n] = z, GELU(z) or residual + gate z with z = (a_scale a) (w_scale w)^T + bias:
+        a int8 [m][k], w int8 [n][k], a_scale float [m], w_scale float [n], bias [n] and
+        residual [m][n] (may be c) in the context's dtype, gate float [n]."""
+        self._here(a=a, a_scale=a_scale, w=w, w_scale=w_scale, c=c, bias=bias, residual=residual, gate=gate)
+        (m, k), n = a.shape, w.shape[0]
+        f32 = torch.float32
+        ap, lda = _rows(a, torch.int8, (m, k), "a")
+        wp, ldw = _rows(w, torch.int8, (n, k), "w")
+        rp, ldr = _rows(residual, self.act_dtype, (m, n), "residual")
+        cp, ldc = _rows(c, self.act_dtype, (m, n), "c")
+        self._ok(self.lib.swam_gemm_i8(
+            self.h, ap, lda, _ptr(a_scale, f32, m, "a_scale"), wp, ldw, _ptr(w_scale, f32, n, "w_scale"),
+            _ptr(bias, self.act_dtype, n, "bias"), rp, ldr, _ptr(gate, f32, n, "gate"),
+            GEMM_GELU if gelu else 0, cp, ldc, m, n, k))
+
+    def cross_attention(self, q, k, v, o, cu_q=None, cu_k=None, kv_seq=None, key_mask=None,
+                        scale: float | None = None, lse=None):
+        """o [n_q][heads][head_dim] = attention of the tokens q to the encoder states k, v
+        [n_k][kv_heads][head_dim].  cu_q, cu_k: int32 row offsets of the sequences (None: one
+        sequence); kv_seq: int32, the key sequence of each query sequence (None: its own);
+        key_mask: bool or uint8 [n_k], 0 hides a key; scale: 1 / sqrt(head_dim) by default;
+        lse float [n_q][heads] receives the normalisers."""
+        self._here(q=q, k=k, v=v, o=o, cu_q=cu_q, cu_k=cu_k, kv_seq=kv_seq, key_mask=key_mask, lse=lse)
+        (n_q, heads, dim), (n_k, kv_heads, _) = q.shape, k.shape
+        i32 = torch.int32
+        qp, qs = _rows(q, self.act_dtype, (n_q, heads, dim), "q")
+        kp, ks = _rows(k, self.act_dtype, (n_k, kv_heads, dim), "k")
+        vp, vs = _rows(v, self.act_dtype, (n_k, kv_heads, dim), "v")
+        op, os_ = _rows(o, self.act_dtype, (n_q, heads, dim), "o")
+        if key_mask is not None and key_mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"key_mask must be bool or uint8, got {key_mask.dtype}")
+        n_kv = 1 if cu_k is None else cu_k.numel() - 1
+        n_seqs = 1 if cu_q is None else cu_q.numel() - 1
+        if kv_seq is not None and kv_seq.numel() != n_seqs:
+            raise ValueError(f"kv_seq has {kv_seq.numel()} elements, needs {n_seqs}")
+        self._ok(self.lib.swam_cross_attention(
+            self.h, qp, qs, kp, ks, vp, vs, _ptr(key_mask, None, n_k, "key_mask"),
+            _ptr(cu_q, i32, None, "cu_q"), _ptr(cu_k, i32, None, "cu_k"), _ptr(kv_seq, i32, None, "kv_seq"),
+            n_seqs, n_kv, n_q, n_k, heads, kv_heads, dim,
+            float(dim ** -0.5 if scale is None else scale), op, os_,
+            _ptr(lse, torch.float32, n_q * heads, "lse")))
 
     # -- timers ------------------------------------------------------------------
     def timer_enable(self, classes, capacity=8192):

@@ -1,0 +1,706 @@
+"""The operators of swam_ops.h on the GPU against plain float64 forms, at the
+sizes, strides and masks where they can go wrong.  u = 2^-24 is half a step of
+float32 and h that of the storage type (bf16: 2^-8); every bound below is the
+count of such roundings on the way, written beside it."""
+import math
+
+import pytest
+import torch
+
+import workload as W
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+@pytest.fixture(scope="module")
+def contexts():
+    from paper_2609_38984_amd import swam
+    return {t: swam.Context(W.preset(2).replace(dtype=t, n_blocks=1)) for t in TYPES}
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def rows_of(shape, dtype, g, pad=0, std=1.0, fill=None):
+    """A normal tensor whose rows lie `pad` elements apart in a wider buffer, and
+    that buffer (its other elements hold `fill`)."""
+    buf = torch.full((shape[0], math.prod(shape[1:]) + pad), 0.0 if fill is None else fill, device="cuda",
+                     dtype=dtype)
+    view = buf[:, :math.prod(shape[1:])]
+    view.copy_((torch.randn(view.shape, device="cuda", generator=g) * std).to(dtype))
+    return view.unflatten(1, shape[1:]) if len(shape) > 2 else view, buf
+
+
+def same_outside(buf, view_cols, fill):
+    assert bool((buf[:, view_cols:] == fill).all())
+
+
+# ---------------------------------------------------------------------------
+# rows to codes
+# ---------------------------------------------------------------------------
+def exact_codes(x):
+    """Codes with ties to even and scales, from the definition in float64."""
+    top = x.abs().amax(1, keepdim=True)
+    c = torch.where(top > 0, torch.round(127.0 * x / top.clamp_min(1e-320)), torch.zeros_like(x))
+    return c, top[:, 0]
+
+
+WIDTHS = [(1, 1), (5, 7), (3, 64), (4, 512), (2, 520), (7, 1000), (1, 1536), (3, 2048), (2, 2056), (5, 4099),
+          (2, 6144), (3, 8192), (2, 8200), (2, 12001), (1, 32768), (1030, 130)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,d", WIDTHS)
+def test_quantise_codes_are_exact(contexts, dtype, rows, d):
+    dt = TYPES[dtype]
+    for pad in (0, 8, 3):
+        x, _ = rows_of((rows, d), dt, gen(rows + d + pad), pad)
+        x[0, d // 2] = 2.0 * x[0].abs().max()          # half of the largest: codes on a border
+        x[0, d // 3] = x[0].abs().max() / 2.0
+        q = torch.full((rows, d + pad), 77, dtype=torch.int8, device="cuda")
+        s = torch.empty(rows, device="cuda")
+        contexts[dtype].quantize_i8(x, q[:, :d], s)
+        c, top = exact_codes(x.double())
+        assert torch.equal(q[:, :d].double(), c)
+        assert torch.equal(s, (top / 127.0).float())
+        same_outside(q, d, 77)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [64, 100, 4096, 9000])
+def test_quantise_borders_zero_tiny_huge_and_non_finite_rows(contexts, dtype, d):
+    dt = TYPES[dtype]
+    x = torch.zeros((12, d), dtype=dt, device="cuda")
+    j = torch.arange(d, device="cuda")
+    x[1] = (j % 128 - 64).to(dt)                       # every odd half-code: 127 j / 64
+    x[1, 0] = 127.0 / 2                                # borders 63.5 c / 127 ...
+    x[2] = (((j * 37) % 255).double() - 127).to(dt) / 2
+    x[3, d - 1] = 1e-38
+    x[4] = (torch.randn(d, device="cuda", generator=gen(1)) * 1e-37).to(dt)
+    x[5] = (torch.randn(d, device="cuda", generator=gen(2)).clamp(-3, 3) * 1e38).to(dt)
+    x[6] = 1.0
+    x[6, d // 2] = float("nan")
+    x[7, 3] = float("inf")
+    x[8, d - 2] = float("-inf")
+    x[9] = -1.0
+    x[10] = (torch.rand(d, device="cuda", generator=gen(3)) * 2.0 ** -130).to(dt)
+    x[11, 0] = float("-nan")
+    q = torch.full((12, d), 5, dtype=torch.int8, device="cuda")
+    s = torch.empty(12, device="cuda")
+    contexts[dtype].quantize_i8(x, q, s)
+    fine = torch.isfinite(x).all(1)
+    c, top = exact_codes(x[fine].double())
+    assert torch.equal(q[fine].double(), c)
+    assert torch.equal(s[fine], (top / 127.0).float())
+    assert bool((q[~fine] == 0).all()) and bool(torch.isnan(s[~fine]).all()) and int((~fine).sum()) == 4
+    assert float(s[0]) == 0.0
+
+
+def norm_reference(x, r, gain, shift, scale, eps):
+    t = x.double() if r is None else x.double() + r.double()
+    y = t / torch.sqrt(t.square().mean(1, keepdim=True) + eps)
+    if gain is not None:
+        y = y * gain.double()
+    size = y.abs()
+    if shift is not None:
+        size = (y * (1 + scale.double())).abs() + shift.double().abs()
+        y = y * (1 + scale.double()) + shift.double()
+    return t, y, size.amax(1)
+
+
+def check_norm(t, y, size, q, s, total, dt):
+    if total is not None:
+        # one rounding to float32, one to the storage type
+        assert bool(((total.double() - t).abs() <= (HALF[dt] + 2 * U) * t.abs() + 1e-40).all())
+    top = y.abs().amax(1)
+    # y: at most 64 products in a row and 12 additions between lanes under a square
+    # root (38 u), a dozen more roundings: 64 u of the larger term of y
+    err = 64 * U * size
+    assert bool(((s.double() - top / 127).abs() <= err / 127 + 2 * U * top / 127).all())
+    live = top > 0
+    # a code is off by half a step, and by y's and the scale's errors in steps
+    step = torch.where(live, top / 127, torch.ones_like(top))[:, None]
+    off = (q.double() - y / step).abs()
+    assert bool((off <= 0.5 + 3 * (err[:, None] / step)).all())
+    assert bool((q.int().abs() <= 127).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,d", WIDTHS)
+def test_rms_norm_matches_float64(contexts, dtype, rows, d):
+    dt = TYPES[dtype]
+    for n, (res, gain, mod, pad) in enumerate([(1, 1, 1, 0), (1, 0, 0, 5), (0, 1, 1, 8), (0, 0, 0, 0)]):
+        g = gen(100 * n + rows + d)
+        x, _ = rows_of((rows, d), dt, g, pad)
+        r = rows_of((rows, d), dt, g, 2 * pad, 3.0)[0] if res else None
+        w = (1 + 0.3 * torch.randn(d, device="cuda", generator=g)).to(dt) if gain else None
+        sh, sc = (torch.randn((2, d), device="cuda", generator=g) * 0.4).unbind() if mod else (None, None)
+        q = torch.full((rows, d + pad), 77, dtype=torch.int8, device="cuda")
+        total = torch.full((rows, d + pad), 7.0, dtype=dt, device="cuda")
+        s = torch.empty(rows, device="cuda")
+        contexts[dtype].rms_norm_i8(x, q[:, :d], s, residual=r, sum_out=total[:, :d], gain=w, shift=sh, scale=sc)
+        check_norm(*norm_reference(x, r, w, sh, sc, 1e-6), q[:, :d], s, total[:, :d], dt)
+        same_outside(q, d, 77)
+        same_outside(total, d, 7.0)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d,pad", [(1536, 0), (130, 1), (5000, 0), (9000, 8)])
+def test_rms_norm_in_place_and_special_rows(contexts, dtype, d, pad):
+    dt = TYPES[dtype]
+    g = gen(d)
+    x0, _ = rows_of((9, d), dt, g, pad)
+    r0, _ = rows_of((9, d), dt, g, pad)
+    x0[1], r0[1] = 0.0, 0.0
+    x0[2] = -r0[2]                                     # the sum cancels to zeros
+    x0[3, 5] = float("nan")
+    r0[4, d - 1] = float("inf")
+    x0[5] = 1e30                                       # squares overflow float32
+    x0[6] *= 1e-12                                     # below eps
+    r0[6] = 0.0
+    bad = torch.tensor([0, 0, 0, 1, 1, 1, 0, 0, 0], dtype=torch.bool, device="cuda")
+    for place in ("x", "residual", "aside"):
+        x, r = x0.clone(), r0.clone()
+        total = {"x": x, "residual": r, "aside": torch.empty_like(x)}[place]
+        q = torch.empty((9, d), dtype=torch.int8, device="cuda")
+        s = torch.empty(9, device="cuda")
+        contexts[dtype].rms_norm_i8(x, q, s, residual=r, sum_out=total)
+        t, y, size = norm_reference(x0, r0, None, None, None, 1e-6)
+        check_norm(t[~bad], y[~bad], size[~bad], q[~bad], s[~bad], total[~bad], dt)
+        assert bool(torch.isnan(s[bad]).all()) and bool((q[bad] == 0).all())
+        assert bool((q[1:3] == 0).all()) and s[1:3].tolist() == [0.0, 0.0]
+        if place != "x":
+            assert torch.equal(x.view(torch.uint8), x0.clone().view(torch.uint8))
+    # without eps a row of zeros still has the scale 0
+    q = torch.full((9, d), 3, dtype=torch.int8, device="cuda")
+    contexts[dtype].rms_norm_i8(x0[1:2], q[1:2], s[1:2], eps=0.0)
+    assert float(s[1]) == 0.0 and bool((q[1] == 0).all())
+
+
+# ---------------------------------------------------------------------------
+# 8-bit product
+# ---------------------------------------------------------------------------
+def codes(rows, d, g, pad=0):
+    buf = torch.randint(-128, 128, (rows, d + pad), device="cuda", generator=g, dtype=torch.int8)
+    return buf[:, :d]
+
+
+def gelu64(z):
+    return z / (1 + torch.exp(-2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+
+
+def check_gemm(a, sa, w, sw, bias, res, gate, gelu, c):
+    p = (a.double() @ w.double().t().contiguous()) * sa.double()[:, None] * sw.double()
+    z = p if bias is None else p + bias.double()
+    # the sum to float32, the two scales' product, the product, the bias: 4 u
+    err = 3 * U * p.abs() + 2 * U * z.abs()
+    if gelu:
+        y = gelu64(z)
+        # its slope is below 1.13; exp of an argument with 4 roundings, a reciprocal, a product
+        arg = 2.31 * (z.abs() + 0.0448 * z.abs() ** 3)
+        err = 1.13 * err + y.abs() * (4 * arg + 8) * U + 1e-36
+    elif res is not None:
+        gt = torch.ones(w.shape[0], dtype=torch.float64, device="cuda") if gate is None else gate.double()
+        y = res.double() + gt * z
+        err = gt.abs() * err + 2 * U * y.abs()
+    else:
+        y = z
+    err = err + (HALF[c.dtype] * (1 + 2.0 ** -7)) * (y.abs() + err)
+    off = (c.double() - y).abs()
+    assert bool((off <= err).all()), float((off - err).max())
+
+
+GEMMS = [(1, 1, 16), (1, 1536, 1536), (2, 9, 48), (5, 200, 1040), (16, 512, 4096), (17, 130, 112), (32, 1000, 528),
+         (33, 257, 256), (64, 640, 2048), (100, 64, 16), (127, 129, 144), (128, 128, 128), (129, 1, 400),
+         (200, 1536, 1536), (256, 512, 8192), (300, 300, 304), (512, 768, 1536), (700, 520, 640), (1, 24, 131056),
+         (70, 40, 65536), (1312, 1024, 1024), (2000, 1537, 272)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k", GEMMS)
+def test_gemm_matches_float64(contexts, dtype, m, n, k):
+    dt = TYPES[dtype]
+    for i, (bias, res, gate, gelu, pad) in enumerate([(0, 0, 0, 0, 0), (1, 0, 0, 1, 16), (1, 1, 1, 0, 0),
+                                                      (0, 1, 0, 0, 32)]):
+        g = gen(1000 * i + m + n + k)
+        a, w = codes(m, k, g, pad), codes(n, k, g, 2 * pad)
+        sa = torch.rand(m, device="cuda", generator=g) * 0.02 + 1e-3
+        sw = (torch.rand(n, device="cuda", generator=g) + 0.1) * k ** -0.5 / 75
+        b = torch.randn(n, device="cuda", generator=g).to(dt) if bias else None
+        r = rows_of((m, n), dt, g, pad)[0] if res else None
+        gt = torch.randn(n, device="cuda", generator=g) if gate else None
+        # (the padded one starts between two 16-byte boundaries too)
+        buf = torch.full((m, n + pad + 1), 7.0, dtype=dt, device="cuda")
+        c = buf[:, :n] if pad or n % 8 else torch.full((m, n), 7.0, dtype=dt, device="cuda")
+        contexts[dtype].gemm_i8(a, sa, w, sw, c, bias=b, residual=r, gate=gt, gelu=bool(gelu))
+        check_gemm(a, sa, w, sw, b, r, gt, gelu, c)
+        same_outside(buf, n, 7.0)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gemm_extreme_codes_in_place_and_nan_scales(contexts, dtype):
+    dt = TYPES[dtype]
+    ctx = contexts[dtype]
+    # the largest sum that 32 bits hold: 131,056 products of 128 * 128
+    a = torch.full((3, 131056), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((40, 131056), -128, dtype=torch.int8, device="cuda")
+    one = torch.ones(40, device="cuda")
+    c = torch.empty((3, 40), dtype=dt, device="cuda")
+    ctx.gemm_i8(a, one[:3], w, one, c)
+    assert torch.equal(c, torch.full_like(c, 131056.0 * 16384))
+    w[1::2] = 127
+    ctx.gemm_i8(a, one[:3], w, one, c)
+    assert torch.equal(c[:, 1::2], torch.full((3, 20), -131056.0 * 128 * 127, device="cuda").to(dt))
+    # into the residual itself; a token whose scale is NaN is NaN, its neighbours are not
+    g = gen(5)
+    a, w = codes(200, 256, g), codes(96, 256, g)
+    sa, sw = torch.rand(200, device="cuda", generator=g), torch.rand(96, device="cuda", generator=g) * 1e-3
+    sa[17] = float("nan")
+    r = rows_of((200, 96), dt, g)[0]
+    want = torch.empty_like(r)
+    ctx.gemm_i8(a, sa, w, sw, want, residual=r)
+    ctx.gemm_i8(a, sa, w, sw, r, residual=r)
+    assert bool(torch.isnan(r[17]).all()) and int(torch.isnan(r).any(1).sum()) == 1
+    assert torch.equal(torch.nan_to_num(r), torch.nan_to_num(want))
+    # empty products
+    ctx.gemm_i8(a[:0], sa[:0], w, sw, r[:0])
+    ctx.gemm_i8(a, sa, w[:0], sw[:0], torch.empty((200, 0), dtype=dt, device="cuda"))
+
+
+# ---------------------------------------------------------------------------
+# cross attention
+# ---------------------------------------------------------------------------
+def offsets(n):
+    return torch.tensor([0] + list(n), device="cuda").cumsum(0).to(torch.int32)
+
+
+def attend64(q, k, v, scale):
+    """o, lse and the sums of p |v| and of |q| |k| of one sequence and head, in float64."""
+    x = (q @ k.t().contiguous()) * scale
+    m = x.amax(1, keepdim=True)
+    p = torch.exp(x - m)
+    l = p.sum(1, keepdim=True)
+    size = ((q.abs() @ k.abs().t().contiguous()) * scale).amax(1)
+    return (p / l) @ v, (m + torch.log(l))[:, 0], (p / l) @ v.abs(), size
+
+
+def check_attention(q, k, v, o, lse, lq, lk, of, mask, scale, o_before, lse_before):
+    heads, kvh, dim = q.shape[1], k.shape[1], q.shape[2]
+    group = heads // kvh
+    h, at = HALF[q.dtype], 0
+    starts = [sum(lk[:i]) for i in range(len(lk))]
+    for i, n in enumerate(lq):
+        rows = slice(at, at + n)
+        at += n
+        if not 0 <= of[i] < len(lk):
+            keys = torch.zeros(0, dtype=torch.long, device="cuda")
+        else:
+            keys = torch.arange(starts[of[i]], starts[of[i]] + lk[of[i]], device="cuda")
+            if mask is not None:
+                keys = keys[mask[keys] != 0]
+        if n == 0:
+            continue
+        if keys.numel() == 0:
+            assert bool((o[rows] == 0).all())
+            assert lse is None or bool((lse[rows] == -math.inf).all())
+            continue
+        for j in range(heads):
+            want, wl, size, qk = attend64(q[rows, j].double(), k[keys, j // group].double(),
+                                          v[keys, j // group].double(), scale)
+            # a logit: dim products and sums in float32 (twice u for the matrix unit), the
+            # scale and the maximum; then exp2.  Sums over the keys: one rounding per key.
+            lerr = (2 * (dim + 8) * U * qk + 8 * U * wl.abs())[:, None]
+            sums = (keys.numel() + 16) * U
+            err = (h + 2 * lerr + 2 * sums) * 1.01 * size
+            err = err + (h + 4 * U) * (want.abs() + err)
+            assert bool(((o[rows, j].double() - want).abs() <= err).all()), (i, j)
+            if lse is not None:
+                lse_err = 1.01 * (lerr[:, 0] + sums) + 4 * U * wl.abs()
+                assert bool(((lse[rows, j].double() - wl).abs() <= lse_err).all()), (i, j)
+    # rows behind the last sequence
+    assert torch.equal(o[at:], o_before[at:])
+    assert lse is None or torch.equal(lse[at:], lse_before[at:])
+
+
+def run_attention(ctx, dt, lq, lk, heads, kvh, dim, seed, of=None, mask=None, behind=3, pad=0, std=1.0, scale=None,
+                  fused=True, want_lse=True, garbage=True):
+    g = gen(seed)
+    n_q, n_k = sum(lq) + behind, sum(lk) + behind
+    q, _ = rows_of((n_q, heads, dim), dt, g, pad, std)
+    if fused:
+        kv = torch.randn((n_k, 2, kvh, dim), device="cuda", generator=g).mul_(std).to(dt)
+        k, v = kv[:, 0], kv[:, 1]
+    else:
+        k, _ = rows_of((n_k, kvh, dim), dt, g, 0, std)
+        v, _ = rows_of((n_k, kvh, dim), dt, g, pad)
+    m = None
+    if mask is not None:
+        m = mask(n_k, g)
+        if garbage:
+            k[m == 0], v[m == 0] = float("nan"), float("inf")
+    k[sum(lk):], v[sum(lk):] = float("nan"), float("nan")   # behind the last sequence
+    o, obuf = rows_of((n_q, heads, dim), dt, g, pad, fill=7.0)
+    lse = torch.randn((n_q, heads), device="cuda", generator=g) if want_lse else None
+    before = o.clone(), None if lse is None else lse.clone()
+    of_t = None if of is None else torch.tensor(of, dtype=torch.int32, device="cuda")
+    ctx.cross_attention(q, k, v, o, cu_q=offsets(lq), cu_k=offsets(lk), kv_seq=of_t, key_mask=m, lse=lse,
+                        scale=scale)
+    check_attention(q, k, v, o, lse, lq, lk, list(range(len(lq))) if of is None else of, m,
+                    dim ** -0.5 if scale is None else scale, *before)
+    same_outside(obuf, heads * dim, 7.0)
+    return o
+
+
+def pad_mask(n, g):
+    m = torch.zeros(n, dtype=torch.bool, device="cuda")
+    m[: max(1, 2 * n // 3)] = True
+    return m
+
+
+def holes(n, g):
+    return (torch.rand(n, device="cuda", generator=g) < 0.5).to(torch.uint8) * 255
+
+
+def lone(n, g):
+    m = torch.zeros(n, dtype=torch.bool, device="cuda")
+    m[n // 2] = True
+    return m
+
+
+def hidden(n, g):
+    return torch.zeros(n, dtype=torch.bool, device="cuda")
+
+
+SHAPES = {
+    "one_key": ([1], [1], 1, 1, 64), "one_query_long": ([1], [5000], 3, 3, 64),
+    "one_query_group": ([1], [1537], 14, 2, 128), "tokens_of_8": ([1] * 8, [700] * 8, 4, 4, 64),
+    "prompt_77": ([326], [77], 5, 5, 64), "odd": ([129, 1, 63], [65, 64, 1], 3, 1, 64),
+    "empty_sequences": ([0, 5, 0, 40], [3, 0, 9, 130], 2, 2, 64), "group_7": ([37, 70], [200, 31], 7, 1, 64),
+    "wide_head": ([300], [513], 4, 2, 128), "wide_odd": ([31, 33, 257], [129, 63, 1], 6, 3, 128),
+    "many_tiles": ([1000], [300], 4, 4, 64), "sixty_four": ([3] * 64, [17] * 64, 2, 1, 64),
+    "few_long": ([9, 20], [3001, 2000], 2, 2, 128), "small_group_long": ([6], [9999], 8, 4, 64),
+    "mid_batch": ([200, 150, 40], [600, 512, 700], 8, 8, 64),
+}
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_cross_attention_matches_float64(contexts, dtype, name):
+    lq, lk, heads, kvh, dim = SHAPES[name]
+    for i, (mask, pad, fused, want_lse) in enumerate([(None, 0, True, True), (pad_mask, 8, False, True),
+                                                      (holes, 0, True, False)]):
+        run_attention(contexts[dtype], TYPES[dtype], lq, lk, heads, kvh, dim, 10 * i + len(name), mask=mask, pad=pad,
+                      fused=fused, want_lse=want_lse)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("mask", [lone, hidden])
+@pytest.mark.parametrize("name", ["one_query_long", "odd", "wide_head", "many_tiles", "few_long", "mid_batch"])
+def test_cross_attention_masks_that_leave_little_or_nothing(contexts, dtype, name, mask):
+    lq, lk, heads, kvh, dim = SHAPES[name]
+    run_attention(contexts[dtype], TYPES[dtype], lq, lk, heads, kvh, dim, 3, mask=mask)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("lq", [[1] * 5, [150, 3, 80, 260, 1]])
+def test_cross_attention_shared_prompts(contexts, dtype, lq):
+    """Sequences that share a prompt, one whose index is out of range on either
+    side, and more prompts than sequences."""
+    run_attention(contexts[dtype], TYPES[dtype], lq, [400, 90, 700], 4, 2, 64, 11, of=[2, 0, 2, -1, 3], mask=pad_mask)
+    run_attention(contexts[dtype], TYPES[dtype], lq[:2], [40, 90, 70, 10], 4, 2, 128, 12, of=[3, 0])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("scale,std", [(0.5, 1.5), (1.0, 3.0), (1e-3, 1.0), (0.125, 6.0)])
+@pytest.mark.parametrize("lq", [[1], [70]])
+def test_cross_attention_peaked_and_flat_weights(contexts, dtype, scale, std, lq):
+    """The running maximum moves again and again, or never."""
+    run_attention(contexts[dtype], TYPES[dtype], lq, [1500], 3, 3, 64, 21, scale=scale, std=std)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_cross_attention_one_sequence_without_offsets_and_no_keys(contexts, dtype):
+    dt, ctx, g = TYPES[dtype], contexts[dtype], gen(31)
+    q, _ = rows_of((70, 4, 64), dt, g)
+    kv = torch.randn((2, 90, 4, 64), device="cuda", generator=g).to(dt)
+    o, o2, lse = torch.empty_like(q), torch.empty_like(q), torch.empty((70, 4), device="cuda")
+    ctx.cross_attention(q, kv[0], kv[1], o, lse=lse)
+    ctx.cross_attention(q, kv[0], kv[1], o2, cu_q=offsets([70]), cu_k=offsets([90]))
+    assert torch.equal(o, o2)
+    check_attention(q, kv[0], kv[1], o, lse, [70], [90], [0], None, 0.125, o, lse)
+    ctx.cross_attention(q, kv[0, :0], kv[1, :0], o, lse=lse)
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
+    ctx.cross_attention(q[:0], kv[0], kv[1], o[:0])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_cross_attention_offsets_are_clamped(contexts, dtype):
+    """Offsets past the tensors end at them, falling ones make empty sequences."""
+    dt, ctx, g = TYPES[dtype], contexts[dtype], gen(33)
+    q, _ = rows_of((20, 2, 64), dt, g)
+    k, v = rows_of((50, 2, 64), dt, g)[0], rows_of((50, 2, 64), dt, g)[0]
+    o = torch.full_like(q, 7.0)
+    lse = torch.full((20, 2), 7.0, device="cuda")
+    cu_q = torch.tensor([-5, 8, 8, 1 << 30], dtype=torch.int32, device="cuda")
+    cu_k = torch.tensor([-9, 30, 20, 1 << 30], dtype=torch.int32, device="cuda")
+    ctx.cross_attention(q, k, v, o, cu_q=cu_q, cu_k=cu_k, lse=lse)
+    a, b = torch.empty_like(o), torch.empty_like(lse)
+    ctx.cross_attention(q[:8], k[:30], v[:30], a[:8], lse=b[:8])
+    ctx.cross_attention(q[8:], k[20:], v[20:], a[8:], lse=b[8:])
+    for x, y, tol in ((o, a, 2 * HALF[dt]), (lse, b, 64 * U)):
+        assert bool(((x - y).double().abs() <= tol * (1 + y.double().abs())).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_cross_attention_beyond_4_gb_of_keys(contexts, dtype):
+    """The last keys of a cache whose byte offsets pass 32 bits."""
+    dt, g = TYPES[dtype], gen(35)
+    ld = 1 << 20
+    n_k = (5 << 30) // (ld * (2 if dt == torch.bfloat16 else 4)) + 3
+    buf = torch.zeros((n_k, ld), dtype=dt, device="cuda")
+    k, v = buf[:, :64].unflatten(1, (1, 64)), buf[:, -64:].unflatten(1, (1, 64))
+    k.copy_(torch.randn(k.shape, device="cuda", generator=g).to(dt))
+    v.copy_(torch.randn(v.shape, device="cuda", generator=g).to(dt))
+    q, _ = rows_of((40, 1, 64), dt, g)
+    o, lse = torch.empty_like(q), torch.empty((40, 1), device="cuda")
+    contexts[dtype].cross_attention(q, k, v, o, lse=lse)
+    check_attention(q, k, v, o, lse, [40], [n_k], [0], None, 0.125, o, lse)
+    cu = torch.tensor([n_k - 70, n_k], dtype=torch.int32, device="cuda")
+    contexts[dtype].cross_attention(q, k, v, o, cu_q=offsets([40]), cu_k=cu, lse=lse)
+    check_attention(q, k[-70:], v[-70:], o, lse, [40], [70], [0], None, 0.125, o, lse)
+
+
+# ---------------------------------------------------------------------------
+# how they are called
+# ---------------------------------------------------------------------------
+def test_refusals_launch_nothing(contexts):
+    from paper_2609_38984_amd import swam
+    ctx = contexts["bf16"]
+    x = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
+    q, s = torch.full((4, 64), 9, dtype=torch.int8, device="cuda"), torch.full((4,), 9.0, device="cuda")
+    for bad in (dict(x=x.float()), dict(q=q.to(torch.uint8)), dict(x=x[:, ::2]), dict(q=q[:3]), dict(x=x.cpu()),
+                dict(q_scale=s[:3]), dict(q_scale=s.double())):
+        a = dict(x=x, q=q, q_scale=s)
+        a.update(bad)
+        with pytest.raises((TypeError, ValueError)):
+            ctx.quantize_i8(**a)
+        with pytest.raises((TypeError, ValueError)):
+            ctx.rms_norm_i8(**a)
+    with pytest.raises(swam.SwamError, match="SWAM_E_INVALID.*together"):
+        ctx.rms_norm_i8(x, q, s, shift=torch.zeros(64, device="cuda"))
+    c = torch.full((4, 4), 9.0, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(swam.SwamError, match="SWAM_E_SHAPE.*multiple of 16"):
+        ctx.gemm_i8(q[:, :40], s, q[:, :40], s, c)
+    with pytest.raises(swam.SwamError, match="SWAM_E_UNSUPPORTED"):
+        ctx.gemm_i8(q, s, q, s, c, residual=c, gelu=True)
+    with pytest.raises(ValueError):
+        ctx.gemm_i8(q, s, q[:, :48], s, c)
+    with pytest.raises(TypeError):
+        ctx.gemm_i8(q, s, q, s, c.float())
+    t = torch.full((4, 1, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros_like(t)
+    for bad in (dict(v=k[:3]), dict(o=t[:, :, :32]), dict(key_mask=torch.zeros(4, device="cuda")),
+                dict(key_mask=torch.zeros(3, dtype=torch.bool, device="cuda")), dict(kv_seq=offsets([1])),
+                dict(cu_q=torch.zeros(2, dtype=torch.int64, device="cuda")), dict(lse=s[:3])):
+        a = dict(q=k, k=k.clone(), v=k.clone(), o=t)
+        a.update(bad)
+        with pytest.raises((TypeError, ValueError)):
+            ctx.cross_attention(**a)
+    with pytest.raises(swam.SwamError, match="overlaps"):
+        ctx.cross_attention(t, t, t, t)
+    torch.cuda.synchronize()
+    assert bool((q == 9).all()) and bool((s == 9).all()) and bool((c == 9).all()) and bool((t == 9).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_results_repeat_bit_for_bit_and_do_not_depend_on_the_workspace(contexts, dtype):
+    """Twice the same call gives the same bits; a context whose workspace holds
+    few partial sums takes other splits within the same bounds."""
+    from paper_2609_38984_amd import swam
+    dt = TYPES[dtype]
+    small = swam.Context(W.preset(1).replace(dtype=dtype, d_model=64, n_heads=1))
+    g = gen(41)
+    a, w = codes(9, 4096, g), codes(520, 4096, g)
+    sa, sw = torch.rand(9, device="cuda", generator=g), torch.rand(520, device="cuda", generator=g)
+    c = [torch.empty((9, 520), dtype=dt, device="cuda") for _ in range(3)]
+    contexts[dtype].gemm_i8(a, sa, w, sw, c[0])
+    contexts[dtype].gemm_i8(a, sa, w, sw, c[1])
+    small.gemm_i8(a, sa, w, sw, c[2])
+    assert torch.equal(c[0], c[1]) and torch.equal(c[0], c[2])       # integer sums
+    for lq, lk, heads in (([1] * 3, [4000] * 3, 6), ([300], [2500], 4)):
+        o1 = run_attention(contexts[dtype], dt, lq, lk, heads, heads, 64, 43)
+        o2 = run_attention(contexts[dtype], dt, lq, lk, heads, heads, 64, 43)
+        assert torch.equal(o1, o2)
+        run_attention(small, dt, lq, lk, heads, heads, 64, 43)
+
+
+def sublayer(ctx, s, out):
+    """The cross-attention sublayer of a block on 8-bit projections, its MLP up
+    projection behind it."""
+    ctx.rms_norm_i8(s.x, s.codes, s.cs, gain=s.gain, shift=s.shift, scale=s.scale)
+    ctx.gemm_i8(s.codes, s.cs, s.wq, s.wqs, s.q.flatten(1), bias=s.bq)
+    ctx.cross_attention(s.q, s.k, s.v, s.o, cu_q=s.cu_q, cu_k=s.cu_k, key_mask=s.mask)
+    ctx.quantize_i8(s.o.flatten(1), s.codes, s.cs)
+    ctx.gemm_i8(s.codes, s.cs, s.wo, s.wos, s.y, bias=s.bo, residual=s.x, gate=s.gate)
+    ctx.rms_norm_i8(s.y, s.codes, s.cs, residual=s.x, sum_out=out["sum"], gain=s.gain)
+    ctx.gemm_i8(s.codes, s.cs, s.wu, s.wus, out["up"], gelu=True)
+    out["y"].copy_(s.y)
+
+
+class State:
+    pass
+
+
+def sublayer_state(ctx, dt, seed, lq, lk, heads=4):
+    g, s, d = gen(seed), State(), heads * 64
+    n_q, n_k = sum(lq), sum(lk)
+
+    def normal(*shape, std=1.0, dtype=dt):
+        return torch.randn(shape, device="cuda", generator=g).mul_(std).to(dtype)
+
+    def weight(n):
+        w = normal(n, d, std=d ** -0.5)
+        q, sc = torch.empty((n, d), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        ctx.quantize_i8(w, q, sc)
+        return q, sc
+
+    s.x, s.gain, s.bq, s.bo = normal(n_q, d), normal(d), normal(d), normal(d)
+    s.shift, s.scale, s.gate = normal(3, d, std=0.3, dtype=torch.float32).unbind()
+    (s.wq, s.wqs), (s.wo, s.wos), (s.wu, s.wus) = weight(d), weight(d), weight(2 * d)
+    kv = normal(n_k, 2, heads, 64)
+    s.k, s.v = kv[:, 0], kv[:, 1]
+    s.mask = torch.rand(n_k, device="cuda", generator=g) < 0.7
+    s.cu_q, s.cu_k, s.lq, s.lk = offsets(lq), offsets(lk), lq, lk
+    s.codes, s.cs = torch.empty((n_q, d), dtype=torch.int8, device="cuda"), torch.empty(n_q, device="cuda")
+    s.q, s.o, s.y = torch.empty((n_q, heads, 64), dtype=dt, device="cuda"), normal(n_q, heads, 64), normal(n_q, d)
+    return s
+
+
+def sublayer_out(s):
+    n, d = s.x.shape
+    return {"y": torch.empty_like(s.x), "sum": torch.empty_like(s.x),
+            "up": torch.empty((n, 2 * d), dtype=s.x.dtype, device="cuda")}
+
+
+def sublayer64(s):
+    """The same in float64, each tensor that is stored between two calls taken
+    from the run (so that every call is held to its own error)."""
+    d = s.x.shape[1]
+    heads = d // 64
+    x = s.x.double()
+    y = x / torch.sqrt(x.square().mean(1, keepdim=True) + 1e-6) * s.gain.double() * (1 + s.scale.double()) + s.shift.double()
+    q = (y @ (s.wq.double() * s.wqs.double()[:, None]).t().contiguous() + s.bq.double()).reshape(-1, heads, 64)
+    o = torch.zeros_like(q)
+    for i in range(len(s.lq)):
+        rows = slice(int(s.cu_q[i]), int(s.cu_q[i + 1]))
+        keys = torch.arange(int(s.cu_k[i]), int(s.cu_k[i + 1]), device="cuda")
+        keys = keys[s.mask[keys]]
+        for j in range(heads):
+            if keys.numel():
+                o[rows, j] = attend64(q[rows, j], s.k[keys, j].double(), s.v[keys, j].double(), 0.125)[0]
+    z = o.flatten(1) @ (s.wo.double() * s.wos.double()[:, None]).t().contiguous() + s.bo.double()
+    y = x + s.gate.double() * z
+    t = x + y
+    n = t / torch.sqrt(t.square().mean(1, keepdim=True) + 1e-6) * s.gain.double()
+    up = gelu64(n @ (s.wu.double() * s.wus.double()[:, None]).t().contiguous())
+    return {"y": y, "sum": t, "up": up}
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("lq,lk", [([50, 1, 200], [77, 30, 128]), ([1, 1, 1, 1], [300] * 4), ([700], [512])])
+def test_the_sublayer_as_a_whole(contexts, dtype, lq, lk):
+    """Codes have a step of 1/127 of a row's largest value (about 1/35 of its
+    root mean square): a normal row's error is 1/35 / sqrt(12) = 0.8% of it, two
+    such roundings lie before q and before the out projection, one before up, and
+    attention and GELU do not enlarge it by more than twice: 5% in the 2-norm."""
+    s = sublayer_state(contexts[dtype], TYPES[dtype], 51, lq, lk)
+    out = sublayer_out(s)
+    sublayer(contexts[dtype], s, out)
+    want = sublayer64(s)
+    for name, w in want.items():
+        rel = float((out[name].double() - w).norm() / w.norm())
+        print(f"  {dtype} {lq} {name}: {rel:.2e}", flush=True)
+        assert rel < 0.05, name
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_replayed_and_on_other_streams(contexts, dtype):
+    """The sublayer captured once and replayed with eager work of the same context
+    in between, on a stream of its own, gives the eager bits every time, for new
+    inputs in the same buffers too; a second graph of the same context follows."""
+    from paper_2609_38984_amd import swam
+    dt = TYPES[dtype]
+    stream = torch.cuda.Stream()
+    ctx = swam.Context(W.preset(2).replace(dtype=dtype, n_blocks=1), stream)
+    shapes = [([1, 1, 40], [900, 77, 300]), ([64], [1500])]
+    states = [sublayer_state(contexts[dtype], dt, 61 + i, *sh) for i, sh in enumerate(shapes)]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for s in states:
+        out = sublayer_out(s)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            sublayer(ctx, s, out)
+        graphs.append(g)
+        outs.append(out)
+    for turn in range(4):
+        for s, g, out in zip(states, graphs, outs):
+            s.x.copy_(torch.randn(s.x.shape, device="cuda", generator=gen(70 + turn)).to(dt))
+            want = sublayer_out(s)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                g.replay()
+                kept = {n: t.clone() for n, t in out.items()}
+                sublayer(ctx, s, want)                 # eager, same stream
+            torch.cuda.synchronize()
+            for n in want:
+                assert torch.equal(kept[n], want[n]), (turn, n)
+    # the context moves to another stream in the middle of a run
+    s, want = states[0], outs[0]
+    torch.cuda.synchronize()
+    other, got = torch.cuda.Stream(), sublayer_out(states[0])
+    with torch.cuda.stream(stream):
+        sublayer(ctx, s, want)
+    ctx.set_stream(other)
+    with torch.cuda.stream(other):
+        sublayer(ctx, s, got)
+    torch.cuda.synchronize()
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+
+
+def test_steps_and_operators_share_a_context(contexts):
+    """A step of the model between two operator calls leaves both as they were
+    (they use one workspace in turn), and the timers see the operators."""
+    from helpers import dev, model_for
+    from paper_2609_38984_amd import swam
+    cfg = W.preset(2).replace(n_blocks=2)
+    blocks, _, model = model_for(cfg)
+    inp = W.make_inputs(cfg, blocks[0]["w_qkv"])
+    ctx = swam.Context(cfg)
+    x = dev(inp.x(0), torch.bfloat16)
+    temb = dev(inp.temb(0))
+    y = [torch.empty_like(x) for _ in range(2)]
+    s = sublayer_state(ctx, torch.bfloat16, 81, [1, 30], [2000, 300])
+    out = [sublayer_out(s) for _ in range(2)]
+    ctx.timer_enable(["QUANT", "GEMM_I8", "CROSS"], 64)
+    for i in range(2):
+        sublayer(ctx, s, out[i])
+        ctx.step(model, x, temb, 0, y[i])
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1])
+    for n in out[0]:
+        assert torch.equal(out[0][n], out[1][n]), n
+    assert ctx.timer_read("QUANT")[0] == 6 and ctx.timer_read("GEMM_I8")[0] == 6 and ctx.timer_read("CROSS")[0] == 2
