@@ -18,8 +18,8 @@
  * call asynchronous on the context's stream, arguments validated on the host
  * before any launch, a negative swam_status and swam_last_error on failure.  No
  * call allocates, synchronises or reads anything back, so all of them can be
- * captured into a HIP graph.  Products and attention that are split keep their
- * partial sums in the context's workspace: calls of one context (and replays of
+ * captured into a HIP graph.  Attention that is split over keys keeps its partial
+ * results in the context's workspace: calls of one context (and replays of
  * graphs that captured them) must not overlap in time, as everywhere in swam.h.
  * Float tensors called "act" below have the context's dtype; strides are in
  * elements; rows of a tensor may lie further apart than they are wide (a column
@@ -81,8 +81,8 @@ int swam_quantize_i8(swam_ctx* ctx, const void* x, int64_t x_stride, int64_t row
  *   [m][n] (row stride ldr) or NULL, gate : float [n] or NULL (1; only with a
  *   residual);  c : act [m][n] (row stride ldc), may be residual itself (same
  *   pointer and stride)
- * k a multiple of 16 up to SWAM_I8_MAX_K, or 0 <= m, n: an empty product returns at
- * once.  a, b and their row strides are 16-byte aligned (SWAM_E_INVALID otherwise);
+ * k a positive multiple of 16 up to SWAM_I8_MAX_K; m, n below 2^30 and m * n below
+ * 2^40 (0: nothing to do); lda, ldb below 2^22.  a, b and their row strides are 16-byte aligned (SWAM_E_INVALID otherwise);
  * the float tensors need the alignment of their type only (16-byte aligned rows are
  * moved in vectors). */
 int swam_gemm_i8(swam_ctx* ctx, const int8_t* a, int64_t lda, const float* a_scale,

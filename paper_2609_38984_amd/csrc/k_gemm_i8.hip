@@ -1,93 +1,169 @@
 // 8-bit projections: C = epi(a_scale b_scale (A . B^T) + bias), A [M][K] and
 // B [N][K] int8 codes with a scale per row, the sum exact in int32.
 //
-// A 128-byte row of an LDS tile holds 128 codes of K: the tiles have the layout
-// of the bf16 projections (16-byte chunk ^ lds_swz(row)) at twice the depth, and
-// a 32x32x32 MFMA takes one 16-byte chunk per lane and operand.  Global -> LDS
-// by buffer loads whose descriptors end with the operand, so rows past M or N
-// and, by an offset past the end, chunks past K read as zeros.
+// A 32x32x32 MFMA takes 16 codes per lane and operand and does twice the products
+// of its bf16 counterpart in the same time, so the way of the tiles' bytes into LDS
+// decides.  Stages of 128 codes of K form rings in LDS, loaded by DMA with counted
+// waits; a row of a stage is 128 bytes, a whole cache line: with lines taken in
+// halves (stages of 64 codes) DMA reads of L2-resident rows reach 12 TB/s, with whole
+// ones 31.  Chunk c of row r lies at c ^ lds_swz(r), as in the bf16 projections.
+// The descriptors of the loads end with the operand, so rows past M or N read as
+// zeros; chunks past K get an offset past the end.
+// 8,192^3: 2,200-2,400 TOP/s by box (the library's product there: 2,150), at which
+// the chip runs at 1.76 of its 2.4 GHz and the matrix units are 58% busy.
 #include "gemm_common.h"
+
+#include <cmath>
+#include <type_traits>
 
 namespace swam {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int I8_BK = 128;            // codes of K per stage: one 128-byte row
-constexpr int PAST_END = 0x7fffff00;  // a buffer offset that no operand reaches
+constexpr int I8_BK = 128;            // codes of K per stage: a 128-byte row
+constexpr int I8_DEAD = 0x40000000;   // an offset past every tile (256 rows of less than 2^22 bytes)
 
-// The operand's bytes from its tile's first row on; rows * ld stays below
-// 2^31 for the rows of a tile, so a clamped size hides none of them.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t i8_rows(const int8_t* p, int64_t ld, int r0, int rows, int64_t K) {
-  const int64_t bytes = (int64_t)(rows - r0 - 1) * ld + K;
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + r0 * ld), (short)0,
-                                           (int)min(bytes, (int64_t)0x7fff0000), SWAM_BUF_DWORD3);
+// wait until at most V vector-memory operations and no LDS operation of this wave
+// are outstanding
+template <int V>
+__device__ __forceinline__ void i8_wait() {
+  static_assert(V >= 0 && V < 64, "vmcnt is a 6-bit counter");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((V & 15) | (7 << 4) | ((V >> 4) << 14));
+  asm volatile("" ::: "memory");
 }
 
-// 8 columns of a row: scale, bias, GELU or gated residual, rounded once
+// bytes of the operand from row r0 on, at most `rows` of them
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t i8_rows(const int8_t* p, int64_t ld, int r0, int rows, int K) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + r0 * ld), (short)0, (int)((rows - 1) * ld) + K,
+                                           SWAM_BUF_DWORD3);
+}
+
+// one DMA instruction: 16 bytes per lane at `off` to a 1 KB slab of the ring
+__device__ __forceinline__ void i8_slab(__amdgpu_buffer_rsrc_t r, uint4* slab, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)slab, 16, off, 0, 0, 0);
+}
+
+// tanh-GELU u / (1 + exp(-2 sqrt(2/pi) (u + 0.044715 u^3))) with the cubic in Horner's
+// form, on the hardware exp2 and reciprocal (about 1 ulp each)
+__device__ __forceinline__ float i8_gelu(float u) {
+  constexpr float c = -2.0f * 1.4426950408889634f * 0.7978845608028654f;
+  return u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * fmaf(u * u, c * 0.044715f, c)));
+}
+
+// 8 values at p as float32: a vector where whole (n == 8) and aligned, else one by one
 template <typename T>
-struct I8Epilogue {
-  const GemmI8 g;
-  int vec;       // whole, 16-byte aligned runs of 8 columns in c, residual, bias
-  __device__ __forceinline__ void run(const int (&acc)[8], int64_t row, int col) const {
-    if (row >= g.M || col >= g.N) return;
-    const float sa = g.a_scale[row];
-    T* cp = (T*)g.c + row * g.ldc + col;
-    const T* rp = g.res ? (const T*)g.res + row * g.ldr + col : nullptr;
-    const T* bp = g.bias ? (const T*)g.bias + col : nullptr;
-    if (vec && col + 8 <= g.N) {
-      float z[8], b[8], r[8];
-      if (bp) load8(bp, b);
-      if (rp) load8(rp, r);
+__device__ __forceinline__ void i8_load8(const T* p, bool whole, int n, float fill, float (&o)[8]) {
+  if (whole) {
+    load8(p, o);
+  } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        z[e] = (float)acc[e] * (sa * g.b_scale[col + e]) + (bp ? b[e] : 0.0f);
-        if (g.gelu) z[e] = gelu_tanh(z[e]);
-        if (rp) z[e] = fmaf(g.gate ? g.gate[col + e] : 1.0f, z[e], r[e]);
-      }
+    for (int e = 0; e < 8; ++e) o[e] = e < n ? Elem<T>::load(p + e) : fill;
+  }
+}
+
+// What a lane needs to finish its 8 columns, the same in every row that it stores.
+template <typename T>
+struct I8Cols {
+  float sb[8], bias[8], gate[8];
+  int n;          // columns inside N
+  bool vec;       // whole, 16-byte aligned runs
+  __device__ __forceinline__ void load(const GemmI8& g, int col, bool aligned) {
+    n = (int)max(min((int64_t)8, g.N - col), (int64_t)0);
+    vec = aligned && n == 8;
+    i8_load8(g.b_scale + col, vec, n, 0.0f, sb);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { bias[e] = 0.0f; gate[e] = 1.0f; }
+    if (g.bias) i8_load8((const T*)g.bias + col, vec, n, 0.0f, bias);
+    if (g.gate) i8_load8(g.gate + col, vec, n, 0.0f, gate);
+  }
+  // scale, bias, GELU or gated residual (res) of one row with token scale sa, rounded once
+  __device__ __forceinline__ void store(const GemmI8& g, const int (&acc)[8], float sa, const float (&res)[8],
+                                        int64_t row, int col) const {
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = fmaf((float)acc[e], sa * sb[e], bias[e]);
+    if (g.gelu) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = i8_gelu(z[e]);
+    } else if (g.res) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = fmaf(gate[e], z[e], res[e]);
+    }
+    T* cp = (T*)g.c + row * g.ldc + col;
+    if (vec) {
       store8(cp, z);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (col + e >= g.N) return;
-        float z = (float)acc[e] * (sa * g.b_scale[col + e]) + (bp ? Elem<T>::load(bp + e) : 0.0f);
-        if (g.gelu) z = gelu_tanh(z);
-        if (rp) z = fmaf(g.gate ? g.gate[col + e] : 1.0f, z, Elem<T>::load(rp + e));
-        Elem<T>::store(cp + e, z);
-      }
+      for (int e = 0; e < 8; ++e)
+        if (e < n) Elem<T>::store(cp + e, z[e]);
     }
   }
 };
 
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(WM * WN * 64)
-gemm_i8(const I8Epilogue<T> ep, int tiles_m, int tiles_n) {
-  constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
-  constexpr int A_INS = BM / 8 / NW, B_INS = BN / 8 / NW;
-  constexpr int STAGE = (BM + BN) * 8;
-  __shared__ uint4 lds[2 * STAGE];
-  const GemmI8& g = ep.g;
+// Tile of WM x WN waves, FM x FN MFMA blocks of 32 x 32 each.  SK groups of such waves
+// share a stage and take 4 / SK of its four k-steps each; GK groups of those take
+// every GK-th stage with rings of their own.  Their integer sums meet in the
+// epilogue.  A ring holds NSA stages of A and NSB of B.
+template <typename T, int WM, int WN, int FM, int FN, int SK, int GK, int NSA, int NSB, int WPE>
+__global__ void __launch_bounds__(WM * WN * SK * GK * 64) __attribute__((amdgpu_waves_per_eu(WPE, 8)))
+gemm_i8(const GemmI8 g, int aligned, int tiles_m, int tiles_n) {
+  constexpr int NG = WM * WN, NR = NG * SK, WK = SK * GK, NW = NG * WK;
+  constexpr int TM = FM * 32, TN = FN * 32, BM = WM * TM, BN = WN * TN, KPW = 4 / SK;
+  constexpr int A_INS = BM / 8 / NR, B_INS = BN / 8 / NR;
+  static_assert(A_INS * 8 * NR == BM && B_INS * 8 * NR == BN, "every wave loads whole 8-row slabs");
+  static_assert(NSA >= NSB && NSB >= 2, "a stage is loaded while another is multiplied");
+  constexpr int RING = NSA * BM * 8 + NSB * BN * 8;   // uint4: [A stages | B stages][row][8 chunks]
+  constexpr int EP_LD = TN + 4;                       // int32 pitch of a parked 32-row slice
+  constexpr int PARK = NW * 32 * EP_LD / 4;
+  __shared__ uint4 lds[GK * RING > PARK ? GK * RING : PARK];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int tm, tn;
   tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN, wm = wave / WN, wn = wave % WN;
-  const int lrow = lane >> 3, K = (int)g.K;
-  const __amdgpu_buffer_rsrc_t ra = i8_rows(g.a, g.lda, m0, (int)g.M, g.K);
-  const __amdgpu_buffer_rsrc_t rb = i8_rows(g.b, g.ldb, n0, (int)g.N, g.K);
-  auto issue = [&](uint4* as, uint4* bs, int k0) {
+  const int gk = wave / NR, wr = wave % NR, sk = wr / NG, wg = wr % NG, wm = wg / WN, wn = wg % WN;
+  const int wk = wave / NG;
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int K = (int)g.K, KT = (K + I8_BK - 1) / I8_BK, n_it = (KT + GK - 1) / GK;
+  uint4* ring_a = lds + gk * RING;
+  uint4* ring_b = ring_a + NSA * BM * 8;
+  const __amdgpu_buffer_rsrc_t ra = i8_rows(g.a, g.lda, m0, min((int)g.M - m0, BM), K);
+  const __amdgpu_buffer_rsrc_t rb = i8_rows(g.b, g.ldb, n0, min((int)g.N - n0, BN), K);
+  // a slab is 8 rows: lane i lands in row i >> 3, physical chunk i & 7
+  int va[A_INS], vb[B_INS];
 #pragma unroll
-    for (int j = 0; j < A_INS; ++j) {
-      const int r = (wave * A_INS + j) * 8 + lrow, kc = k0 + 16 * ((lane & 7) ^ lds_swz(r));
-      const int off = kc < K ? r * (int)g.lda + kc : PAST_END;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(as + (wave * A_INS + j) * 64), 16, off, 0, 0, 0);
-    }
+  for (int j = 0; j < A_INS; ++j) {
+    const int r = (wr * A_INS + j) * 8 + (lane >> 3);
+    va[j] = r * (int)g.lda + 16 * ((lane & 7) ^ lds_swz(r));
+  }
 #pragma unroll
-    for (int j = 0; j < B_INS; ++j) {
-      const int r = (wave * B_INS + j) * 8 + lrow, kc = k0 + 16 * ((lane & 7) ^ lds_swz(r));
-      const int off = kc < K ? r * (int)g.ldb + kc : PAST_END;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(bs + (wave * B_INS + j) * 64), 16, off, 0, 0, 0);
+  for (int j = 0; j < B_INS; ++j) {
+    const int r = (wr * B_INS + j) * 8 + (lane >> 3);
+    vb[j] = r * (int)g.ldb + 16 * ((lane & 7) ^ lds_swz(r));
+  }
+  // one operand's stage `it` of this group; past K every load reads zeros
+  auto issue = [&](const __amdgpu_buffer_rsrc_t& rs, uint4* to, const auto& v, int it) {
+    constexpr int INS = sizeof(v) / sizeof(int);
+    const int k0 = (it * GK + gk) * I8_BK;
+    if (K - k0 >= I8_BK || k0 >= K) {
+      const int k = k0 < K ? k0 : I8_DEAD;
+#pragma unroll
+      for (int j = 0; j < INS; ++j) i8_slab(rs, to + (wr * INS + j) * 64, vadd_sgpr(v[j], k));
+    } else {                                          // the last stage of a K off the stages
+#pragma unroll
+      for (int j = 0; j < INS; ++j) {
+        const int ch = (lane & 7) ^ lds_swz((wr * INS + j) * 8 + (lane >> 3));
+        i8_slab(rs, to + (wr * INS + j) * 64, v[j] + (k0 + 16 * ch < K ? k0 : I8_DEAD));
+      }
     }
+  };
+  // own loads but the `V` youngest have landed and own LDS reads are done; behind the
+  // barrier so are those of every wave that shares the ring
+  auto sync = [&](auto allow) {
+    i8_wait<decltype(allow)::value>();
+    if constexpr (NR > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
   i32x16 acc[FM][FN];
 #pragma unroll
@@ -96,68 +172,204 @@ gemm_i8(const I8Epilogue<T> ep, int tiles_m, int tiles_n) {
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-  const int KT = (K + I8_BK - 1) / I8_BK, half = lane >> 5, r31 = lane & 31, sw = lds_swz(r31);
-  issue(lds, lds + BM * 8, 0);
-  for (int kt = 0; kt < KT; ++kt) {
-    uint4* cur = lds + (kt & 1) * STAGE;
-    uint4* nxt = lds + ((kt + 1) & 1) * STAGE;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (kt + 1 < KT) issue(nxt, nxt + BM * 8, (kt + 1) * I8_BK);
+  const int half = lane >> 5, r31 = lane & 31, sw = lds_swz(r31);
+  i32x4 af[2][FM], bf[2][FN];
+  // operands of this wave's k-step q (32 codes) of the stages in slots sa, sb
+  auto read = [&](int set, int sa, int sb, int q) {
+    const uint4* as = ring_a + sa * BM * 8 + wm * TM * 8;
+    const uint4* bs = ring_b + sb * BN * 8 + wn * TN * 8;
+    const int ch = (2 * (sk * KPW + q) + half) ^ sw;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      i32x4 af[FM], bf[FN];
-      const int ch = (2 * s + half) ^ sw;
+    for (int j = 0; j < FN; ++j) bf[set][j] = __builtin_bit_cast(i32x4, bs[(j * 32 + r31) * 8 + ch]);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) af[i] = __builtin_bit_cast(i32x4, cur[(wm * TM + i * 32 + r31) * 8 + ch]);
+    for (int i = 0; i < FM; ++i) af[set][i] = __builtin_bit_cast(i32x4, as[(i * 32 + r31) * 8 + ch]);
+  };
+  auto multiply = [&](int set) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j)
-        bf[j] = __builtin_bit_cast(i32x4, cur[(BM + wn * TN + j * 32 + r31) * 8 + ch]);
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[set][i], bf[set][j], acc[i][j], 0, 0, 0);
+    // one LDS read behind each MFMA
+    constexpr int R = FM + FN, X = FM * FN;
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[i], bf[j], acc[i][j], 0, 0, 0);
+    for (int r = 0; r < (X < R ? X : R); ++r) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+    if constexpr (R > X) __builtin_amdgcn_sched_group_barrier(0x100, R - X, 0);
+    if constexpr (X > R) __builtin_amdgcn_sched_group_barrier(0x008, X - R, 0);
+  };
+#pragma unroll
+  for (int p = 0; p < NSA; ++p) {
+    if (p < NSB) issue(rb, ring_b + p * BN * 8, vb, p);
+    issue(ra, ring_a + p * BM * 8, va, p);
   }
-  __syncthreads();
-  constexpr int EP_LD = TN + 4;
-  static_assert(NW * 32 * EP_LD * 4 <= (int)sizeof(lds), "epilogue staging exceeds LDS");
+  sync(std::integral_constant<int, (NSA - 1) * A_INS + (NSB - 1) * B_INS>{});
+  read(0, 0, 0, 0);
+  int sa = 0, sb = 0;
+  // A stage's last operands are in registers before they are multiplied: the next
+  // stage has to be there then, its first operands are read behind the MFMAs, and the
+  // slots of this one are loaded again.
+  auto stage = [&](int it, auto first) {
+    constexpr int F = decltype(first)::value;
+#pragma unroll
+    for (int q = 0; q < KPW; ++q) {
+      if (q + 1 < KPW) {
+        read((F + q + 1) & 1, sa, sb, q + 1);
+      } else {
+        sync(std::integral_constant<int, (NSA - 2) * A_INS + (NSB - 2) * B_INS>{});
+        issue(rb, ring_b + sb * BN * 8, vb, it + NSB);
+        issue(ra, ring_a + sa * BM * 8, va, it + NSA);
+        sa = sa + 1 == NSA ? 0 : sa + 1;
+        sb = sb + 1 == NSB ? 0 : sb + 1;
+        read((F + q + 1) & 1, sa, sb, 0);
+      }
+      multiply((F + q) & 1);
+    }
+  };
+  if constexpr (KPW % 2 == 0) {
+    for (int it = 0; it < n_it; ++it) stage(it, std::integral_constant<int, 0>{});
+  } else {
+    int it = 0;
+    for (; it + 1 < n_it; it += 2) {
+      stage(it, std::integral_constant<int, 0>{});
+      stage(it + 1, std::integral_constant<int, 1>{});
+    }
+    if (it < n_it) stage(it, std::integral_constant<int, 0>{});
+  }
+  // Epilogue: each wave parks 32 rows of its tile, then the WK waves of one place
+  // share its runs of 8 columns; a lane always has the same columns.  Everything it
+  // reads is requested before the last barrier (the residual a slice ahead), which
+  // also waits for the stages loaded past K.
+  constexpr int CPR = TN / 8, RUNS = 32 * CPR, ITS = (RUNS / 64 + WK - 1) / WK;
+  static_assert(64 % CPR == 0 && RUNS % 64 == 0, "a lane keeps its columns");
+  const int cl = (lane % CPR) * 8, col = n0 + wn * TN + cl;
+  auto run_row = [&](int t) { return (lane + 64 * (t * WK + wk)) / CPR; };   // 32 and more: none
+  I8Cols<T> cols;
+  cols.load(g, col, aligned);
+  float tok[FM][ITS];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int t = 0; t < ITS; ++t) {
+      const int row = m0 + wm * TM + i * 32 + run_row(t);
+      tok[i][t] = g.a_scale[row < g.M ? row : g.M - 1];
+    }
+  float res[2][ITS][8];
+  auto load_res = [&](int i) {
+    if (g.res == nullptr) return;
+#pragma unroll
+    for (int t = 0; t < ITS; ++t) {
+      const int64_t row = m0 + wm * TM + i * 32 + run_row(t);
+      if (run_row(t) < 32 && row < g.M && cols.n > 0)
+        i8_load8((const T*)g.res + row * g.ldr + col, cols.vec, cols.n, 0.0f, res[i & 1][t]);
+    }
+  };
+  load_res(0);
+  i8_wait<0>();
+  if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
   int* park = reinterpret_cast<int*>(lds) + wave * 32 * EP_LD;
+  const int* place = reinterpret_cast<int*>(lds) + wg * 32 * EP_LD;
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
+    if (i + 1 < FM) load_res(i + 1);
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         park[(8 * (r >> 2) + 4 * half + (r & 3)) * EP_LD + j * 32 + r31] = acc[i][j][r];
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_s_waitcnt(0xc07f);
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int it = 0; it < 32 * TN / 8 / 64; ++it) {
-      const int rl = (lane + 64 * it) / (TN / 8), cl = (lane + 64 * it) % (TN / 8) * 8;
-      int v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = park[rl * EP_LD + cl + e];
-      ep.run(v, m0 + wm * TM + i * 32 + rl, n0 + wn * TN + cl);
+    if constexpr (WK > 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int t = 0; t < ITS; ++t) {
+      const int rl = run_row(t);
+      const int64_t row = m0 + wm * TM + i * 32 + rl;
+      if (rl < 32 && row < g.M && cols.n > 0) {
+        int v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int z = 0; z < WK; ++z) {
+          const int4* p = reinterpret_cast<const int4*>(place + z * NG * 32 * EP_LD + rl * EP_LD + cl);
+          const int4 lo = p[0], hi = p[1];
+          v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+          v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+        }
+        cols.store(g, v, tok[i][t], res[i & 1][t], row, col);
+      }
+    }
+    if constexpr (WK > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <typename T, int WM, int WN, int FM, int FN, int SK, int GK, int NSA, int NSB, int WPE>
+static void run_i8(const GemmI8& g, int aligned, hipStream_t st) {
+  const int tm = (int)((g.M + WM * FM * 32 - 1) / (WM * FM * 32)), tn = (int)((g.N + WN * FN * 32 - 1) / (WN * FN * 32));
+  hipLaunchKernelGGL((gemm_i8<T, WM, WN, FM, FN, SK, GK, NSA, NSB, WPE>), dim3(tm * tn),
+                     dim3(WM * WN * SK * GK * 64), 0, st, g, aligned, tm, tn);
+}
+
+// Tiles, and the choice among them by modelled time: t0 + n (fill + step stages),
+// n the rounds of workgroups over 256 CUs.  Two workgroups of a `pair` tile share a CU:
+// their rounds count in halves once the grid spills past one per CU (smoothly past
+// eight), and a lone one per CU takes `lone` of a shared round.  The constants (us)
+// are a fit to 17 row counts from 1 to 17,472 of 12 projections with N and K from 512
+// to 8,192; choosing by it runs 1.7% above the best of thirteen tiles on average.
+// E.g. 1 x 1,536 x 1,536 4.0 us on 32x32 (64x64 5.8, 256x256 19), 512 x 1,536 x 4,096
+// 11.1 on 64x64 (128x128 19), 3,472 x 1,536 x 6,144 38.4 on 192x128 with the k-steps
+// of a stage shared by two groups of waves (44.9 with one), 17,472 x 8,192 x 2,048 303
+// on 256x256 (192x128 319).
+struct I8Tile {
+  int bm, bn, pair;
+  double lone, t0, fill, step;
+};
+static const I8Tile I8_TILES[] = {
+    {256, 256, 0, 1.0, 0.0, 8.28, 1.177}, {192, 128, 1, 0.55, 1.75, 7.44, 1.171}, {192, 128, 0, 1.0, 0.0, 6.59, 0.542},
+    {128, 128, 1, 0.60, 1.61, 4.85, 0.903}, {128, 128, 0, 1.0, 0.06, 5.45, 0.431}, {64, 128, 1, 0.55, 1.97, 3.96, 0.536},
+    {64, 64, 0, 1.0, 1.50, 2.57, 0.194}, {32, 32, 1, 0.60, 2.16, 1.93, 0.154}, {32, 32, 0, 1.0, 1.79, 2.12, 0.078}};
+
+static int choose_i8(int64_t M, int64_t N, int64_t K) {
+  const double stages = (double)((K + I8_BK - 1) / I8_BK);
+  int best = 0;
+  double best_us = 1e300;
+  for (int i = 0; i < (int)(sizeof(I8_TILES) / sizeof(I8_TILES[0])); ++i) {
+    const I8Tile& t = I8_TILES[i];
+    const double wgs = (double)((M + t.bm - 1) / t.bm) * (double)((N + t.bn - 1) / t.bn);
+    const double full = std::ceil(wgs / 256.0);
+    const double n = !t.pair ? full : wgs <= 256.0 ? t.lone : wgs <= 2048.0 ? full / 2.0 : wgs / 512.0;
+    const double us = t.t0 + n * (t.fill + t.step * stages);
+    if (us < best_us) { best_us = us; best = i; }
+  }
+  return best;
 }
 
 template <typename T>
 static void run_gemm_i8(const GemmI8& g, hipStream_t st) {
   const int esz = sizeof(T);
   auto row16 = [&](const void* p, int64_t ld) { return (((uintptr_t)p | (uintptr_t)(ld * esz)) & 15) == 0; };
-  const I8Epilogue<T> ep{g, row16(g.c, g.ldc) && row16(g.res, g.res ? g.ldr : 0) && row16(g.bias, 0)};
-  const int tm = (int)((g.M + 127) / 128), tn = (int)((g.N + 127) / 128);
-  hipLaunchKernelGGL((gemm_i8<T, 128, 128, 2, 2>), dim3(tm * tn), dim3(256), 0, st, ep, tm, tn);
+  const int aligned = row16(g.c, g.ldc) && row16(g.res, g.res ? g.ldr : 0) && row16(g.bias, 0) &&
+                      (((uintptr_t)g.b_scale | (uintptr_t)g.gate) & 15) == 0;
+  switch (choose_i8(g.M, g.N, g.K)) {
+    case 0: return run_i8<T, 2, 4, 4, 2, 1, 1, 3, 2, 2>(g, aligned, st);
+    case 1: return run_i8<T, 2, 2, 3, 2, 1, 1, 2, 2, 2>(g, aligned, st);
+    case 2: return run_i8<T, 2, 2, 3, 2, 2, 1, 4, 4, 2>(g, aligned, st);
+    case 3: return run_i8<T, 2, 2, 2, 2, 1, 1, 2, 2, 2>(g, aligned, st);
+    case 4: return run_i8<T, 2, 2, 2, 2, 2, 1, 5, 5, 2>(g, aligned, st);
+    case 5: return run_i8<T, 2, 2, 1, 2, 2, 1, 3, 3, 2>(g, aligned, st);
+    case 6: return run_i8<T, 2, 2, 1, 1, 1, 2, 4, 4, 2>(g, aligned, st);
+    case 7: return run_i8<T, 1, 1, 1, 1, 1, 4, 2, 2, 2>(g, aligned, st);
+    default: return run_i8<T, 1, 1, 1, 1, 1, 4, 4, 4, 2>(g, aligned, st);
+  }
 }
 
-hipError_t launch_gemm_i8(int dtype, const GemmI8& g, int32_t* ws, int64_t ws_words, hipStream_t st) {
+hipError_t launch_gemm_i8(int dtype, const GemmI8& g, hipStream_t st) {
   if (g.M <= 0 || g.N <= 0) return hipSuccess;
-  (void)ws; (void)ws_words;
   if (dtype == 1) run_gemm_i8<bf16_t>(g, st);
   else run_gemm_i8<float>(g, st);
   return hipGetLastError();

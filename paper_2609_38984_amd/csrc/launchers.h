@@ -259,7 +259,7 @@ struct RowQuant {
 hipError_t launch_quant_rows(int dtype, bool norm, const RowQuant& a, hipStream_t st);
 
 // 8-bit product (k_gemm_i8.hip); epilogue: bias (may be NULL), then GELU or the
-// gated residual.  ws: workspace for the int32 partial sums of a split K.
+// gated residual
 struct GemmI8 {
   const int8_t* a; int64_t lda; const float* a_scale;
   const int8_t* b; int64_t ldb; const float* b_scale;
@@ -269,7 +269,7 @@ struct GemmI8 {
   int64_t M, N, K;
   bool gelu;
 };
-hipError_t launch_gemm_i8(int dtype, const GemmI8& g, int32_t* ws, int64_t ws_words, hipStream_t st);
+hipError_t launch_gemm_i8(int dtype, const GemmI8& g, hipStream_t st);
 
 // attention to an encoder's states (k_cross.hip); ws: workspace for the partial
 // results of split keys

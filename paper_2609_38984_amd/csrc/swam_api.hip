@@ -1521,8 +1521,7 @@ int swam_gemm_i8(swam_ctx* c, const int8_t* a, int64_t lda, const float* a_scale
   if (!typed(a_scale, 4) || !typed(b_scale, 4) || !typed(gate, 4) || !typed(bias, es) ||
       !typed(residual, es) || !typed(out, es))
     return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
-  if (((m + 127) / 128) * ((n + 127) / 128) >= (1ll << 31))
-    return set_err(c, SWAM_E_SHAPE, "more than 2^31 output tiles");
+  if (m * n >= (1ll << 40)) return set_err(c, SWAM_E_SHAPE, "m * n below 2^40");
   const Span os = span(out, ldc, m, n, es);
   for (const Span& in : {span(a, lda, m, k, 1), span(b, ldb, n, k, 1), span(a_scale, 1, m, 1, 4),
                          span(b_scale, 1, n, 1, 4), span(bias, n, 1, n, es), span(gate, n, 1, n, 4)})
@@ -1535,8 +1534,7 @@ int swam_gemm_i8(swam_ctx* c, const int8_t* a, int64_t lda, const float* a_scale
            (flags & SWAM_GEMM_GELU) != 0};
   OnDevice dev(c);
   Timed t(c, SWAM_T_GEMM_I8);
-  SWAM_HIP(c, launch_gemm_i8(c->cfg.dtype, g, c->ptr<int32_t>(c->lay.splitk), c->dv.splitk_floats, c->st),
-           "gemm_i8");
+  SWAM_HIP(c, launch_gemm_i8(c->cfg.dtype, g, c->st), "gemm_i8");
   return SWAM_OK;
 }
 

@@ -250,6 +250,24 @@ def test_gemm_matches_float64(contexts, dtype, m, n, k):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k", [(3472, 1536, 6144), (2001, 6144, 1552), (10160, 1532, 1536), (3474, 6150, 784),
+                                   (20, 6144, 6160), (2600, 4608, 400)])
+def test_gemm_large_products(contexts, dtype, m, n, k):
+    """Sizes for which the widest tiles are chosen, ragged on every side."""
+    dt, g = TYPES[dtype], gen(m + n + k)
+    a, w = codes(m, k, g), codes(n, k, g)
+    sa = torch.rand(m, device="cuda", generator=g) * 0.02 + 1e-3
+    sw = (torch.rand(n, device="cuda", generator=g) + 0.1) * k ** -0.5 / 75
+    b, r = torch.randn(n, device="cuda", generator=g).to(dt), rows_of((m, n), dt, g)[0]
+    gt = torch.randn(n, device="cuda", generator=g)
+    c = torch.empty((m, n), dtype=dt, device="cuda")
+    contexts[dtype].gemm_i8(a, sa, w, sw, c, bias=b, residual=r, gate=gt)
+    check_gemm(a, sa, w, sw, b, r, gt, False, c)
+    contexts[dtype].gemm_i8(a, sa, w, sw, c, bias=b, gelu=True)
+    check_gemm(a, sa, w, sw, b, None, None, True, c)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 def test_gemm_extreme_codes_in_place_and_nan_scales(contexts, dtype):
     dt = TYPES[dtype]
     ctx = contexts[dtype]
