@@ -26,6 +26,7 @@ HIPCC_FLAGS = [
 # softmax can rescale them without AGPR round trips
 EXTRA_DEVICE_FLAGS = {
     "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+    "k_cross.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

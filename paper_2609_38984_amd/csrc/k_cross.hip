@@ -25,10 +25,14 @@ typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 constexpr int CR_BK = 64;                      // keys per tile: one bit of a mask word each
 constexpr int CR_DWORD3 = 0x00020000;          // raw buffer descriptor, 32-bit data
 constexpr int CR_PAST_END = 0x7fffff00;        // an offset that no tile reaches
+// one DMA instruction: 16 bytes per lane at `off` to a 1 KB slab of LDS
+__device__ __forceinline__ void cr_slab(__amdgpu_buffer_rsrc_t r, uint4* slab, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)slab, 16, off, 0, 0, 0);
+}
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // The sequence that holds tile t of `bq` rows (rows are tokens x group): lane b
-// looks at sequence b, a scan over the lanes finds the one.
+// looks at sequence b and its keys, a scan over the lanes finds the one.
 struct TileAt {
   int a, rows;        // first token, token x group rows of the sequence
   int r0;             // first row of the tile
@@ -36,15 +40,19 @@ struct TileAt {
 };
 __device__ __forceinline__ bool tile_at(const CrossArgs& c, int group, int bq, int t, TileAt& o) {
   const int lane = threadIdx.x & 63;
-  int a = 0, e = 0;
+  int a = 0, e = 0, s0 = 0, s1 = 0;
   if (lane < c.n_seqs) {
+    const int kb = c.kv_seq ? c.kv_seq[lane] : lane;
     e = c.cu_q ? min(max(c.cu_q[lane + 1], 0), c.n_q) : c.n_q;
     a = c.cu_q ? min(max(c.cu_q[lane], 0), e) : 0;
+    if (kb >= 0 && kb < c.n_kv_seqs) {
+      s1 = c.cu_k ? min(max(c.cu_k[kb + 1], 0), c.n_k) : c.n_k;
+      s0 = c.cu_k ? min(max(c.cu_k[kb], 0), s1) : 0;
+    }
   }
   const int nt = ((e - a) * group + bq - 1) / bq;
   int upto = nt;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
+  for (int s = 1; s < c.n_seqs; s <<= 1) {
     const int v = __shfl_up(upto, s);
     if (lane >= s) upto += v;
   }
@@ -54,12 +62,8 @@ __device__ __forceinline__ bool tile_at(const CrossArgs& c, int group, int bq, i
   o.a = __builtin_amdgcn_readlane(a, b);
   o.rows = (__builtin_amdgcn_readlane(e, b) - o.a) * group;
   o.r0 = (t - (__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(nt, b))) * bq;
-  const int kb = c.kv_seq ? __builtin_amdgcn_readfirstlane(c.kv_seq[b]) : b;
-  o.s0 = o.s1 = 0;
-  if (kb >= 0 && kb < c.n_kv_seqs) {
-    o.s1 = c.cu_k ? min(max(__builtin_amdgcn_readfirstlane(c.cu_k[kb + 1]), 0), c.n_k) : c.n_k;
-    o.s0 = c.cu_k ? min(max(__builtin_amdgcn_readfirstlane(c.cu_k[kb]), 0), o.s1) : 0;
-  }
+  o.s0 = __builtin_amdgcn_readlane(s0, b);
+  o.s1 = __builtin_amdgcn_readlane(s1, b);
   return true;
 }
 
@@ -78,11 +82,12 @@ struct Partial {
   int splits;
 };
 
-template <int D, int NW>
-__global__ void __launch_bounds__(NW * 64)
+// Four waves of 32 rows each.
+template <int D>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, 8)))
 cross_bf16(const CrossArgs c, int slots, const Partial part) {
   constexpr int H2 = D / 64;                     // 128-byte halves of a head's row
-  constexpr int BQ = 32 * NW;
+  constexpr int NW = 4, BQ = 32 * NW;
   constexpr int TILE = CR_BK * 8 * H2;           // uint4 of a K or V tile
   __shared__ uint4 kv[2][2][TILE];               // [stage][K | V][half][key][8 chunks]
   const int group = c.heads / c.kv_heads;
@@ -95,8 +100,7 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r31 = lane & 31;
-  const int rr = min(ta.r0 + wave * 32 + r31, ta.rows - 1);
-  const bool live = ta.r0 + wave * 32 + r31 < ta.rows;
+  const int want = ta.r0 + wave * 32 + r31, rr = min(want, ta.rows - 1);
   const int64_t tok = ta.a + rr / group;
   const int head = hk * group + rr % group;
   bf16x8 qf[D / 16];
@@ -109,30 +113,45 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
   int t0, t1;
   slice_of(ta.s0, ta.s1, CR_BK, blockIdx.y, part.splits, t0, t1);
 
-  // visible keys of tile t, one bit each
+  // whether this lane's key of tile t is visible
   auto mask_byte = [&](int t) -> int {
     const int key = ta.s0 + t * CR_BK + lane;
     return t < t1 && key < ta.s1 && (c.mask == nullptr || c.mask[key] != 0);
   };
-  const int lrow = lane >> 3, kld = (int)c.k_ld, vld = (int)c.v_ld;
+  const int lrow = lane >> 3;
   constexpr int SLABS = 8 * H2;                  // 8-row slabs of a tile
   static_assert(SLABS % NW == 0, "every wave stages whole slabs");
-  auto issue = [&](int buf, int t, uint64_t vis) {
+  int off_k[SLABS / NW], off_v[SLABS / NW], row_of[SLABS / NW];
+#pragma unroll
+  for (int j = 0; j < SLABS / NW; ++j) {
+    const int slab = wave * (SLABS / NW) + j, half = slab >> 3;
+    const int r = (slab & 7) * 8 + lrow, col = 64 * half + 8 * ((lane & 7) ^ lds_swz(r));
+    row_of[j] = r;
+    off_k[j] = (r * (int)c.k_ld + col) * 2;
+    off_v[j] = (r * (int)c.v_ld + col) * 2;
+  }
+  // K and V of tile t into LDS; hidden keys are zeros
+  auto issue = [&](uint4 (&to)[2][TILE], int t, uint64_t vis) {
     const int64_t row = ta.s0 + (int64_t)t * CR_BK;
     const int rows = min(ta.s1 - (int)row, CR_BK);
     const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)((const bf16_t*)c.k + row * c.k_ld + hk * D), (short)0, ((rows - 1) * kld + D) * 2, CR_DWORD3);
+        (void*)((const bf16_t*)c.k + row * c.k_ld + hk * D), (short)0, ((rows - 1) * (int)c.k_ld + D) * 2, CR_DWORD3);
     const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)((const bf16_t*)c.v + row * c.v_ld + hk * D), (short)0, ((rows - 1) * vld + D) * 2, CR_DWORD3);
+        (void*)((const bf16_t*)c.v + row * c.v_ld + hk * D), (short)0, ((rows - 1) * (int)c.v_ld + D) * 2, CR_DWORD3);
+    const int at = wave * (SLABS / NW) * 64;
+    if (vis == ~(uint64_t)0) {
 #pragma unroll
-    for (int j = 0; j < SLABS / NW; ++j) {
-      const int slab = wave * (SLABS / NW) + j, half = slab >> 3;
-      const int r = (slab & 7) * 8 + lrow, col = 64 * half + 8 * ((lane & 7) ^ lds_swz(r));
-      const bool see = (vis >> r) & 1;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(&kv[buf][0][slab * 64]), 16,
-                                               see ? (r * kld + col) * 2 : CR_PAST_END, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(&kv[buf][1][slab * 64]), 16,
-                                               see ? (r * vld + col) * 2 : CR_PAST_END, 0, 0, 0);
+      for (int j = 0; j < SLABS / NW; ++j) {
+        cr_slab(rk, &to[0][at + j * 64], off_k[j]);
+        cr_slab(rv, &to[1][at + j * 64], off_v[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < SLABS / NW; ++j) {
+        const bool see = (vis >> row_of[j]) & 1;
+        cr_slab(rk, &to[0][at + j * 64], see ? off_k[j] : CR_PAST_END);
+        cr_slab(rv, &to[1][at + j * 64], see ? off_v[j] : CR_PAST_END);
+      }
     }
   };
   // V^T operand by transposed LDS reads: in each 16-lane group lane a addresses
@@ -160,8 +179,9 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
   float m_run = -FLT_MAX, l_run = 0.0f;
   const float sc = LOG2E * c.scale;
 
-  auto tile = [&](int buf, uint64_t vis, auto masked) {
-    const uint4* Kt = kv[buf][0];
+  // one tile of keys; `fresh`: the first visible one
+  auto tile = [&](const uint4 (&from)[2][TILE], uint64_t vis, bool fresh, auto masked) {
+    const uint4* Kt = from[0];
     auto scores = [&](f32x16 (&st)[2]) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -173,15 +193,19 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
           st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[t], 0, 0, 0);
         }
         if constexpr (decltype(masked)::value) {
-          const uint32_t w = (uint32_t)(vis >> (32 * t)) >> (4 * g);
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!((w >> (8 * (r >> 2) + (r & 3))) & 1u)) st[t][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r) {
+            // register r holds key b of the lower 32 lanes and key b + 4 of the upper: the
+            // select's mask is two scalar bits spread
+            const int b = 32 * t + 8 * (r >> 2) + (r & 3);
+            const uint64_t see = ((vis >> b) & 1 ? 0xffffffffull : 0) | ((vis >> (b + 4)) & 1 ? 0xffffffffull << 32 : 0);
+            if (!__builtin_amdgcn_inverse_ballot_w64(see)) st[t][r] = -INFINITY;
+          }
         }
       }
     };
     bf16x8 pf[2][2];
-    float ps0, ps1;
+    float ps0 = 0.0f, ps1 = 0.0f;
     auto probs = [&](const f32x16 (&st)[2]) {
       ps0 = 0.0f; ps1 = 0.0f;
 #pragma unroll
@@ -197,14 +221,14 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
             pf[t][u][mm] = (__bf16)p0; pf[t][u][mm + 1] = (__bf16)p1;
           }
     };
-    {
+    if (!fresh) {
       f32x16 st[2];
       scores(st);
       probs(st);
     }
     // the running maximum moves only when a row sum shows that some weight passed
     // 2^8 (or is NaN): the scores are then formed again against the new one
-    if (__any(!(ps0 + ps1 <= 256.0f))) {
+    if (fresh || __any(!(ps0 + ps1 <= 256.0f))) {
       asm volatile("" ::: "memory");
       f32x16 st[2];
       scores(st);
@@ -225,7 +249,7 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
       probs(st);
     }
     l_run += ps0 + ps1;
-    const unsigned short* vs = reinterpret_cast<const unsigned short*>(kv[buf][1]);
+    const unsigned short* vs = reinterpret_cast<const unsigned short*>(from[1]);
 #pragma unroll
     for (int ht = 0; ht < D / 32; ++ht)
 #pragma unroll
@@ -241,26 +265,32 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
         }
   };
 
-  // all waves of the workgroup form the same words; a tile without a visible key is
-  // neither loaded nor multiplied
+  // All waves of the workgroup form the same mask words: that of the tile at hand, of the
+  // next, whose loads run meanwhile, and the bytes of the one after it.  A tile without a
+  // visible key is neither loaded nor multiplied.
   uint64_t vis = __ballot(mask_byte(t0));
-  if (vis) issue(0, t0, vis);
   int next = mask_byte(t0 + 1);
+  if (vis) issue(kv[0], t0, vis);
+  bool fresh = true;
+  int buf = 0;
   for (int t = t0; t < t1; ++t) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const int buf = (t - t0) & 1;
     const uint64_t ahead = __ballot(next);
-    if (ahead) issue(buf ^ 1, t + 1, ahead);
+    if (vis | ahead) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    }
+    if (ahead) issue(kv[buf ^ 1], t + 1, ahead);
     next = mask_byte(t + 2);
-    if (vis == ~0ull) tile(buf, vis, std::false_type{});
-    else if (vis) tile(buf, vis, std::true_type{});
+    if (vis == ~(uint64_t)0) tile(kv[buf], vis, fresh, std::false_type{});
+    else if (vis) tile(kv[buf], vis, fresh, std::true_type{});
+    fresh = fresh && vis == 0;
     vis = ahead;
+    buf ^= 1;
   }
-  float l = l_run + __shfl_xor(l_run, 32);
-  if (!live) return;
+  const float l = l_run + __shfl_xor(l_run, 32);
   const int64_t row = tok * c.heads + head;
   if (part.splits > 1) {
+    if (want >= ta.rows) return;
     float* po = part.o + ((int64_t)blockIdx.y * c.n_q * c.heads + row) * D;
 #pragma unroll
     for (int ht = 0; ht < D / 32; ++ht)
@@ -277,15 +307,21 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bf16_t* op = (bf16_t*)c.o + tok * c.o_ld + head * D;
+  // a lane holds 4 of every 8 columns, its partner (lane ^ 32) the others: two runs are
+  // exchanged into one whole run of 8 each
 #pragma unroll
   for (int ht = 0; ht < D / 32; ++ht)
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      uint2 w;
-      w.x = pack_bf16x2(o[ht][4 * q4] * inv, o[ht][4 * q4 + 1] * inv);
-      w.y = pack_bf16x2(o[ht][4 * q4 + 2] * inv, o[ht][4 * q4 + 3] * inv);
-      *(uint2*)(op + 32 * ht + 8 * q4 + 4 * g) = w;
+    for (int q4 = 0; q4 < 4; q4 += 2) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] = pack_bf16x2(o[ht][4 * q4 + 2 * e] * inv, o[ht][4 * q4 + 2 * e + 1] * inv);
+      const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+      const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+      if (want < ta.rows) *(uint4*)(op + 32 * ht + 8 * (q4 + g)) = make_uint4(x[0], y[0], x[1], y[1]);
     }
+  if (want >= ta.rows) return;
   if (c.lse != nullptr && g == 0) c.lse[row] = l == 0.0f ? -INFINITY : (m_run + log2f(l)) * LN2;
 }
 
@@ -324,16 +360,27 @@ cross_f32(const CrossArgs c, int slots, const Partial part) {
     const int key = kb + r31;
     const uint32_t vis = (uint32_t)__ballot(key < ta.s1 && (c.mask == nullptr || c.mask[min(key, ta.s1 - 1)] != 0));
     if (vis == 0) continue;
+    // all operands of the tile are requested before the first product
     const float* kp = (const float*)c.k + (int64_t)min(key, ta.s1 - 1) * c.k_ld + hk * D;
     const float* vb = (const float*)c.v + hk * D + r31;
+    f32x4 kf[D / 8];
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) kf[s] = *reinterpret_cast<const f32x4*>(kp + 4 * (2 * s + g));
+    float vf[D / 32][16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int kr = 8 * (r >> 2) + 4 * g + (r & 3);
+      const float* vp = vb + (int64_t)min(kb + kr, ta.s1 - 1) * c.v_ld;
+#pragma unroll
+      for (int h = 0; h < D / 32; ++h) vf[h][r] = vp[32 * h];
+    }
     f32x16 st;
 #pragma unroll
     for (int r = 0; r < 16; ++r) st[r] = 0.0f;
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) {
-      const f32x4 kf = *reinterpret_cast<const f32x4*>(kp + 4 * (2 * s + g));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[s][e], st, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[s][e], qf[s][e], st, 0, 0, 0);
     }
     const uint32_t w = vis >> (4 * g);
     float mx = -INFINITY;
@@ -352,16 +399,12 @@ cross_f32(const CrossArgs c, int slots, const Partial part) {
       for (int r = 0; r < 16; ++r) o[h][r] *= corr;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int kr = 8 * (r >> 2) + 4 * g + (r & 3);
-      const bool see = (vis >> kr) & 1u;
+      const bool see = (w >> (8 * (r >> 2) + (r & 3))) & 1u;
       const float p = exp2f(st[r] - m_new);
       l += p;
-      const float* vp = vb + (int64_t)min(kb + kr, ta.s1 - 1) * c.v_ld;
 #pragma unroll
-      for (int h = 0; h < D / 32; ++h) {
-        const float v = vp[32 * h];
-        o[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(see ? v : 0.0f, p, o[h], 0, 0, 0);
-      }
+      for (int h = 0; h < D / 32; ++h)
+        o[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(see ? vf[h][r] : 0.0f, p, o[h], 0, 0, 0);
     }
   }
   l += __shfl_xor(l, 32);
@@ -444,23 +487,29 @@ cross_join(const CrossArgs c, const Partial part) {
   if (c.lse != nullptr && lane == 0) c.lse[row] = l == 0.0f ? -INFINITY : (mt + log2f(l)) * LN2;
 }
 
+// workgroups of `bq` rows at most, the lengths being on the device
+static int64_t cross_slots(const CrossArgs& c, int64_t bq) {
+  return ((int64_t)c.n_q * (c.heads / c.kv_heads) + (bq - 1) * c.n_seqs) / bq;
+}
+
+// Few rows leave CUs idle: the keys are split until there are three workgroups to a
+// CU, but into slices of at least four tiles, as far as the workspace holds their
+// partial results.  us without | with the split: 8 x 1 query of 24 heads, 10,160 keys 249 |
+// 116; 32 x 24, 2,048 keys 40 | 15; 300 x 16, 4,096 keys 73 | 28; 1 x 24, 512 keys 12 | 10.
 template <int D>
 static void run_cross(int dtype, const CrossArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
-  const int group = c.heads / c.kv_heads;
-  const int bq = dtype == 1 ? 128 : 32;
-  const int64_t rows = (int64_t)c.n_q * group;
-  const int slots = (int)((rows + (int64_t)(bq - 1) * c.n_seqs) / bq);
-  const int64_t wgs = (int64_t)slots * c.kv_heads;
-  const int64_t tiles = (c.n_k / c.n_kv_seqs + 63) / 64;
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(wgs, 1), tiles / 4), 64));
-  splits = std::max<int64_t>(1, std::min<int64_t>(splits, ws_floats / std::max<int64_t>(1, (int64_t)c.n_q * c.heads * (D + 2))));
-  Partial p{ws, ws + splits * c.n_q * c.heads * D, (int)splits};
-  if (dtype == 1)
-    hipLaunchKernelGGL((cross_bf16<D, 4>), dim3((unsigned)wgs, (unsigned)splits), dim3(256), 0, st, c, slots, p);
-  else
-    hipLaunchKernelGGL((cross_f32<D>), dim3((unsigned)wgs, (unsigned)splits), dim3(256), 0, st, c, slots, p);
+  const int64_t slots = cross_slots(c, dtype == 1 ? 128 : 32), wgs = slots * c.kv_heads;
+  const int64_t tiles = (c.n_k / c.n_kv_seqs + CR_BK - 1) / CR_BK;
+  const int64_t rows = (int64_t)c.n_q * c.heads;
+  const int splits = (int)std::max<int64_t>(
+      1, std::min(std::min<int64_t>(768 / std::max<int64_t>(wgs, 1), tiles / 4),
+                  std::min<int64_t>(64, ws_floats / (rows * (D + 2)))));
+  const Partial p{ws, ws + splits * rows * D, splits};
+  const dim3 grid((unsigned)wgs, splits);
+  if (dtype == 1) hipLaunchKernelGGL((cross_bf16<D>), grid, dim3(256), 0, st, c, (int)slots, p);
+  else hipLaunchKernelGGL((cross_f32<D>), grid, dim3(256), 0, st, c, (int)slots, p);
   if (splits > 1) {
-    const unsigned n = (unsigned)(((int64_t)c.n_q * c.heads + 3) / 4);
+    const unsigned n = (unsigned)((rows + 3) / 4);
     if (dtype == 1) hipLaunchKernelGGL((cross_join<bf16_t, D>), dim3(n), dim3(256), 0, st, c, p);
     else hipLaunchKernelGGL((cross_join<float, D>), dim3(n), dim3(256), 0, st, c, p);
   }
