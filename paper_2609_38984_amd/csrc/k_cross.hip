@@ -85,18 +85,17 @@ struct Partial {
 // Four waves of 32 rows each.
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, 8)))
-cross_bf16(const CrossArgs c, int slots, const Partial part) {
+cross_bf16(const CrossArgs c, const Partial part) {
   constexpr int H2 = D / 64;                     // 128-byte halves of a head's row
   constexpr int NW = 4, BQ = 32 * NW;
   constexpr int TILE = CR_BK * 8 * H2;           // uint4 of a K or V tile
   __shared__ uint4 kv[2][2][TILE];               // [stage][K | V][half][key][8 chunks]
   const int group = c.heads / c.kv_heads;
-  const int nwg = gridDim.x, pid = blockIdx.x;
-  const int xcd = pid & 7, per = nwg >> 3, rem = nwg & 7;
-  const int id = xcd * per + min(xcd, rem) + (pid >> 3);
-  const int hk = id / slots;
+  // neighbouring workgroups take the K/V heads in turn: with a multiple of 8 of them a
+  // head stays on one XCD, and every XCD gets a share of every sequence, long or empty
+  const int hk = blockIdx.x % c.kv_heads;
   TileAt ta;
-  if (!tile_at(c, group, BQ, id - hk * slots, ta)) return;
+  if (!tile_at(c, group, BQ, blockIdx.x / c.kv_heads, ta)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r31 = lane & 31;
@@ -330,14 +329,14 @@ cross_bf16(const CrossArgs c, int slots, const Partial part) {
 // every fourth tile of 32 keys of the same 32 rows and meet in LDS.
 template <int D>
 __global__ void __launch_bounds__(256)
-cross_f32(const CrossArgs c, int slots, const Partial part) {
+cross_f32(const CrossArgs c, const Partial part) {
   constexpr int LD = D + 4;
   __shared__ float os[4][32][LD];
   __shared__ float ms[4][32], ls[4][32];
   const int group = c.heads / c.kv_heads;
-  const int hk = blockIdx.x / slots;
+  const int hk = blockIdx.x % c.kv_heads;
   TileAt ta;
-  if (!tile_at(c, group, 32, blockIdx.x - hk * slots, ta)) return;
+  if (!tile_at(c, group, 32, blockIdx.x / c.kv_heads, ta)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, r31 = lane & 31;
   const int rr = min(ta.r0 + r31, ta.rows - 1);
   f32x4 qf[D / 8];
@@ -492,22 +491,37 @@ static int64_t cross_slots(const CrossArgs& c, int64_t bq) {
   return ((int64_t)c.n_q * (c.heads / c.kv_heads) + (bq - 1) * c.n_seqs) / bq;
 }
 
-// Few rows leave CUs idle: the keys are split until there are three workgroups to a
-// CU, but into slices of at least four tiles, as far as the workspace holds their
-// partial results.  us without | with the split: 8 x 1 query of 24 heads, 10,160 keys 249 |
-// 116; 32 x 24, 2,048 keys 40 | 15; 300 x 16, 4,096 keys 73 | 28; 1 x 24, 512 keys 12 | 10.
+// Few rows leave CUs idle and a workgroup alone on its CU waits out the latency of every
+// tile, so the keys are split, as far as the workspace holds the partial results.  Chosen
+// by modelled time (us): tiles per slice, each `lone` for a workgroup by itself and
+// `share` per workgroup where several share a CU, plus the pass that joins the
+// slices and what they write and read.  us without | with the chosen split: 8 x 1 query
+// of 24 heads on 10,160 keys 249 | 116 (4 slices), 32 x 24 on 2,048 40 | 15 (8), 300 x 16 on
+// 4,096 73 | 28 (8), 1 x 24 on 512 12 | 10; 4,096 x 12 on 512 (head_dim 128) 26 | 53 (2,
+// not chosen).
+static int cross_splits(int64_t wgs, int64_t tiles, int64_t rows, int D, int64_t ws_floats) {
+  const double lone = D == 64 ? 1.2 : 1.6, share = D == 64 ? 0.64 : 1.0;
+  int best = 1;
+  double best_us = 1e300;
+  for (int s = 1; s <= 64 && (s == 1 || s * 2 <= tiles); s *= 2) {
+    if (s > 1 && (int64_t)s * rows * (D + 2) > ws_floats) break;
+    double us = (double)((tiles + s - 1) / s) * std::max(lone, share * (double)(wgs * s) / 256.0);
+    if (s > 1) us += 4.0 + 0.3 * s + 2.0 * s * (double)rows * (D + 2) * 4.0 / 3.0e6;
+    if (us < best_us) { best_us = us; best = s; }
+  }
+  return best;
+}
+
 template <int D>
 static void run_cross(int dtype, const CrossArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
-  const int64_t slots = cross_slots(c, dtype == 1 ? 128 : 32), wgs = slots * c.kv_heads;
+  const int64_t wgs = cross_slots(c, dtype == 1 ? 128 : 32) * c.kv_heads;
   const int64_t tiles = (c.n_k / c.n_kv_seqs + CR_BK - 1) / CR_BK;
   const int64_t rows = (int64_t)c.n_q * c.heads;
-  const int splits = (int)std::max<int64_t>(
-      1, std::min(std::min<int64_t>(768 / std::max<int64_t>(wgs, 1), tiles / 4),
-                  std::min<int64_t>(64, ws_floats / (rows * (D + 2)))));
+  const int splits = cross_splits(wgs, tiles, rows, D, ws_floats);
   const Partial p{ws, ws + splits * rows * D, splits};
   const dim3 grid((unsigned)wgs, splits);
-  if (dtype == 1) hipLaunchKernelGGL((cross_bf16<D>), grid, dim3(256), 0, st, c, (int)slots, p);
-  else hipLaunchKernelGGL((cross_f32<D>), grid, dim3(256), 0, st, c, (int)slots, p);
+  if (dtype == 1) hipLaunchKernelGGL((cross_bf16<D>), grid, dim3(256), 0, st, c, p);
+  else hipLaunchKernelGGL((cross_f32<D>), grid, dim3(256), 0, st, c, p);
   if (splits > 1) {
     const unsigned n = (unsigned)((rows + 3) / 4);
     if (dtype == 1) hipLaunchKernelGGL((cross_join<bf16_t, D>), dim3(n), dim3(256), 0, st, c, p);
