@@ -193,23 +193,45 @@ def _ptr(t, dtype=None, numel=None, name="tensor"):
     return t.data_ptr()
 
 
-def _rows(t, dtype, shape, name):
-    """Device pointer and row stride of a GPU tensor of `shape` whose rows are
-    contiguous (None -> NULL); the rows themselves may lie further apart."""
+def _rows(t, dtype, shape, name, device):
+    """Device pointer and row stride of a tensor of `shape` on GPU `device` whose
+    rows are contiguous (None -> NULL); the rows themselves may lie further
+    apart."""
     if t is None:
         return None, 0
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
-    width = 1
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on GPU {t.get_device()}, the context on {device}")
+    width = shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    if t.is_contiguous():
+        return t.data_ptr(), width
+    run = 1
     for n, step in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
-        if n != 1 and step != width:
+        if n != 1 and step != run:
             raise ValueError(f"{name} must have contiguous rows")
-        width *= n
+        run *= n
     return t.data_ptr(), t.stride(0) if shape[0] > 1 else width
+
+
+def _vec(t, dtype, numel, name, device):
+    """Device pointer of a contiguous tensor of at least `numel` elements on GPU
+    `device` (None -> NULL)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() < numel or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, with {numel} elements (it has {t.numel()})")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on GPU {t.get_device()}, the context on {device}")
+    return t.data_ptr()
 
 
 class Model:
@@ -270,6 +292,7 @@ class Context:
         self.plan = plan(self.c_cfg)
         self.act_dtype = torch.bfloat16 if self.c_cfg.dtype == SWAM_BF16 else torch.float32
         self.stream = stream or torch.cuda.current_stream()
+        self.device = self.stream.device.index   # the GPU that the operators' tensors lie on
         h = C.c_void_p()
         _check(self.lib, None, self.lib.swam_create(C.byref(self.c_cfg),
                                                     C.c_void_p(self.stream.cuda_stream),
@@ -493,56 +516,54 @@ class Context:
         return kind.value
 
     # -- 8-bit, encoder-conditioned block (include/swam_ops.h) -------------------------
-    def _here(self, **tensors):
-        """Every tensor lies on the context's device."""
-        for name, t in tensors.items():
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != self.stream.device:
-                raise ValueError(f"{name} is on {t.device}, the context on {self.stream.device}")
-
     def rms_norm_i8(self, x, q, q_scale, residual=None, sum_out=None, gain=None, shift=None,
                     scale=None, eps: float = 1e-6):
         """q, q_scale = 8-bit codes of RMSnorm(x + residual) gain (1 + scale) + shift, a scale
         per row.  x, residual, sum_out [rows][d] (sum_out receives x + residual and may be
         either of them), gain [d] in the context's dtype; shift, scale float [d]; q int8
         [rows][d]; q_scale float [rows]."""
-        self._here(x=x, q=q, q_scale=q_scale, residual=residual, sum_out=sum_out, gain=gain, shift=shift,
-                   scale=scale)
-        rows, d = x.shape
-        f32 = torch.float32
-        xp, xs = _rows(x, self.act_dtype, (rows, d), "x")
-        rp, rs = _rows(residual, self.act_dtype, (rows, d), "residual")
-        sp, ss = _rows(sum_out, self.act_dtype, (rows, d), "sum_out")
-        qp, qs = _rows(q, torch.int8, (rows, d), "q")
-        self._ok(self.lib.swam_rms_norm_i8(
-            self.h, xp, xs, rp, rs, _ptr(gain, self.act_dtype, d, "gain"), _ptr(shift, f32, d, "shift"),
-            _ptr(scale, f32, d, "scale"), float(eps), rows, d, sp, ss, qp, qs,
-            _ptr(q_scale, f32, rows, "q_scale")))
+        shape, act, f32, dev = x.shape, self.act_dtype, torch.float32, self.device
+        rows, d = shape
+        xp, xs = _rows(x, act, shape, "x", dev)
+        rp, rs = _rows(residual, act, shape, "residual", dev)
+        sp, ss = _rows(sum_out, act, shape, "sum_out", dev)
+        qp, qs = _rows(q, torch.int8, shape, "q", dev)
+        rc = self.lib.swam_rms_norm_i8(
+            self.h, xp, xs, rp, rs, _vec(gain, act, d, "gain", dev), _vec(shift, f32, d, "shift", dev),
+            _vec(scale, f32, d, "scale", dev), eps, rows, d, sp, ss, qp, qs,
+            _vec(q_scale, f32, rows, "q_scale", dev))
+        if rc:
+            self._ok(rc)
 
     def quantize_i8(self, x, q, q_scale):
         """q int8 [rows][d], q_scale float [rows] = 8-bit codes of the rows of x with a scale
         each: activations per token, a weight [out][in] per output channel."""
-        self._here(x=x, q=q, q_scale=q_scale)
-        rows, d = x.shape
-        xp, xs = _rows(x, self.act_dtype, (rows, d), "x")
-        qp, qs = _rows(q, torch.int8, (rows, d), "q")
-        self._ok(self.lib.swam_quantize_i8(self.h, xp, xs, rows, d, qp, qs,
-                                           _ptr(q_scale, torch.float32, rows, "q_scale")))
+        shape, dev = x.shape, self.device
+        rows, d = shape
+        xp, xs = _rows(x, self.act_dtype, shape, "x", dev)
+        qp, qs = _rows(q, torch.int8, shape, "q", dev)
+        rc = self.lib.swam_quantize_i8(self.h, xp, xs, rows, d, qp, qs,
+                                       _vec(q_scale, torch.float32, rows, "q_scale", dev))
+        if rc:
+            self._ok(rc)
 
     def gemm_i8(self, a, a_scale, w, w_scale, c, bias=None, residual=None, gate=None, gelu: bool = False):
         """c [m][n] = z, GELU(z) or residual + gate z with z = (a_scale a) (w_scale w)^T + bias:
         a int8 [m][k], w int8 [n][k], a_scale float [m], w_scale float [n], bias [n] and
         residual [m][n] (may be c) in the context's dtype, gate float [n]."""
-        self._here(a=a, a_scale=a_scale, w=w, w_scale=w_scale, c=c, bias=bias, residual=residual, gate=gate)
+        act, i8, f32, dev = self.act_dtype, torch.int8, torch.float32, self.device
         (m, k), n = a.shape, w.shape[0]
-        f32 = torch.float32
-        ap, lda = _rows(a, torch.int8, (m, k), "a")
-        wp, ldw = _rows(w, torch.int8, (n, k), "w")
-        rp, ldr = _rows(residual, self.act_dtype, (m, n), "residual")
-        cp, ldc = _rows(c, self.act_dtype, (m, n), "c")
-        self._ok(self.lib.swam_gemm_i8(
-            self.h, ap, lda, _ptr(a_scale, f32, m, "a_scale"), wp, ldw, _ptr(w_scale, f32, n, "w_scale"),
-            _ptr(bias, self.act_dtype, n, "bias"), rp, ldr, _ptr(gate, f32, n, "gate"),
-            GEMM_GELU if gelu else 0, cp, ldc, m, n, k))
+        out = (m, n)
+        ap, lda = _rows(a, i8, (m, k), "a", dev)
+        wp, ldw = _rows(w, i8, (n, k), "w", dev)
+        rp, ldr = _rows(residual, act, out, "residual", dev)
+        cp, ldc = _rows(c, act, out, "c", dev)
+        rc = self.lib.swam_gemm_i8(
+            self.h, ap, lda, _vec(a_scale, f32, m, "a_scale", dev), wp, ldw, _vec(w_scale, f32, n, "w_scale", dev),
+            _vec(bias, act, n, "bias", dev), rp, ldr, _vec(gate, f32, n, "gate", dev),
+            GEMM_GELU if gelu else 0, cp, ldc, m, n, k)
+        if rc:
+            self._ok(rc)
 
     def cross_attention(self, q, k, v, o, cu_q=None, cu_k=None, kv_seq=None, key_mask=None,
                         scale: float | None = None, lse=None):
@@ -551,25 +572,26 @@ class Context:
         sequence); kv_seq: int32, the key sequence of each query sequence (None: its own);
         key_mask: bool or uint8 [n_k], 0 hides a key; scale: 1 / sqrt(head_dim) by default;
         lse float [n_q][heads] receives the normalisers."""
-        self._here(q=q, k=k, v=v, o=o, cu_q=cu_q, cu_k=cu_k, kv_seq=kv_seq, key_mask=key_mask, lse=lse)
+        act, i32, dev = self.act_dtype, torch.int32, self.device
         (n_q, heads, dim), (n_k, kv_heads, _) = q.shape, k.shape
-        i32 = torch.int32
-        qp, qs = _rows(q, self.act_dtype, (n_q, heads, dim), "q")
-        kp, ks = _rows(k, self.act_dtype, (n_k, kv_heads, dim), "k")
-        vp, vs = _rows(v, self.act_dtype, (n_k, kv_heads, dim), "v")
-        op, os_ = _rows(o, self.act_dtype, (n_q, heads, dim), "o")
-        if key_mask is not None and key_mask.dtype not in (torch.bool, torch.uint8):
-            raise TypeError(f"key_mask must be bool or uint8, got {key_mask.dtype}")
+        keys = (n_k, kv_heads, dim)
+        qp, qs = _rows(q, act, q.shape, "q", dev)
+        kp, ks = _rows(k, act, keys, "k", dev)
+        vp, vs = _rows(v, act, keys, "v", dev)
+        op, os_ = _rows(o, act, q.shape, "o", dev)
+        mp = None
+        if key_mask is not None:
+            mp = _vec(key_mask, torch.uint8 if key_mask.dtype is torch.uint8 else torch.bool, n_k, "key_mask", dev)
         n_kv = 1 if cu_k is None else cu_k.numel() - 1
         n_seqs = 1 if cu_q is None else cu_q.numel() - 1
         if kv_seq is not None and kv_seq.numel() != n_seqs:
             raise ValueError(f"kv_seq has {kv_seq.numel()} elements, needs {n_seqs}")
-        self._ok(self.lib.swam_cross_attention(
-            self.h, qp, qs, kp, ks, vp, vs, _ptr(key_mask, None, n_k, "key_mask"),
-            _ptr(cu_q, i32, None, "cu_q"), _ptr(cu_k, i32, None, "cu_k"), _ptr(kv_seq, i32, None, "kv_seq"),
-            n_seqs, n_kv, n_q, n_k, heads, kv_heads, dim,
-            float(dim ** -0.5 if scale is None else scale), op, os_,
-            _ptr(lse, torch.float32, n_q * heads, "lse")))
+        rc = self.lib.swam_cross_attention(
+            self.h, qp, qs, kp, ks, vp, vs, mp, _vec(cu_q, i32, 0, "cu_q", dev), _vec(cu_k, i32, 0, "cu_k", dev),
+            _vec(kv_seq, i32, 0, "kv_seq", dev), n_seqs, n_kv, n_q, n_k, heads, kv_heads, dim,
+            dim ** -0.5 if scale is None else scale, op, os_, _vec(lse, torch.float32, n_q * heads, "lse", dev))
+        if rc:
+            self._ok(rc)
 
     # -- timers ------------------------------------------------------------------
     def timer_enable(self, classes, capacity=8192):
