@@ -54,8 +54,7 @@ extern "C" {
  *   gain     : act [d] or NULL;  shift, scale : float [d], both or neither
  *   q        : int8 [rows][d], row stride q_stride;  q_scale : float [rows]
  * 1 <= d <= SWAM_I8_MAX_WIDTH, 0 <= rows < 2^31, eps >= 0 and finite.  Any alignment of
- * the element type; 16-byte aligned rows (8-byte for q) with d a multiple of 8
- * are read and written in vectors. */
+ * the element type. */
 int swam_rms_norm_i8(swam_ctx* ctx, const void* x, int64_t x_stride, const void* residual,
                      int64_t residual_stride, const void* gain, const float* shift,
                      const float* scale, float eps, int64_t rows, int64_t d, void* sum_out,

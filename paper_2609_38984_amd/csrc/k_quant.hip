@@ -10,6 +10,8 @@
 // sum + 1) bytes).
 #include "launchers.h"
 
+#include <type_traits>
+
 namespace swam {
 
 // Bits of |v|: as unsigned integers they order like the magnitudes, with
@@ -100,16 +102,60 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v, uint32_t* red) {
   return v;
 }
 
-// Aligned rows of up to NW * 64 * 8 * NV elements in registers: NW waves to a
-// row, lane t holding the 8-element vectors t, t + 64 NW, ...  NW = 1 puts four
-// rows on a workgroup and needs no barrier.
-template <typename T, bool NORM, int NW, int NV>
-__global__ void __launch_bounds__(256)
+// 8 elements at p, of which the first n are inside the row (n <= 0: none), as float32,
+// and back; WHOLE: rows of whole vectors, n is never 1..7.  A vector moves in one access at any alignment of the element type
+// (the hardware takes unaligned vectors; scalar accesses reach a third of the rate:
+// 17,472 x 8,192 bf16 with rows 10 bytes off 200 us, with vectors 100).
+template <typename T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void row_load8(const T* p, int n, float (&o)[8]) {
+  if (n >= 8) {
+    Raw8<T> r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[2 * e] = __uint_as_float(r.w[e] << 16);
+        o[2 * e + 1] = __uint_as_float(r.w[e] & 0xFFFF0000u);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(r.w[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = !WHOLE && e < n ? Elem<T>::load(p + e) : 0.0f;
+  }
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void row_store8(T* p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.w[e] = __float_as_uint(v[e]);
+    }
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!WHOLE && e < n) Elem<T>::store(p + e, v[e]);
+  }
+}
+
+// Rows of up to NW * 64 * 8 * NV elements in registers: NW waves to a row, lane t
+// holding the 8-element vectors t, t + 64 NW, ...  NW = 1 puts four rows on a workgroup
+// and needs no barrier.
+template <typename T, bool NORM, bool WHOLE, int NW, int NV>
+__global__ void __launch_bounds__(NW < 4 ? 256 : NW * 64)
 quant_rows(const RowQuant a) {
-  constexpr int TPR = NW * 64, RPW = 4 / NW;
-  __shared__ float red[4];
-  __shared__ uint32_t redu[4];
-  const int64_t row = (int64_t)blockIdx.x * RPW + (NW == 4 ? 0 : threadIdx.x / TPR);
+  constexpr int TPR = NW * 64, RPW = NW == 1 ? 4 : 1;
+  __shared__ float red[NW];
+  __shared__ uint32_t redu[NW];
+  const int64_t row = (int64_t)blockIdx.x * RPW + (NW == 1 ? threadIdx.x / TPR : 0);
   if (row >= a.rows) return;                    // whole waves
   const int t = threadIdx.x % TPR, d = a.d;
   const T* xp = (const T*)a.x + row * a.x_ld;
@@ -117,12 +163,7 @@ quant_rows(const RowQuant a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int e = (i * TPR + t) * 8;
-    if (e < d) {
-      load8(xp + e, v[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-    }
+    row_load8<WHOLE>(xp + e, d - e, v[i]);
   }
   if constexpr (NORM) {
     float ss = 0.0f;
@@ -131,12 +172,10 @@ quant_rows(const RowQuant a) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int e = (i * TPR + t) * 8;
-        if (e < d) {
-          float r[8];
-          load8(rp + e, r);
+        float r[8];
+        row_load8<WHOLE>(rp + e, d - e, r);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] += r[j];
-        }
+        for (int j = 0; j < 8; ++j) v[i][j] += r[j];
       }
     }
     if (a.sum != nullptr) {
@@ -144,7 +183,7 @@ quant_rows(const RowQuant a) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int e = (i * TPR + t) * 8;
-        if (e < d) store8(sp + e, v[i]);
+        row_store8<WHOLE>(sp + e, d - e, v[i]);
       }
     }
 #pragma unroll
@@ -161,14 +200,14 @@ quant_rows(const RowQuant a) {
         for (int j = 0; j < 8; ++j) v[i][j] *= r;
         if (a.gain != nullptr) {
           float g[8];
-          load8((const T*)a.gain + e, g);
+          row_load8<WHOLE>((const T*)a.gain + e, d - e, g);
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
         }
         if (a.shift != nullptr) {
           float sc[8], sh[8];
-          load8(a.scale + e, sc);
-          load8(a.shift + e, sh);
+          row_load8<WHOLE>(a.scale + e, d - e, sc);
+          row_load8<WHOLE>(a.shift + e, d - e, sh);
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j], 1.0f + sc[j], sh[j]);
         }
@@ -189,90 +228,50 @@ quant_rows(const RowQuant a) {
       int c[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) c[j] = code_of<!NORM>(v[i][j], rs);
-      *reinterpret_cast<uint2*>(qp + e) = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
+      if (WHOLE || d - e >= 8) {
+        const uint32_t w[2] = {pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7])};
+        __builtin_memcpy(qp + e, w, 8);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (e + j < d) qp[e + j] = (int8_t)c[j];
+      }
     }
   }
   if (t == 0) a.q_scale[row] = rs.s;
 }
 
-// Any alignment and width: the row in LDS as float32, one row to a workgroup.
-template <typename T, bool NORM, int CAP>
-__global__ void __launch_bounds__(512)
-quant_rows_any(const RowQuant a) {
-  __shared__ float buf[CAP];
-  __shared__ float red[8];
-  __shared__ uint32_t redu[8];
-  const int64_t row = blockIdx.x;
-  const int d = a.d, t = threadIdx.x;
-  const T* xp = (const T*)a.x + row * a.x_ld;
-  float r = 1.0f;
-  if constexpr (NORM) {
-    float ss = 0.0f;
-    for (int e = t; e < d; e += 512) {
-      float v = Elem<T>::load(xp + e);
-      if (a.res != nullptr) v += Elem<T>::load((const T*)a.res + row * a.res_ld + e);
-      if (a.sum != nullptr) Elem<T>::store((T*)a.sum + row * a.sum_ld + e, v);
-      buf[e] = v;
-      ss = fmaf(v, v, ss);
-    }
-    ss = row_sum<8>(ss, red);
-    r = inv_rms(ss, d, a.eps);
-  }
-  uint32_t top = 0;
-  for (int e = t; e < d; e += 512) {            // every thread its own elements of buf
-    float v;
-    if constexpr (NORM) {
-      v = buf[e] * r;
-      if (a.gain != nullptr) v *= Elem<T>::load((const T*)a.gain + e);
-      if (a.shift != nullptr) v = fmaf(v, 1.0f + a.scale[e], a.shift[e]);
-    } else {
-      v = Elem<T>::load(xp + e);
-    }
-    buf[e] = v;
-    top = max(top, mag_bits(v));
-  }
-  const RowScale rs = row_scale(row_umax<8>(top, redu));
-  for (int e = t; e < d; e += 512) a.q[row * a.q_ld + e] = (int8_t)code_of<!NORM>(buf[e], rs);
-  if (t == 0) a.q_scale[row] = rs.s;
-}
-
-template <typename T, bool NORM>
-static void run_quant(const RowQuant& a, bool vec, hipStream_t st) {
+template <typename T, bool NORM, bool WHOLE>
+static void run_quant(const RowQuant& a, hipStream_t st) {
   const int vecs = (a.d + 7) / 8;
-#define SWAM_Q(NW_, NV_)                                                                         \
-  hipLaunchKernelGGL((quant_rows<T, NORM, NW_, NV_>), dim3((unsigned)((a.rows + 4 / NW_ - 1) / (4 / NW_))), \
-                     dim3(256), 0, st, a)
-  if (vec && vecs <= 256) {
-    if (vecs <= 64) SWAM_Q(1, 1);
-    else if (vecs <= 128) SWAM_Q(1, 2);
-    else if (vecs <= 192) SWAM_Q(1, 3);
-    else SWAM_Q(1, 4);
-  } else if (vec && vecs <= 1024) {
-    if (vecs <= 512) SWAM_Q(4, 2);
-    else SWAM_Q(4, 4);
-  } else if (a.d <= 8192) {
-    hipLaunchKernelGGL((quant_rows_any<T, NORM, 8192>), dim3((unsigned)a.rows), dim3(512), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((quant_rows_any<T, NORM, 32768>), dim3((unsigned)a.rows), dim3(512), 0, st, a);
-  }
+#define SWAM_Q(NW_, NV_)                                                                                   \
+  hipLaunchKernelGGL((quant_rows<T, NORM, WHOLE, NW_, NV_>), dim3((unsigned)(NW_ == 1 ? (a.rows + 3) / 4 : a.rows)), \
+                     dim3(NW_ == 1 ? 256 : NW_ * 64), 0, st, a)
+  if (vecs <= 64) SWAM_Q(1, 1);
+  else if (vecs <= 128) SWAM_Q(1, 2);
+  else if (vecs <= 192) SWAM_Q(1, 3);
+  else if (vecs <= 256) SWAM_Q(1, 4);
+  else if (vecs <= 512) SWAM_Q(4, 2);
+  else if (vecs <= 1024) SWAM_Q(4, 4);
+  else if (vecs <= 2048) SWAM_Q(16, 2);
+  else SWAM_Q(16, 4);
 #undef SWAM_Q
 }
 
 hipError_t launch_quant_rows(int dtype, bool norm, const RowQuant& a, hipStream_t st) {
   if (a.rows <= 0) return hipSuccess;
-  const int esz = dtype == 1 ? 2 : 4;
-  auto row16 = [&](const void* p, int64_t ld) {
-    return p == nullptr || (((uintptr_t)p | (uintptr_t)(ld * esz)) & 15) == 0;
+  auto run = [&](auto type, auto with_norm) {
+    using T = decltype(type);
+    constexpr bool N = decltype(with_norm)::value;
+    if (a.d % 8 == 0) run_quant<T, N, true>(a, st);
+    else run_quant<T, N, false>(a, st);
   };
-  const bool vec = a.d % 8 == 0 && row16(a.x, a.x_ld) && row16(a.res, a.res_ld) && row16(a.sum, a.sum_ld) &&
-                   row16(a.gain, 0) && (((uintptr_t)a.shift | (uintptr_t)a.scale) & 15) == 0 &&
-                   (((uintptr_t)a.q | (uintptr_t)a.q_ld) & 7) == 0;
   if (dtype == 1) {
-    if (norm) run_quant<bf16_t, true>(a, vec, st);
-    else run_quant<bf16_t, false>(a, vec, st);
+    if (norm) run(bf16_t{}, std::true_type{});
+    else run(bf16_t{}, std::false_type{});
   } else {
-    if (norm) run_quant<float, true>(a, vec, st);
-    else run_quant<float, false>(a, vec, st);
+    if (norm) run(float{}, std::true_type{});
+    else run(float{}, std::false_type{});
   }
   return hipGetLastError();
 }
