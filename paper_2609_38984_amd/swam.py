@@ -193,20 +193,26 @@ def _ptr(t, dtype=None, numel=None, name="tensor"):
     return t.data_ptr()
 
 
+def _refuse(t, dtype, name, device):
+    """The error for a tensor of another kind, type or GPU."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on GPU {t.get_device()}, the context on {device}")
+
+
 def _rows(t, dtype, shape, name, device):
     """Device pointer and row stride of a tensor of `shape` on GPU `device` whose
     rows are contiguous (None -> NULL); the rows themselves may lie further
     apart."""
     if t is None:
         return None, 0
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        _refuse(t, dtype, name, device)
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name} is on GPU {t.get_device()}, the context on {device}")
     width = shape[1] if len(shape) == 2 else shape[1] * shape[2]
     if t.is_contiguous():
         return t.data_ptr(), width
@@ -223,14 +229,10 @@ def _vec(t, dtype, numel, name, device):
     `device` (None -> NULL)."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        _refuse(t, dtype, name, device)
     if t.numel() < numel or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous, with {numel} elements (it has {t.numel()})")
-    if t.get_device() != device:
-        raise ValueError(f"{name} is on GPU {t.get_device()}, the context on {device}")
     return t.data_ptr()
 
 
