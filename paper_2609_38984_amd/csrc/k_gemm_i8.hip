@@ -63,15 +63,23 @@ __device__ __forceinline__ void i8_load8(const T* p, bool whole, int n, float fi
   }
 }
 
+// how the output is stored: whole, 16-byte aligned runs of 8 columns in every operand of
+// the epilogue; larger than the 256 MB cache behind the L2 (stored past the caches, which
+// then keep A and B: 17,472 x 8,192 x 2,048 317 us, through them 325)
+enum { I8_ALIGNED = 1, I8_PAST_CACHE = 2 };
+constexpr int64_t I8_CACHE_BYTES = 256 << 20;
+
 // What a lane needs to finish its 8 columns, the same in every row that it stores.
 template <typename T>
 struct I8Cols {
   float sb[8], bias[8], gate[8];
   int n;          // columns inside N
   bool vec;       // whole, 16-byte aligned runs
-  __device__ __forceinline__ void load(const GemmI8& g, int col, bool aligned) {
+  bool past;      // stores that no cache needs to keep
+  __device__ __forceinline__ void load(const GemmI8& g, int col, int how) {
     n = (int)max(min((int64_t)8, g.N - col), (int64_t)0);
-    vec = aligned && n == 8;
+    vec = (how & I8_ALIGNED) && n == 8;
+    past = how & I8_PAST_CACHE;
     i8_load8(g.b_scale + col, vec, n, 0.0f, sb);
 #pragma unroll
     for (int e = 0; e < 8; ++e) { bias[e] = 0.0f; gate[e] = 1.0f; }
@@ -93,7 +101,14 @@ struct I8Cols {
     }
     T* cp = (T*)g.c + row * g.ldc + col;
     if (vec) {
-      store8(cp, z);
+      if (sizeof(T) == 2 && past) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 w = {pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]),
+                         pack_bf16x2(z[6], z[7])};
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(cp));
+      } else {
+        store8(cp, z);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -108,7 +123,7 @@ struct I8Cols {
 // epilogue.  A ring holds NSA stages of A and NSB of B.
 template <typename T, int WM, int WN, int FM, int FN, int SK, int GK, int NSA, int NSB, int WPE>
 __global__ void __launch_bounds__(WM * WN * SK * GK * 64) __attribute__((amdgpu_waves_per_eu(WPE, 8)))
-gemm_i8(const GemmI8 g, int aligned, int tiles_m, int tiles_n) {
+gemm_i8(const GemmI8 g, int how, int tiles_m, int tiles_n) {
   constexpr int NG = WM * WN, NR = NG * SK, WK = SK * GK, NW = NG * WK;
   constexpr int TM = FM * 32, TN = FN * 32, BM = WM * TM, BN = WN * TN, KPW = 4 / SK;
   constexpr int A_INS = BM / 8 / NR, B_INS = BN / 8 / NR;
@@ -247,7 +262,7 @@ gemm_i8(const GemmI8 g, int aligned, int tiles_m, int tiles_n) {
   const int cl = (lane % CPR) * 8, col = n0 + wn * TN + cl;
   auto run_row = [&](int t) { return (lane + 64 * (t * WK + wk)) / CPR; };   // 32 and more: none
   I8Cols<T> cols;
-  cols.load(g, col, aligned);
+  cols.load(g, col, how);
   float tok[FM][ITS];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -309,10 +324,10 @@ gemm_i8(const GemmI8 g, int aligned, int tiles_m, int tiles_n) {
 }
 
 template <typename T, int WM, int WN, int FM, int FN, int SK, int GK, int NSA, int NSB, int WPE>
-static void run_i8(const GemmI8& g, int aligned, hipStream_t st) {
+static void run_i8(const GemmI8& g, int how, hipStream_t st) {
   const int tm = (int)((g.M + WM * FM * 32 - 1) / (WM * FM * 32)), tn = (int)((g.N + WN * FN * 32 - 1) / (WN * FN * 32));
   hipLaunchKernelGGL((gemm_i8<T, WM, WN, FM, FN, SK, GK, NSA, NSB, WPE>), dim3(tm * tn),
-                     dim3(WM * WN * SK * GK * 64), 0, st, g, aligned, tm, tn);
+                     dim3(WM * WN * SK * GK * 64), 0, st, g, how, tm, tn);
 }
 
 // Tiles, and the choice among them by modelled time: t0 + n (fill + step stages),
@@ -353,18 +368,19 @@ template <typename T>
 static void run_gemm_i8(const GemmI8& g, hipStream_t st) {
   const int esz = sizeof(T);
   auto row16 = [&](const void* p, int64_t ld) { return (((uintptr_t)p | (uintptr_t)(ld * esz)) & 15) == 0; };
-  const int aligned = row16(g.c, g.ldc) && row16(g.res, g.res ? g.ldr : 0) && row16(g.bias, 0) &&
-                      (((uintptr_t)g.b_scale | (uintptr_t)g.gate) & 15) == 0;
+  const bool aligned = row16(g.c, g.ldc) && row16(g.res, g.res ? g.ldr : 0) && row16(g.bias, 0) &&
+                       (((uintptr_t)g.b_scale | (uintptr_t)g.gate) & 15) == 0;
+  const int how = (aligned ? I8_ALIGNED : 0) | (g.M * g.N * esz > I8_CACHE_BYTES ? I8_PAST_CACHE : 0);
   switch (choose_i8(g.M, g.N, g.K)) {
-    case 0: return run_i8<T, 2, 4, 4, 2, 1, 1, 3, 2, 2>(g, aligned, st);
-    case 1: return run_i8<T, 2, 2, 3, 2, 1, 1, 2, 2, 2>(g, aligned, st);
-    case 2: return run_i8<T, 2, 2, 3, 2, 2, 1, 4, 4, 2>(g, aligned, st);
-    case 3: return run_i8<T, 2, 2, 2, 2, 1, 1, 2, 2, 2>(g, aligned, st);
-    case 4: return run_i8<T, 2, 2, 2, 2, 2, 1, 5, 5, 2>(g, aligned, st);
-    case 5: return run_i8<T, 2, 2, 1, 2, 2, 1, 3, 3, 2>(g, aligned, st);
-    case 6: return run_i8<T, 2, 2, 1, 1, 1, 2, 4, 4, 2>(g, aligned, st);
-    case 7: return run_i8<T, 1, 1, 1, 1, 1, 4, 2, 2, 2>(g, aligned, st);
-    default: return run_i8<T, 1, 1, 1, 1, 1, 4, 4, 4, 2>(g, aligned, st);
+    case 0: return run_i8<T, 2, 4, 4, 2, 1, 1, 3, 2, 2>(g, how, st);
+    case 1: return run_i8<T, 2, 2, 3, 2, 1, 1, 2, 2, 2>(g, how, st);
+    case 2: return run_i8<T, 2, 2, 3, 2, 2, 1, 4, 4, 2>(g, how, st);
+    case 3: return run_i8<T, 2, 2, 2, 2, 1, 1, 2, 2, 2>(g, how, st);
+    case 4: return run_i8<T, 2, 2, 2, 2, 2, 1, 5, 5, 2>(g, how, st);
+    case 5: return run_i8<T, 2, 2, 1, 2, 2, 1, 3, 3, 2>(g, how, st);
+    case 6: return run_i8<T, 2, 2, 1, 1, 1, 2, 4, 4, 2>(g, how, st);
+    case 7: return run_i8<T, 1, 1, 1, 1, 1, 4, 2, 2, 2>(g, how, st);
+    default: return run_i8<T, 1, 1, 1, 1, 1, 4, 4, 4, 2>(g, how, st);
   }
 }
 
