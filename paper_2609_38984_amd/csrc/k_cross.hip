@@ -67,11 +67,11 @@ __device__ __forceinline__ bool tile_at(const CrossArgs& c, int group, int bq, i
   return true;
 }
 
-// tiles [t0, t1) of the keys of one of `splits` slices
-__device__ __forceinline__ void slice_of(int s0, int s1, int bk, int y, int splits, int& t0, int& t1) {
+// tiles [t0, t1) of the keys of slice y of 2^lg
+__device__ __forceinline__ void slice_of(int s0, int s1, int bk, int y, int lg, int& t0, int& t1) {
   const int64_t n = (s1 - s0 + bk - 1) / bk;
-  t0 = (int)(n * y / splits);
-  t1 = (int)(n * (y + 1) / splits);
+  t0 = (int)(n * y >> lg);
+  t1 = (int)(n * (y + 1) >> lg);
 }
 
 // partial results of slice y: [y][token][head][head_dim] sums, then [y][token][head][2]
@@ -79,7 +79,7 @@ __device__ __forceinline__ void slice_of(int s0, int s1, int bk, int y, int spli
 struct Partial {
   float* o;
   float* ml;
-  int splits;
+  int splits, lg;     // splits = 2^lg
 };
 
 // Four waves of 32 rows each.
@@ -110,7 +110,7 @@ cross_bf16(const CrossArgs c, const Partial part) {
       qf[s] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 8 * (2 * s + g)));
   }
   int t0, t1;
-  slice_of(ta.s0, ta.s1, CR_BK, blockIdx.y, part.splits, t0, t1);
+  slice_of(ta.s0, ta.s1, CR_BK, blockIdx.y, part.lg, t0, t1);
 
   // whether this lane's key of tile t is visible
   auto mask_byte = [&](int t) -> int {
@@ -181,7 +181,7 @@ cross_bf16(const CrossArgs c, const Partial part) {
   // one tile of keys; `fresh`: the first visible one
   auto tile = [&](const uint4 (&from)[2][TILE], uint64_t vis, bool fresh, auto masked) {
     const uint4* Kt = from[0];
-    auto scores = [&](f32x16 (&st)[2]) {
+    auto scores = [&](f32x16 (&st)[2], uint64_t vis) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -222,15 +222,17 @@ cross_bf16(const CrossArgs c, const Partial part) {
     };
     if (!fresh) {
       f32x16 st[2];
-      scores(st);
+      scores(st, vis);
       probs(st);
     }
     // the running maximum moves only when a row sum shows that some weight passed
     // 2^8 (or is NaN): the scores are then formed again against the new one
     if (fresh || __any(!(ps0 + ps1 <= 256.0f))) {
-      asm volatile("" ::: "memory");
+      // formed anew: neither operands nor masks of the first time are kept for this
+      uint64_t again = vis;
+      asm volatile("" : "+s"(again) : : "memory");
       f32x16 st[2];
-      scores(st);
+      scores(st, again);
       float mx = st[0][0];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -346,7 +348,7 @@ cross_f32(const CrossArgs c, const Partial part) {
     for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 4 * (2 * s + g));
   }
   int t0, t1;
-  slice_of(ta.s0, ta.s1, 32, blockIdx.y, part.splits, t0, t1);
+  slice_of(ta.s0, ta.s1, 32, blockIdx.y, part.lg, t0, t1);
   f32x16 o[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t)
@@ -518,7 +520,7 @@ static void run_cross(int dtype, const CrossArgs& c, float* ws, int64_t ws_float
   const int64_t tiles = (c.n_k / c.n_kv_seqs + CR_BK - 1) / CR_BK;
   const int64_t rows = (int64_t)c.n_q * c.heads;
   const int splits = cross_splits(wgs, tiles, rows, D, ws_floats);
-  const Partial p{ws, ws + splits * rows * D, splits};
+  const Partial p{ws, ws + splits * rows * D, splits, __builtin_ctz(splits)};
   const dim3 grid((unsigned)wgs, splits);
   if (dtype == 1) hipLaunchKernelGGL((cross_bf16<D>), grid, dim3(256), 0, st, c, p);
   else hipLaunchKernelGGL((cross_f32<D>), grid, dim3(256), 0, st, c, p);
