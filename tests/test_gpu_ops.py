@@ -297,6 +297,48 @@ def test_gemm_extreme_codes_in_place_and_nan_scales(contexts, dtype):
     ctx.gemm_i8(a, sa, w[:0], sw[:0], torch.empty((200, 0), dtype=dt, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gemm_outputs_larger_than_the_cache(contexts, dtype):
+    """Stored past the caches where whole runs are aligned; ragged columns beside them."""
+    dt, g = TYPES[dtype], gen(11)
+    for m, n in ((8400, 16384), (8200, 16390)):
+        a, w = codes(m, 80, g), codes(n, 80, g)
+        sa = torch.rand(m, device="cuda", generator=g) * 0.02 + 1e-3
+        sw = torch.rand(n, device="cuda", generator=g) * 1e-3 + 1e-4
+        c = torch.full((m, n), 7.0, dtype=dt, device="cuda")
+        contexts[dtype].gemm_i8(a, sa, w, sw, c, gelu=True)
+        check_gemm(a, sa, w, sw, None, None, None, True, c)
+        r = torch.randn((m, n), device="cuda", generator=g).to(dt)
+        c.copy_(r)
+        contexts[dtype].gemm_i8(a, sa, w, sw, c, residual=c)
+        check_gemm(a, sa, w, sw, None, r, None, False, c)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_beyond_4_gb(contexts, dtype):
+    """Row offsets past 32 bits: codes, activations and outputs that are column ranges of
+    buffers of more than 4 GB."""
+    dt, g, ctx = TYPES[dtype], gen(12), contexts[dtype]
+    m, n, k, far = 1200, 72, 160, (1 << 22) - 16
+    big = torch.empty(m * far, dtype=torch.int8, device="cuda")          # 5.0 GB
+    a, w = big.view(m, far)[:, 64:64 + k], codes(n, k, g)
+    a.copy_(codes(m, k, g))
+    sa = torch.rand(m, device="cuda", generator=g) * 0.02 + 1e-3
+    sw = torch.rand(n, device="cuda", generator=g) * 1e-3 + 1e-4
+    out = torch.empty(m * far // 2, dtype=dt, device="cuda").view(m, far // 2)[:, 8:8 + n]
+    ctx.gemm_i8(a, sa, w, sw, out)
+    check_gemm(a, sa, w, sw, None, None, None, False, out)
+    # the rows of `out` to codes beside those of a, plain and through the norm
+    q, s = big.view(m, far)[:, 1024:1024 + n], torch.empty(m, device="cuda")
+    ctx.quantize_i8(out, q, s)
+    c, top = exact_codes(out.double())
+    assert torch.equal(q.double(), c) and torch.equal(s, (top / 127.0).float())
+    near, q2, s2 = out.contiguous(), torch.empty((m, n), dtype=torch.int8, device="cuda"), torch.empty_like(s)
+    ctx.rms_norm_i8(near, q2, s2, residual=near, sum_out=near)
+    ctx.rms_norm_i8(out, q, s, residual=out, sum_out=out)
+    assert torch.equal(q, q2) and torch.equal(s, s2) and torch.equal(out, near)
+
+
 # ---------------------------------------------------------------------------
 # cross attention
 # ---------------------------------------------------------------------------
