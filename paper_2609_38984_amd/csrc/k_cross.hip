@@ -14,7 +14,6 @@
 
 #include <algorithm>
 #include <cfloat>
-#include <type_traits>
 
 namespace swam {
 
@@ -82,9 +81,14 @@ struct Partial {
   int splits, lg;     // splits = 2^lg
 };
 
-// Four waves of 32 rows each.
+// Four waves of 32 rows each.  The registers decide at head_dim 64: with 128 of them four
+// waves share a SIMD, and what one waits for (LDS, its own chain from scores to weights
+// to products) the others hide.  So a tile has one body, masked behind a branch (a second
+// one for whole tiles keeps more alive: 154 registers, three waves), and what only the
+// end needs is formed there.  Four waves | three, 24 heads: 10,160 rows on 512 keys 47 us
+// | 56, on 2,048 156 | 183; 4,096 rows on 10,160 295 | 338 (870 TFLOP/s).
 template <int D>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, 8)))
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, 8)))
 cross_bf16(const CrossArgs c, const Partial part) {
   constexpr int H2 = D / 64;                     // 128-byte halves of a head's row
   constexpr int NW = 4, BQ = 32 * NW;
@@ -99,11 +103,11 @@ cross_bf16(const CrossArgs c, const Partial part) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r31 = lane & 31;
-  const int want = ta.r0 + wave * 32 + r31, rr = min(want, ta.rows - 1);
-  const int64_t tok = ta.a + rr / group;
-  const int head = hk * group + rr % group;
   bf16x8 qf[D / 16];
   {
+    const int rr = min(ta.r0 + wave * 32 + r31, ta.rows - 1);
+    const int64_t tok = ta.a + rr / group;
+    const int head = hk * group + rr % group;
     const bf16_t* qp = (const bf16_t*)c.q + tok * c.q_ld + head * D;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
@@ -114,18 +118,17 @@ cross_bf16(const CrossArgs c, const Partial part) {
 
   // whether this lane's key of tile t is visible
   auto mask_byte = [&](int t) -> int {
-    const int key = ta.s0 + t * CR_BK + lane;
+    const int key = ta.s0 + t * CR_BK + __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
     return t < t1 && key < ta.s1 && (c.mask == nullptr || c.mask[key] != 0);
   };
   const int lrow = lane >> 3;
   constexpr int SLABS = 8 * H2;                  // 8-row slabs of a tile
   static_assert(SLABS % NW == 0, "every wave stages whole slabs");
-  int off_k[SLABS / NW], off_v[SLABS / NW], row_of[SLABS / NW];
+  int off_k[SLABS / NW], off_v[SLABS / NW];
 #pragma unroll
   for (int j = 0; j < SLABS / NW; ++j) {
     const int slab = wave * (SLABS / NW) + j, half = slab >> 3;
     const int r = (slab & 7) * 8 + lrow, col = 64 * half + 8 * ((lane & 7) ^ lds_swz(r));
-    row_of[j] = r;
     off_k[j] = (r * (int)c.k_ld + col) * 2;
     off_v[j] = (r * (int)c.v_ld + col) * 2;
   }
@@ -147,7 +150,7 @@ cross_bf16(const CrossArgs c, const Partial part) {
     } else {
 #pragma unroll
       for (int j = 0; j < SLABS / NW; ++j) {
-        const bool see = (vis >> row_of[j]) & 1;
+        const bool see = (vis >> (8 * ((wave * (SLABS / NW) + j) & 7) + lrow)) & 1;
         cr_slab(rk, &to[0][at + j * 64], see ? off_k[j] : CR_PAST_END);
         cr_slab(rv, &to[1][at + j * 64], see ? off_v[j] : CR_PAST_END);
       }
@@ -157,14 +160,13 @@ cross_bf16(const CrossArgs c, const Partial part) {
   // V[key0 + (a >> 2)][col0 + 4 (a & 3)] and lane i receives keys key0..key0+3 of
   // column col0 + i, the order in which the P^T accumulators hold the keys
   const int a16 = lane & 15, G = lane >> 4, rlo = 4 * g + (a16 >> 2);
-  int vofs[2][2];
+  // (8 rows or 32 columns further the swizzle flips the same bit of the chunk)
+  int vofs[2];
 #pragma unroll
-  for (int ht = 0; ht < 2; ++ht)
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int r = rlo + 8 * hf, hd = 32 * ht + 16 * (G & 1) + 4 * (a16 & 3);
-      vofs[ht][hf] = r * 64 + 8 * ((hd >> 3) ^ lds_swz(r)) + (hd & 7);
-    }
+  for (int x = 0; x < 2; ++x) {
+    const int hd = 32 * x + 16 * (G & 1) + 4 * (a16 & 3);
+    vofs[x] = rlo * 64 + 8 * ((hd >> 3) ^ lds_swz(rlo)) + (hd & 7);
+  }
   int kofs[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) kofs[s] = r31 * 8 + ((2 * s + g) ^ lds_swz(r31));
@@ -179,7 +181,7 @@ cross_bf16(const CrossArgs c, const Partial part) {
   const float sc = LOG2E * c.scale;
 
   // one tile of keys; `fresh`: the first visible one
-  auto tile = [&](const uint4 (&from)[2][TILE], uint64_t vis, bool fresh, auto masked) {
+  auto tile = [&](const uint4 (&from)[2][TILE], uint64_t vis, bool fresh) {
     const uint4* Kt = from[0];
     auto scores = [&](f32x16 (&st)[2], uint64_t vis) {
 #pragma unroll
@@ -191,7 +193,7 @@ cross_bf16(const CrossArgs c, const Partial part) {
           const bf16x8 kf = __builtin_bit_cast(bf16x8, Kt[(s >> 2) * CR_BK * 8 + kofs[s & 3] + t * 32 * 8]);
           st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[t], 0, 0, 0);
         }
-        if constexpr (decltype(masked)::value) {
+        if (vis != ~(uint64_t)0) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             // register r holds key b of the lower 32 lanes and key b + 4 of the upper: the
@@ -258,8 +260,8 @@ cross_bf16(const CrossArgs c, const Partial part) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int base = (ht >> 1) * CR_BK * 64 + (32 * t + 16 * u) * 64;
-          const v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1][0] + base));
-          const v4i16 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1][1] + base));
+          const v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1] + base));
+          const v4i16 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[(ht & 1) ^ 1] + 8 * 64 + base));
           const uint2 w1 = __builtin_bit_cast(uint2, x1), w2 = __builtin_bit_cast(uint2, x2);
           const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(w1.x, w1.y, w2.x, w2.y));
           o[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t][u], o[ht], 0, 0, 0);
@@ -282,13 +284,17 @@ cross_bf16(const CrossArgs c, const Partial part) {
     }
     if (ahead) issue(kv[buf ^ 1], t + 1, ahead);
     next = mask_byte(t + 2);
-    if (vis == ~(uint64_t)0) tile(kv[buf], vis, fresh, std::false_type{});
-    else if (vis) tile(kv[buf], vis, fresh, std::true_type{});
+    if (vis) tile(kv[buf], vis, fresh);
     fresh = fresh && vis == 0;
     vis = ahead;
     buf ^= 1;
   }
   const float l = l_run + __shfl_xor(l_run, 32);
+  int me = tid;
+  asm volatile("" : "+v"(me));
+  const int want = ta.r0 + (me >> 6) * 32 + (me & 31), rr = min(want, ta.rows - 1);
+  const int64_t tok = ta.a + rr / group;
+  const int head = hk * group + rr % group;
   const int64_t row = tok * c.heads + head;
   if (part.splits > 1) {
     if (want >= ta.rows) return;
@@ -498,9 +504,9 @@ static int64_t cross_slots(const CrossArgs& c, int64_t bq) {
 // by modelled time (us): tiles per slice, each `lone` for a workgroup by itself and
 // `share` per workgroup where several share a CU, plus the pass that joins the
 // slices and what they write and read.  us without | with the chosen split: 8 x 1 query
-// of 24 heads on 10,160 keys 249 | 116 (4 slices), 32 x 24 on 2,048 40 | 15 (8), 300 x 16 on
-// 4,096 73 | 28 (8), 1 x 24 on 512 12 | 10; 4,096 x 12 on 512 (head_dim 128) 26 | 53 (2,
-// not chosen).
+// of 24 heads on 10,160 keys 240 | 118 (4 slices), 32 x 24 on 2,048 39 | 14 (8), 300 x 16 on
+// 4,096 70 | 25 (8), 326 x 24 on 2,048 38 | 24 (4); 512 x 24 on 512 11 | 17 (2, not chosen),
+// 4,096 x 12 on 512 (head_dim 128) 24 | 52 (2, not chosen).
 static int cross_splits(int64_t wgs, int64_t tiles, int64_t rows, int D, int64_t ws_floats) {
   const double lone = D == 64 ? 1.2 : 1.6, share = D == 64 ? 0.64 : 1.0;
   int best = 1;
