@@ -103,9 +103,10 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v, uint32_t* red) {
 }
 
 // 8 elements at p, of which the first n are inside the row (n <= 0: none), as float32,
-// and back; WHOLE: rows of whole vectors, n is never 1..7.  A vector moves in one access at any alignment of the element type
-// (the hardware takes unaligned vectors; scalar accesses reach a third of the rate:
-// 17,472 x 8,192 bf16 with rows 10 bytes off 200 us, with vectors 100).
+// and back; WHOLE: rows of whole vectors, n is never 1..7.  A vector moves in one
+// access at any alignment of the element type (the hardware takes unaligned vectors;
+// with scalar accesses 17,472 x 8,192 bf16 with rows 10 bytes off take 200 us, with
+// vectors 90, aligned 88: 4.9 TB/s).
 template <typename T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void row_load8(const T* p, int n, float (&o)[8]) {
@@ -148,9 +149,12 @@ __device__ __forceinline__ void row_store8(T* p, int n, const float (&v)[8]) {
 
 // Rows of up to NW * 64 * 8 * NV elements in registers: NW waves to a row, lane t
 // holding the 8-element vectors t, t + 64 NW, ...  NW = 1 puts four rows on a workgroup
-// and needs no barrier.
+// and needs no barrier; it pays to 1,024 elements (17,472 x 1,001 with the norm 41.7 us,
+// two waves to a row 43.3).  From there on more, shorter waves leave less of a last round
+// half empty (17,472 x 2,048 56 us, with one wave to a row 60; 10,160 x 1,536 28.1 | 29.4,
+// 3.9 TB/s), and rows of more than 2,048 need the registers of several.
 template <typename T, bool NORM, bool WHOLE, int NW, int NV>
-__global__ void __launch_bounds__(NW < 4 ? 256 : NW * 64)
+__global__ void __launch_bounds__(NW == 1 ? 256 : NW * 64)
 quant_rows(const RowQuant a) {
   constexpr int TPR = NW * 64, RPW = NW == 1 ? 4 : 1;
   __shared__ float red[NW];
@@ -249,8 +253,8 @@ static void run_quant(const RowQuant& a, hipStream_t st) {
                      dim3(NW_ == 1 ? 256 : NW_ * 64), 0, st, a)
   if (vecs <= 64) SWAM_Q(1, 1);
   else if (vecs <= 128) SWAM_Q(1, 2);
-  else if (vecs <= 192) SWAM_Q(1, 3);
-  else if (vecs <= 256) SWAM_Q(1, 4);
+  else if (vecs <= 192) SWAM_Q(3, 1);
+  else if (vecs <= 256) SWAM_Q(4, 1);
   else if (vecs <= 512) SWAM_Q(4, 2);
   else if (vecs <= 1024) SWAM_Q(4, 4);
   else if (vecs <= 2048) SWAM_Q(16, 2);
