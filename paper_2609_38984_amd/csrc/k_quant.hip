@@ -10,6 +10,7 @@
 // sum + 1) bytes).
 #include "launchers.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace swam {
@@ -102,164 +103,220 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v, uint32_t* red) {
   return v;
 }
 
-// 8 elements at p, of which the first n are inside the row (n <= 0: none), as float32,
-// and back; WHOLE: rows of whole vectors, n is never 1..7.  A vector moves in one
-// access at any alignment of the element type (the hardware takes unaligned vectors;
-// with scalar accesses 17,472 x 8,192 bf16 with rows 10 bytes off take 200 us, with
-// vectors 90, aligned 88: 4.9 TB/s).
+// 8 neighbouring elements as they lie in memory, moved in one access at any alignment
+// of the element type (the hardware takes unaligned vectors; with scalar accesses 17,472
+// x 8,192 bf16 with rows 10 bytes off take 200 us, with vectors 83, aligned 75: 5.7 TB/s).
 template <typename T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
-template <bool WHOLE, typename T>
-__device__ __forceinline__ void row_load8(const T* p, int n, float (&o)[8]) {
-  if (n >= 8) {
-    Raw8<T> r;
-    __builtin_memcpy(&r, p, sizeof(r));
-    if constexpr (sizeof(T) == 2) {
+template <typename T>
+__device__ __forceinline__ void raw_to_f32(const Raw8<T>& r, float (&o)[8]) {
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o[2 * e] = __uint_as_float(r.w[e] << 16);
-        o[2 * e + 1] = __uint_as_float(r.w[e] & 0xFFFF0000u);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(r.w[e]);
+    for (int e = 0; e < 4; ++e) {
+      o[2 * e] = __uint_as_float(r.w[e] << 16);
+      o[2 * e + 1] = __uint_as_float(r.w[e] & 0xFFFF0000u);
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = !WHOLE && e < n ? Elem<T>::load(p + e) : 0.0f;
+    for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(r.w[e]);
   }
 }
-template <bool WHOLE, typename T>
-__device__ __forceinline__ void row_store8(T* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    Raw8<T> r;
-    if constexpr (sizeof(T) == 2) {
+template <typename T>
+__device__ __forceinline__ void raw_store(T* p, const float (&v)[8]) {
+  Raw8<T> r;
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) r.w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) r.w[e] = __float_as_uint(v[e]);
-    }
-    __builtin_memcpy(p, &r, sizeof(r));
+    for (int e = 0; e < 4; ++e) r.w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (!WHOLE && e < n) Elem<T>::store(p + e, v[e]);
+    for (int e = 0; e < 8; ++e) r.w[e] = __float_as_uint(v[e]);
   }
+  __builtin_memcpy(p, &r, sizeof(r));
+}
+
+// How a row divides into vectors of 8.  WHOLE: evenly.  TAIL: the last lane with any
+// elements reads the last 8 of the row and owns those that no other lane has; lanes past
+// the end read them too and own none, so no read is behind a branch (with the odd
+// elements read one by one there, 10,038 x 2,402 with the norm took 64 us instead of
+// 54, and the plain quantiser on aligned rows of 8,192 85 instead of 75).  SHORT: fewer
+// than 8 elements, one by one.
+enum { WHOLE, TAIL, SHORT };
+
+// Waves of the norm per CU, all resident at once: what the registers of the form allow in
+// whole workgroups, and no more than 24 (10,160 x 1,536 23.6 us, with 30 25.5, with 16
+// 25.2) except where 16 waves share a row (17,472 x 8,192 192 us with 32, with 16 210).
+constexpr int norm_waves(int esz, int fit, int nw, int nv) {
+  if (nv > 1) return 16;
+  if (nw == 16) return fit == WHOLE && esz == 2 ? 32 : 16;
+  return fit == WHOLE ? 24 : nw == 8 ? 16 : 20;
 }
 
 // Rows of up to NW * 64 * 8 * NV elements in registers: NW waves to a row, lane t
 // holding the 8-element vectors t, t + 64 NW, ...  NW = 1 puts four rows on a workgroup
-// and needs no barrier; it pays to 1,024 elements (17,472 x 1,001 with the norm 41.7 us,
-// two waves to a row 43.3).  From there on more, shorter waves leave less of a last round
-// half empty (17,472 x 2,048 56 us, with one wave to a row 60; 10,160 x 1,536 28.1 | 29.4,
-// 3.9 TB/s), and rows of more than 2,048 need the registers of several.
-template <typename T, bool NORM, bool WHOLE, int NW, int NV>
-__global__ void __launch_bounds__(NW == 1 ? 256 : NW * 64)
+// and needs no barrier.  With the norm a workgroup takes every gridDim-th row: gain and
+// modulation (more bytes than a bf16 row itself) are read once where they fit the
+// registers, and the next row is requested before this one's sums.
+template <typename T, bool NORM, int FIT, int NW, int NV>
+__global__ void __launch_bounds__(NW == 1 ? 256 : NW * 64) __attribute__((amdgpu_waves_per_eu(
+    NORM ? norm_waves(sizeof(T), FIT, NW, NV) / 4 : 1, 8)))
 quant_rows(const RowQuant a) {
   constexpr int TPR = NW * 64, RPW = NW == 1 ? 4 : 1;
+  constexpr bool KEEP = NORM && NV == 1, MORE = NORM && NV <= 2;
   __shared__ float red[NW];
   __shared__ uint32_t redu[NW];
-  const int64_t row = (int64_t)blockIdx.x * RPW + (NW == 1 ? threadIdx.x / TPR : 0);
+  int64_t row = (int64_t)blockIdx.x * RPW + (NW == 1 ? threadIdx.x / TPR : 0);
   if (row >= a.rows) return;                    // whole waves
   const int t = threadIdx.x % TPR, d = a.d;
-  const T* xp = (const T*)a.x + row * a.x_ld;
-  float v[NV][8];
+  auto first = [&](int i) { return (i * TPR + t) * 8; };                 // first own element
+  auto from = [&](int i) { return FIT == SHORT ? first(i) : min(first(i), d - 8); };
+  // whether element j of vector i is this lane's (a vector starts at from())
+  auto own = [&](int i, int j) {
+    return FIT == WHOLE ? first(i) < d : FIT == TAIL ? from(i) + j >= first(i) : first(i) + j < d;
+  };
+  auto read = [&](const auto* p, int i, auto& o) {
+    if constexpr (FIT != SHORT) {
+      __builtin_memcpy(&o, p + from(i), sizeof(o));
+    } else {
+      o = {};
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = (i * TPR + t) * 8;
-    row_load8<WHOLE>(xp + e, d - e, v[i]);
-  }
-  if constexpr (NORM) {
-    float ss = 0.0f;
-    if (a.res != nullptr) {
-      const T* rp = (const T*)a.res + row * a.res_ld;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int e = (i * TPR + t) * 8;
-        float r[8];
-        row_load8<WHOLE>(rp + e, d - e, r);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] += r[j];
+      for (int j = 0; j < 8; ++j) {
+        if (!own(i, j)) continue;
+        if constexpr (sizeof(*p) == 2) o.w[j / 2] |= (uint32_t)p[first(i) + j] << (16 * (j & 1));
+        else o.w[j] = __float_as_uint(p[first(i) + j]);
       }
     }
-    if (a.sum != nullptr) {
-      T* sp = (T*)a.sum + row * a.sum_ld;
+  };
+  // y = (t / rms) fac + add
+  auto factors = [&](int i, float (&fac)[8], float (&add)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { fac[j] = 1.0f; add[j] = 0.0f; }
+    if (a.gain != nullptr) {
+      Raw8<T> g;
+      read((const T*)a.gain, i, g);
+      raw_to_f32(g, fac);
+    }
+    if (a.shift != nullptr) {
+      Raw8<float> sc, sh;
+      read(a.scale, i, sc);
+      read(a.shift, i, sh);
+      raw_to_f32(sh, add);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fac[j] *= 1.0f + __uint_as_float(sc.w[j]);
+    }
+  };
+  Raw8<T> x[NV], r[NV];
+  auto fetch = [&](int64_t at) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) read((const T*)a.x + at * a.x_ld, i, x[i]);
+    if (NORM && a.res != nullptr) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) read((const T*)a.res + at * a.res_ld, i, r[i]);
+    }
+  };
+  fetch(row);
+  float kfac[8], kadd[8];
+  if constexpr (KEEP) factors(0, kfac, kadd);
+  for (;;) {
+    float v[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      raw_to_f32(x[i], v[i]);
+      if (NORM && a.res != nullptr) {
+        float o[8];
+        raw_to_f32(r[i], o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] += o[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!own(i, j)) v[i][j] = 0.0f;
+    }
+    const int64_t next = row + (int64_t)gridDim.x * RPW;
+    const bool more = MORE && next < a.rows;
+    if constexpr (NORM) {
+      if (more) fetch(next);
+      if (a.sum != nullptr) {
+        T* sp = (T*)a.sum + row * a.sum_ld;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          if (first(i) + 8 <= d) {
+            raw_store(sp + first(i), v[i]);
+          } else if (FIT != WHOLE) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (first(i) < d && own(i, j)) Elem<T>::store(sp + from(i) + j, v[i][j]);
+          }
+        }
+      }
+      float ss = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+      const float inv = inv_rms(row_sum<NW>(ss, red), d, a.eps);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int e = (i * TPR + t) * 8;
-        row_store8<WHOLE>(sp + e, d - e, v[i]);
+        float fac[8], add[8];
+        if constexpr (!KEEP) factors(i, fac, add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[i][j] = KEEP ? fmaf(v[i][j] * inv, kfac[j], kadd[j]) : fmaf(v[i][j] * inv, fac[j], add[j]);
+          if (!own(i, j)) v[i][j] = 0.0f;
+        }
       }
     }
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
-    ss = row_sum<NW>(ss, red);
-    const float r = inv_rms(ss, d, a.eps);
+      for (int j = 0; j < 8; ++j) top = max(top, mag_bits(v[i][j]));
+    const RowScale rs = row_scale(row_umax<NW>(top, redu));
+    int8_t* qp = a.q + row * a.q_ld;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int e = (i * TPR + t) * 8;
-      if (e < d) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] *= r;
-        if (a.gain != nullptr) {
-          float g[8];
-          row_load8<WHOLE>((const T*)a.gain + e, d - e, g);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
-        }
-        if (a.shift != nullptr) {
-          float sc[8], sh[8];
-          row_load8<WHOLE>(a.scale + e, d - e, sc);
-          row_load8<WHOLE>(a.shift + e, d - e, sh);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j], 1.0f + sc[j], sh[j]);
-        }
-      }
-    }
-  }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, mag_bits(v[i][j]));
-  const RowScale rs = row_scale(row_umax<NW>(top, redu));
-  int8_t* qp = a.q + row * a.q_ld;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = (i * TPR + t) * 8;
-    if (e < d) {
+      if (first(i) >= d) continue;
       int c[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) c[j] = code_of<!NORM>(v[i][j], rs);
-      if (WHOLE || d - e >= 8) {
+      if (FIT == WHOLE || first(i) + 8 <= d) {
         const uint32_t w[2] = {pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7])};
-        __builtin_memcpy(qp + e, w, 8);
+        __builtin_memcpy(qp + first(i), w, 8);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (e + j < d) qp[e + j] = (int8_t)c[j];
+          if (own(i, j)) qp[from(i) + j] = (int8_t)c[j];
       }
     }
+    if (t == 0) a.q_scale[row] = rs.s;
+    if (!more) return;
+    row = next;
   }
-  if (t == 0) a.q_scale[row] = rs.s;
 }
 
-template <typename T, bool NORM, bool WHOLE>
+template <typename T, bool NORM, int FIT, int NW, int NV>
+static void run_rows(const RowQuant& a, hipStream_t st) {
+  constexpr int RPW = NW == 1 ? 4 : 1, WAVES = NW == 1 ? 4 : NW;
+  const int64_t sets = (a.rows + RPW - 1) / RPW;
+  const unsigned n = (unsigned)(NORM && NV <= 2 ? std::min<int64_t>(sets, 256 * (norm_waves(sizeof(T), FIT, NW, NV) / WAVES)) : sets);
+  hipLaunchKernelGGL((quant_rows<T, NORM, FIT, NW, NV>), dim3(n), dim3(WAVES * 64), 0, st, a);
+}
+
+// One wave to a row up to 512 elements.  Beyond, the norm adds waves, so that a lane's one
+// vector of factors stays in registers (17,472 x 8,192 bf16 over 16 waves 192 us; over 4
+// with the factors read anew for every row 227); the plain quantiser has none and adds
+// vectors first (17,472 x 1,001 float32 15.6 us with one wave, 17.1 with two).
+template <typename T, bool NORM, int FIT>
 static void run_quant(const RowQuant& a, hipStream_t st) {
   const int vecs = (a.d + 7) / 8;
-#define SWAM_Q(NW_, NV_)                                                                                   \
-  hipLaunchKernelGGL((quant_rows<T, NORM, WHOLE, NW_, NV_>), dim3((unsigned)(NW_ == 1 ? (a.rows + 3) / 4 : a.rows)), \
-                     dim3(NW_ == 1 ? 256 : NW_ * 64), 0, st, a)
-  if (vecs <= 64) SWAM_Q(1, 1);
-  else if (vecs <= 128) SWAM_Q(1, 2);
-  else if (vecs <= 192) SWAM_Q(3, 1);
-  else if (vecs <= 256) SWAM_Q(4, 1);
-  else if (vecs <= 512) SWAM_Q(4, 2);
-  else if (vecs <= 1024) SWAM_Q(4, 4);
-  else if (vecs <= 2048) SWAM_Q(16, 2);
-  else SWAM_Q(16, 4);
-#undef SWAM_Q
+  if (vecs <= 64) return run_rows<T, NORM, FIT, 1, 1>(a, st);
+  if constexpr (FIT != SHORT) {
+    if (vecs <= 128) return run_rows<T, NORM, FIT, NORM ? 2 : 1, NORM ? 1 : 2>(a, st);
+    if (vecs <= 192) return run_rows<T, NORM, FIT, 3, 1>(a, st);
+    if (vecs <= 256) return run_rows<T, NORM, FIT, 4, 1>(a, st);
+    if (vecs <= 512) return run_rows<T, NORM, FIT, NORM ? 8 : 4, NORM ? 1 : 2>(a, st);
+    if (vecs <= 1024) return run_rows<T, NORM, FIT, NORM ? 16 : 4, NORM ? 1 : 4>(a, st);
+    if (vecs <= 2048) return run_rows<T, NORM, FIT, 16, 2>(a, st);
+    return run_rows<T, NORM, FIT, 16, 4>(a, st);
+  }
 }
 
 hipError_t launch_quant_rows(int dtype, bool norm, const RowQuant& a, hipStream_t st) {
@@ -267,8 +324,9 @@ hipError_t launch_quant_rows(int dtype, bool norm, const RowQuant& a, hipStream_
   auto run = [&](auto type, auto with_norm) {
     using T = decltype(type);
     constexpr bool N = decltype(with_norm)::value;
-    if (a.d % 8 == 0) run_quant<T, N, true>(a, st);
-    else run_quant<T, N, false>(a, st);
+    if (a.d % 8 == 0) run_quant<T, N, WHOLE>(a, st);
+    else if (a.d > 8) run_quant<T, N, TAIL>(a, st);
+    else run_quant<T, N, SHORT>(a, st);
   };
   if (dtype == 1) {
     if (norm) run(bf16_t{}, std::true_type{});
