@@ -189,6 +189,25 @@ def test_rms_norm_in_place_and_special_rows(contexts, dtype, d, pad):
     assert float(s[1]) == 0.0 and bool((q[1] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,d", [(27001, 101), (27000, 5), (8001, 1000), (7000, 1001), (5003, 1536), (4001, 2047),
+                                    (2600, 4000), (1700, 2410), (1201, 8192), (1100, 5003), (600, 16384)])
+def test_rms_norm_of_more_rows_than_run_at_once(contexts, dtype, rows, d):
+    """Workgroups that take several rows in turn, in place; a row that is not finite leaves
+    those after it alone."""
+    dt, g = TYPES[dtype], gen(rows + d)
+    x0, r = rows_of((rows, d), dt, g)[0], rows_of((rows, d), dt, g, 3)[0]
+    x0[::7, d // 2] = float("nan")
+    w = (1 + 0.3 * torch.randn(d, device="cuda", generator=g)).to(dt)
+    sh, sc = (torch.randn((2, d), device="cuda", generator=g) * 0.4).unbind()
+    x, q, s = x0.clone(), torch.full((rows, d), 77, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    contexts[dtype].rms_norm_i8(x, q, s, residual=r, sum_out=x, gain=w, shift=sh, scale=sc)
+    bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    bad[::7] = True
+    check_norm(*norm_reference(x0[~bad], r[~bad], w, sh, sc, 1e-6), q[~bad], s[~bad], x[~bad], dt)
+    assert bool(torch.isnan(s[bad]).all()) and bool((q[bad] == 0).all())
+
+
 # ---------------------------------------------------------------------------
 # 8-bit product
 # ---------------------------------------------------------------------------
