@@ -7,7 +7,8 @@
 // Two numbers of the whole row (the mean square and the largest magnitude) stand
 // between reading x and writing the codes.  The row stays on chip in float32
 // between them, so every byte moves once: memory bounds it (rows * d * (x + r +
-// sum + 1) bytes).
+// sum + 1) bytes): bf16 with residual, sum, gain and modulation 10,160 x 1,536 23.6 us
+// (4.6 TB/s), 17,472 x 8,192 192 us (5.2); plain 76 us (5.6).  A large copy reaches 5.1.
 #include "launchers.h"
 
 #include <algorithm>
