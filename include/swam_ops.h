@@ -23,7 +23,8 @@
  * graphs that captured them) must not overlap in time, as everywhere in swam.h.
  * Float tensors called "act" below have the context's dtype; strides are in
  * elements; rows of a tensor may lie further apart than they are wide (a column
- * range of a wider buffer).  An output may not overlap an input unless stated.
+ * range of a wider buffer); rows times row stride is below 2^48.  An output may not
+ * overlap an input unless stated.
  * The calls run on the context's device whatever device is current.
  */
 #ifndef SWAM_OPS_H
@@ -81,9 +82,9 @@ int swam_quantize_i8(swam_ctx* ctx, const void* x, int64_t x_stride, int64_t row
  *   residual);  c : act [m][n] (row stride ldc), may be residual itself (same
  *   pointer and stride)
  * k a positive multiple of 16 up to SWAM_I8_MAX_K; m, n below 2^30 and m * n below
- * 2^40 (0: nothing to do); lda, ldb below 2^22.  a, b and their row strides are 16-byte aligned (SWAM_E_INVALID otherwise);
- * the float tensors need the alignment of their type only (16-byte aligned rows are
- * moved in vectors). */
+ * 2^40 (0: nothing to do); lda, ldb below 2^22.  a, b and their row strides are
+ * 16-byte aligned (SWAM_E_INVALID otherwise); the float tensors need the alignment of
+ * their type only (16-byte aligned rows are moved in vectors). */
 int swam_gemm_i8(swam_ctx* ctx, const int8_t* a, int64_t lda, const float* a_scale,
                  const int8_t* b, int64_t ldb, const float* b_scale, const void* bias,
                  const void* residual, int64_t ldr, const float* gate, int32_t flags, void* c,

@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(NW == 1 ? 256 : NW * 64) __attribute__((amdgpu
     NORM ? norm_waves(sizeof(T), FIT, NW, NV) / 4 : 1, 8)))
 quant_rows(const RowQuant a) {
   constexpr int TPR = NW * 64, RPW = NW == 1 ? 4 : 1;
-  constexpr bool KEEP = NORM && NV == 1, MORE = NORM && NV <= 2;
+  constexpr bool KEEP = NORM && NV == 1, TURNS = NORM && NV <= 2;
   __shared__ float red[NW];
   __shared__ uint32_t redu[NW];
   int64_t row = (int64_t)blockIdx.x * RPW + (NW == 1 ? threadIdx.x / TPR : 0);
@@ -232,7 +232,7 @@ quant_rows(const RowQuant a) {
         if (!own(i, j)) v[i][j] = 0.0f;
     }
     const int64_t next = row + (int64_t)gridDim.x * RPW;
-    const bool more = MORE && next < a.rows;
+    const bool more = TURNS && next < a.rows;
     if constexpr (NORM) {
       if (more) fetch(next);
       if (a.sum != nullptr) {
@@ -294,11 +294,23 @@ quant_rows(const RowQuant a) {
 }
 
 template <typename T, bool NORM, int FIT, int NW, int NV>
-static void run_rows(const RowQuant& a, hipStream_t st) {
+static void run_rows(RowQuant a, hipStream_t st) {
   constexpr int RPW = NW == 1 ? 4 : 1, WAVES = NW == 1 ? 4 : NW;
-  const int64_t sets = (a.rows + RPW - 1) / RPW;
-  const unsigned n = (unsigned)(NORM && NV <= 2 ? std::min<int64_t>(sets, 256 * (norm_waves(sizeof(T), FIT, NW, NV) / WAVES)) : sets);
-  hipLaunchKernelGGL((quant_rows<T, NORM, FIT, NW, NV>), dim3(n), dim3(WAVES * 64), 0, st, a);
+  constexpr bool TURNS = NORM && NV <= 2;
+  // a grid holds less than 2^32 threads: more rows than that take another launch
+  constexpr int64_t MOST = TURNS ? (int64_t)1 << 31 : (int64_t)RPW << 20;
+  for (int64_t left = a.rows;; left -= MOST) {
+    a.rows = std::min(left, MOST);
+    const int64_t sets = (a.rows + RPW - 1) / RPW;
+    const unsigned n = (unsigned)(TURNS ? std::min<int64_t>(sets, 256 * (norm_waves(sizeof(T), FIT, NW, NV) / WAVES)) : sets);
+    hipLaunchKernelGGL((quant_rows<T, NORM, FIT, NW, NV>), dim3(n), dim3(WAVES * 64), 0, st, a);
+    if (left <= MOST) return;
+    a.x = (const T*)a.x + MOST * a.x_ld;
+    if (a.res != nullptr) a.res = (const T*)a.res + MOST * a.res_ld;
+    if (a.sum != nullptr) a.sum = (T*)a.sum + MOST * a.sum_ld;
+    a.q += MOST * a.q_ld;
+    a.q_scale += MOST;
+  }
 }
 
 // One wave to a row up to 512 elements.  Beyond, the norm adds waves, so that a lane's one

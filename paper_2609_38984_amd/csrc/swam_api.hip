@@ -306,6 +306,9 @@ int64_t ops_esz(const swam_ctx* c) { return c ? c->dv.esz : 2; }
 
 bool typed(const void* p, int64_t esz) { return ((uintptr_t)p & (uintptr_t)(esz - 1)) == 0; }
 
+// rows that no memory holds: their last offset could pass 64 bits
+bool far_apart(int64_t rows, int64_t ld) { return rows > 1 && ld > (1ll << 48) / rows; }
+
 // the bytes of `rows` rows of `width` elements, `ld` elements apart
 struct Span { uintptr_t lo, hi, pitch, width; };
 Span span(const void* p, int64_t ld, int64_t rows, int64_t width, int64_t esz) {
@@ -328,6 +331,8 @@ int check_rows(swam_ctx* c, const void* x, int64_t x_stride, int64_t rows, int64
   if (d < 1 || d > SWAM_I8_MAX_WIDTH) return set_err(c, SWAM_E_SHAPE, "d must be in [1, SWAM_I8_MAX_WIDTH]");
   if (rows > 0 && (!x || !q || !q_scale)) return set_err(c, SWAM_E_INVALID, "x, q, q_scale required");
   if (x_stride < d || q_stride < d) return set_err(c, SWAM_E_INVALID, "a row stride is smaller than its row");
+  if (far_apart(rows, x_stride) || far_apart(rows, q_stride))
+    return set_err(c, SWAM_E_SHAPE, "rows times row stride below 2^48");
   if (!typed(q_scale, 4)) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
   return SWAM_OK;
 }
@@ -1447,6 +1452,8 @@ int swam_rms_norm_i8(swam_ctx* c, const void* x, int64_t x_stride, const void* r
   if (int rc = check_rows(c, x, x_stride, rows, d, q, q_stride, q_scale)) return rc;
   if (residual && residual_stride < d) return set_err(c, SWAM_E_INVALID, "residual row stride < d");
   if (sum_out && sum_stride < d) return set_err(c, SWAM_E_INVALID, "sum_out row stride < d");
+  if ((residual && far_apart(rows, residual_stride)) || (sum_out && far_apart(rows, sum_stride)))
+    return set_err(c, SWAM_E_SHAPE, "rows times row stride below 2^48");
   if (!shift != !scale) return set_err(c, SWAM_E_INVALID, "shift and scale come together");
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return set_err(c, SWAM_E_INVALID, "eps must be finite and >= 0");
   const int64_t es = ops_esz(c);
@@ -1522,6 +1529,8 @@ int swam_gemm_i8(swam_ctx* c, const int8_t* a, int64_t lda, const float* a_scale
       !typed(residual, es) || !typed(out, es))
     return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
   if (m * n >= (1ll << 40)) return set_err(c, SWAM_E_SHAPE, "m * n below 2^40");
+  if (far_apart(m, ldc) || (residual && far_apart(m, ldr)))
+    return set_err(c, SWAM_E_SHAPE, "m times a row stride below 2^48");
   const Span os = span(out, ldc, m, n, es);
   for (const Span& in : {span(a, lda, m, k, 1), span(b, ldb, n, k, 1), span(a_scale, 1, m, 1, 4),
                          span(b_scale, 1, n, 1, 4), span(bias, n, 1, n, es), span(gate, n, 1, n, 4)})

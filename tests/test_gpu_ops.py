@@ -108,6 +108,21 @@ def test_quantise_borders_zero_tiny_huge_and_non_finite_rows(contexts, dtype, d)
     assert float(s[0]) == 0.0
 
 
+@pytest.mark.parametrize("rows,d", [((1 << 22) + 1001, 5), ((1 << 22) + 1002, 24), ((1 << 26) + 3, 8),
+                                    ((1 << 20) + 501, 2050)])
+def test_quantise_more_rows_than_a_grid_holds(contexts, rows, d):
+    g = gen(rows + d)
+    x = torch.randn((rows, d), device="cuda", generator=g, dtype=torch.bfloat16)
+    q, s = torch.full((rows, d), 77, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    contexts["bf16"].quantize_i8(x, q, s)
+    for part in (slice(0, 700), slice(rows // 2, rows // 2 + 700), slice((1 << 20) - 300, (1 << 20) + 300),
+                 slice(rows - 1500, rows)):
+        c, top = exact_codes(x[part].double())
+        assert torch.equal(q[part].double(), c)
+        assert torch.equal(s[part], (top / 127.0).float())
+    assert int(q.amax()) == 127 and bool((s > 0).all())
+
+
 def norm_reference(x, r, gain, shift, scale, eps):
     t = x.double() if r is None else x.double() + r.double()
     y = t / torch.sqrt(t.square().mean(1, keepdim=True) + eps)

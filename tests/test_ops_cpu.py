@@ -160,3 +160,15 @@ def test_cross_attention_takes_empty_and_interleaved_tensors(lib):
                    dict(n_seqs=64, n_kv=64, kv=None), dict(n_seqs=1, n_kv=1, cu_q=None, cu_k=None, kv=None),
                    dict(mask=None, lse=None)):
         assert _call(lib, "swam_cross_attention", ATTN, change) == (INVALID, "ctx is NULL"), change
+
+
+@pytest.mark.parametrize("fn,base,name,rows", [
+    ("swam_quantize_i8", QUANT, "xs", 8), ("swam_quantize_i8", QUANT, "qs", 8), ("swam_rms_norm_i8", NORM, "rs", 8),
+    ("swam_rms_norm_i8", NORM, "ss", 8), ("swam_gemm_i8", GEMM, "ldc", 8), ("swam_gemm_i8", GEMM, "ldr", 8)])
+def test_rows_that_no_memory_holds_are_refused(lib, fn, base, name, rows):
+    for far in ((1 << 48) // rows + 1, 1 << 62):
+        rc, msg = _call(lib, fn, base, {name: far})
+        assert rc == SHAPE and "2^48" in msg, msg
+    # one row has no second to reach
+    one = {"rows": 1} if "rows" in base else {"m": 1}
+    assert _call(lib, fn, base, {name: 1 << 62, **one}) == (INVALID, "ctx is NULL")
