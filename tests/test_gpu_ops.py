@@ -775,6 +775,33 @@ def test_replayed_and_on_other_streams(contexts, dtype):
         assert torch.equal(got[n], want[n]), n
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_two_contexts_at_once(contexts, dtype):
+    """Two contexts on two streams, their calls in flight together (split attention has a
+    workspace in each), give what each gives alone."""
+    from paper_2609_38984_amd import swam
+    dt = TYPES[dtype]
+    shapes = [([1, 1, 40], [2000, 77, 300]), ([30, 1], [1500, 4000])]
+    states = [sublayer_state(contexts[dtype], dt, 91 + i, *sh) for i, sh in enumerate(shapes)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ctxs = [swam.Context(W.preset(2).replace(dtype=dtype, n_blocks=1), st) for st in streams]
+    wants, gots = [], [[sublayer_out(s) for _ in range(6)] for s in states]
+    for s in states:
+        wants.append(sublayer_out(s))
+        sublayer(contexts[dtype], s, wants[-1])
+    torch.cuda.synchronize()
+    for i in range(6):
+        for ctx, st, s, got in zip(ctxs, streams, states, gots):
+            with torch.cuda.stream(st):
+                sublayer(ctx, s, got[i])
+    torch.cuda.synchronize()
+    for want, got in zip(wants, gots):
+        for g in got:
+            for n in want:
+                assert torch.equal(g[n], want[n]), n
+
+
 def test_steps_and_operators_share_a_context(contexts):
     """A step of the model between two operator calls leaves both as they were
     (they use one workspace in turn), and the timers see the operators."""
