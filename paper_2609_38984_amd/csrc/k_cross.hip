@@ -473,11 +473,13 @@ cross_f32(const CrossArgs c, const Partial part) {
   }
 }
 
-// One wave per token and head adds up the slices in their order.  Rows outside
-// every sequence have none and are left as they are.
+// One wave per token and head adds up the slices, in a fixed order.  Lane s weighs slice
+// s; D / 4 lanes hold a slice's row, so a wave reads several at once and eight such
+// loads are in flight (32 slices of 32 rows 4 us; one slice after the other 12).  Rows outside every sequence have none and are left as they are.
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
 cross_join(const CrossArgs c, const Partial part) {
+  constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8;
   const int64_t n = (int64_t)c.n_q * c.heads;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= n) return;
@@ -485,22 +487,45 @@ cross_join(const CrossArgs c, const Partial part) {
   const int tok = (int)(row / c.heads), head = (int)(row % c.heads);
   bool in = c.cu_q == nullptr;
   if (c.cu_q != nullptr && lane < c.n_seqs) in = tok >= c.cu_q[lane] && tok < c.cu_q[lane + 1];
+  float m = -FLT_MAX, l = 0.0f;
+  if (lane < part.splits) {
+    const float2 ml = *reinterpret_cast<const float2*>(part.ml + (lane * n + row) * 2);
+    m = ml.x;
+    l = ml.y;
+  }
   if (!__any(in)) return;
-  float mt = -FLT_MAX;
-  for (int s = lane; s < part.splits; s += 64) mt = fmaxf(mt, part.ml[(s * n + row) * 2]);
-  mt = warp_max(mt);
-  float l = 0.0f, acc[D / 64] = {};
-  for (int s = 0; s < part.splits; ++s) {
-    const float* pm = part.ml + (s * n + row) * 2;
-    const float f = exp2f(pm[0] - mt);
-    l = fmaf(pm[1], f, l);
+  const float mt = warp_max(m);
+  const float f = lane < part.splits ? exp2f(m - mt) : 0.0f;
+  l = warp_sum(l * f);
+  const int set = lane / PER, col = lane % PER * 4;
+  float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = 0; s0 < part.splits; s0 += SETS * AHEAD) {
+    float4 v[AHEAD];
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(part.o[(s * n + row) * D + 64 * e + lane], f, acc[e]);
+    for (int a = 0; a < AHEAD; ++a) {
+      const int s = min(s0 + SETS * a + set, part.splits - 1);
+      v[a] = *reinterpret_cast<const float4*>(part.o + (s * n + row) * D + col);
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int s = s0 + SETS * a + set;
+      if (s0 + SETS * a >= part.splits) break;
+      const float w = __shfl(f, min(s, 63));
+      if (s < part.splits) {
+        acc[0] = fmaf(v[a].x, w, acc[0]);
+        acc[1] = fmaf(v[a].y, w, acc[1]);
+        acc[2] = fmaf(v[a].z, w, acc[2]);
+        acc[3] = fmaf(v[a].w, w, acc[3]);
+      }
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e)
-    Elem<T>::store((T*)c.o + tok * c.o_ld + head * D + 64 * e + lane, acc[e] * inv);
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int o = PER; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
+    if (set == 0) Elem<T>::store((T*)c.o + tok * c.o_ld + head * D + col + e, acc[e] * inv);
+  }
   if (c.lse != nullptr && lane == 0) c.lse[row] = l == 0.0f ? -INFINITY : (mt + log2f(l)) * LN2;
 }
 
@@ -514,9 +539,9 @@ static int64_t cross_slots(const CrossArgs& c, int64_t bq) {
 // by modelled time (us): tiles per slice, each `lone` for a workgroup by itself and
 // `share` per workgroup where several share a CU, plus the pass that joins the
 // slices and what they write and read.  us without | with the chosen split: 8 x 1 query
-// of 24 heads on 10,160 keys 240 | 118 (4 slices), 32 x 24 on 2,048 39 | 14 (8), 300 x 16 on
-// 4,096 70 | 25 (8), 326 x 24 on 2,048 38 | 24 (4); 512 x 24 on 512 11 | 17 (2, not chosen),
-// 4,096 x 12 on 512 (head_dim 128) 24 | 52 (2, not chosen).
+// of 24 heads on 10,160 keys 240 | 118 (4 slices), 1 x 32 of 128 on 10,160 229 | 18.7 (64),
+// 32 x 24 on 2,048 39 | 12.7 (16), 300 x 16 on 4,096 70 | 25 (8), 326 x 24 on 2,048 38 | 24
+// (4); 512 x 24 on 512 11 | 19 (2, not chosen), 4,096 x 12 of 128 on 512 25 | 58 (2, not chosen).
 static int cross_splits(int64_t wgs, int64_t tiles, int64_t rows, int D, int64_t ws_floats) {
   const double lone = D == 64 ? 1.2 : 1.6, share = D == 64 ? 0.64 : 1.0;
   int best = 1;
@@ -524,7 +549,7 @@ static int cross_splits(int64_t wgs, int64_t tiles, int64_t rows, int D, int64_t
   for (int s = 1; s <= 64 && (s == 1 || s * 2 <= tiles); s *= 2) {
     if (s > 1 && (int64_t)s * rows * (D + 2) > ws_floats) break;
     double us = (double)((tiles + s - 1) / s) * std::max(lone, share * (double)(wgs * s) / 256.0);
-    if (s > 1) us += 4.0 + 0.3 * s + 2.0 * s * (double)rows * (D + 2) * 4.0 / 3.0e6;
+    if (s > 1) us += 4.5 + 0.05 * s + 2.0 * s * (double)rows * (D + 2) * 4.0 / 3.0e6;
     if (us < best_us) { best_us = us; best = s; }
   }
   return best;
