@@ -137,9 +137,9 @@ __device__ __forceinline__ void raw_store(T* p, const float (&v)[8]) {
 // How a row divides into vectors of 8.  WHOLE: evenly.  TAIL: the last lane with any
 // elements reads the last 8 of the row and owns those that no other lane has; lanes past
 // the end read them too and own none, so no read is behind a branch (with the odd
-// elements read one by one there, 10,038 x 2,402 with the norm took 64 us instead of
-// 54, and the plain quantiser on aligned rows of 8,192 85 instead of 75).  SHORT: fewer
-// than 8 elements, one by one.
+// elements read one by one there, 10,038 x 2,402 with the norm over eight waves took 64 us
+// instead of 54, and the plain quantiser on aligned rows of 8,192 85 instead of 75).
+// SHORT: fewer than 8 elements, one by one.
 enum { WHOLE, TAIL, SHORT };
 
 // Waves of the norm per CU, all resident at once: what the registers of the form allow in
@@ -315,7 +315,9 @@ static void run_rows(RowQuant a, hipStream_t st) {
 
 // One wave to a row up to 512 elements.  Beyond, the norm adds waves, so that a lane's one
 // vector of factors stays in registers (17,472 x 8,192 bf16 over 16 waves 192 us; over 4
-// with the factors read anew for every row 227); the plain quantiser has none and adds
+// with the factors read anew for every row 227), five of them to 2,560 elements
+// (10,038 x 2,402 38.7 us, over eight 54, 10,160 x 2,560 38 | 41.5; six or seven gain less,
+// and lose with float32's odd widths).  The plain quantiser has no factors and adds
 // vectors first (17,472 x 1,001 float32 15.6 us with one wave, 17.1 with two).
 template <typename T, bool NORM, int FIT>
 static void run_quant(const RowQuant& a, hipStream_t st) {
@@ -325,6 +327,9 @@ static void run_quant(const RowQuant& a, hipStream_t st) {
     if (vecs <= 128) return run_rows<T, NORM, FIT, NORM ? 2 : 1, NORM ? 1 : 2>(a, st);
     if (vecs <= 192) return run_rows<T, NORM, FIT, 3, 1>(a, st);
     if (vecs <= 256) return run_rows<T, NORM, FIT, 4, 1>(a, st);
+    if constexpr (NORM) {
+      if (vecs <= 320) return run_rows<T, NORM, FIT, 5, 1>(a, st);
+    }
     if (vecs <= 512) return run_rows<T, NORM, FIT, NORM ? 8 : 4, NORM ? 1 : 2>(a, st);
     if (vecs <= 1024) return run_rows<T, NORM, FIT, NORM ? 16 : 4, NORM ? 1 : 4>(a, st);
     if (vecs <= 2048) return run_rows<T, NORM, FIT, 16, 2>(a, st);

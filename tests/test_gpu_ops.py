@@ -206,7 +206,8 @@ def test_rms_norm_in_place_and_special_rows(contexts, dtype, d, pad):
 
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("rows,d", [(27001, 101), (27000, 5), (8001, 1000), (7000, 1001), (5003, 1536), (4001, 2047),
-                                    (2600, 4000), (1700, 2410), (1201, 8192), (1100, 5003), (600, 16384)])
+                                    (2600, 4000), (1700, 2410), (2301, 2560), (1900, 3501), (1201, 8192), (1100, 5003),
+                                    (600, 16384)])
 def test_rms_norm_of_more_rows_than_run_at_once(contexts, dtype, rows, d):
     """Workgroups that take several rows in turn, in place; a row that is not finite leaves
     those after it alone."""
