@@ -43,8 +43,9 @@ extern "C" {
  *   t = x + residual                       (t = x when residual is NULL)
  *   y = t / sqrt(mean(t^2) + eps) * gain * (1 + scale) + shift
  *   q_scale = max|y| / 127,   q = round(y / q_scale) in [-127, 127]
- * in float32 from the unrounded t; rounding is to nearest even.  A row of zeros
- * gets the scale 0 and zeros.  A row with a NaN or an infinity, or whose sum of
+ * in float32 from the unrounded t; rounding is to nearest even.  Rows however small
+ * keep their y, also where eps does not hide them (their squares are summed of a row
+ * lifted by a power of two).  A row of zeros gets the scale 0 and zeros.  A row with a NaN or an infinity, or whose sum of
  * squares exceeds float32, gets the scale NaN and zeros, so what is made of it
  * is NaN.
  *   x        : act [rows][d], row stride x_stride >= d

@@ -67,12 +67,17 @@ __device__ __forceinline__ int code_of(float y, const RowScale& r) {
   return (int)c;
 }
 
-// 1 / sqrt(mean square + eps); NaN for a sum that is NaN or overflowed, so that every
-// y and with it the scale is NaN; 0 for a row of zeros without eps
-__device__ __forceinline__ float inv_rms(float ss, int d, float eps) {
-  const float ms = ss / (float)d + eps;
+// 1 / sqrt(ms), ms = mean square + eps; NaN for a sum of squares ss that is NaN or
+// overflowed, so that every y and with it the scale is NaN; 0 for a row of zeros without eps
+__device__ __forceinline__ float inv_rms(float ss, float ms) {
   return !(ss < INFINITY) ? __uint_as_float(0x7fc00000u) : ms > 0.0f ? 1.0f / sqrtf(ms) : 0.0f;
 }
+
+// Below this ms a row is lifted by 2^100 (and eps by its square) before its squares are
+// summed again, which leaves y as it is: a square loses at most 2^-150 to float32's end of
+// range, 2^-30 of a mean that is not below.  Lifted, elements are below 2^48 and the smallest
+// one that a row can hold is 2^-49, its square far inside the range.
+constexpr float TINY_MS = 0x1p-120f, LIFT = 0x1p100f;
 
 __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
   return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)d << 24);
@@ -88,6 +93,21 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
     v = red[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) v += red[w];
+  }
+  return v;
+}
+// A second sum of the row, once every wave has read the parts of the first; one part after
+// the other, for it is rare and the registers of the common path are counted.
+template <int NW>
+__device__ __forceinline__ float row_sum_again(float v, float* red) {
+  v = warp_sum(v);
+  if constexpr (NW > 1) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll 1
+    for (int w = 0; w < NW; ++w) v += red[w];
   }
   return v;
 }
@@ -173,9 +193,16 @@ quant_rows(const RowQuant a) {
   auto own = [&](int i, int j) {
     return FIT == WHOLE ? first(i) < d : FIT == TAIL ? from(i) + j >= first(i) : first(i) + j < d;
   };
+  // An element's place beside the row's scalar pointer.  With 16 waves it is added anew each
+  // time: a 64-bit pointer per lane and tensor is more than their 64 registers hold (17,472 x
+  // 8,192 203 us with 4 of them spilled); with fewer waves the additions cost 1-5%.
+  auto offset = [&](int at) {
+    if constexpr (NW == 16) asm volatile("" : "+v"(at));
+    return (uint32_t)at;
+  };
   auto read = [&](const auto* p, int i, auto& o) {
     if constexpr (FIT != SHORT) {
-      __builtin_memcpy(&o, p + from(i), sizeof(o));
+      __builtin_memcpy(&o, p + offset(from(i)), sizeof(o));
     } else {
       o = {};
 #pragma unroll
@@ -240,7 +267,7 @@ quant_rows(const RowQuant a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           if (first(i) + 8 <= d) {
-            raw_store(sp + first(i), v[i]);
+            raw_store(sp + offset(first(i)), v[i]);
           } else if (FIT != WHOLE) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -248,12 +275,26 @@ quant_rows(const RowQuant a) {
           }
         }
       }
-      float ss = 0.0f;
+      auto squares = [&] {
+        float ss = 0.0f;
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
-      const float inv = inv_rms(row_sum<NW>(ss, red), d, a.eps);
+          for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+        return ss;
+      };
+      float ss = row_sum<NW>(squares(), red), ms = ss / (float)d + a.eps;
+      if (__any(ms < TINY_MS)) {                // one answer for all waves of the row
+        float eps = a.eps;
+        asm volatile("" : "+s"(eps));           // formed here: no register holds it for every row
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] *= LIFT;
+        ss = row_sum_again<NW>(squares(), red);
+        ms = ss / (float)d + eps * LIFT * LIFT;
+      }
+      const float inv = inv_rms(ss, ms);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         float fac[8], add[8];
@@ -280,7 +321,7 @@ quant_rows(const RowQuant a) {
       for (int j = 0; j < 8; ++j) c[j] = code_of<!NORM>(v[i][j], rs);
       if (FIT == WHOLE || first(i) + 8 <= d) {
         const uint32_t w[2] = {pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7])};
-        __builtin_memcpy(qp + first(i), w, 8);
+        __builtin_memcpy(qp + offset(first(i)), w, 8);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
