@@ -13,6 +13,7 @@
 // the chip runs at 1.76 of its 2.4 GHz and the matrix units are 58% busy.
 #include "gemm_common.h"
 
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -324,10 +325,25 @@ gemm_i8(const GemmI8 g, int how, int tiles_m, int tiles_n) {
 }
 
 template <typename T, int WM, int WN, int FM, int FN, int SK, int GK, int NSA, int NSB, int WPE>
-static void run_i8(const GemmI8& g, int how, hipStream_t st) {
-  const int tm = (int)((g.M + WM * FM * 32 - 1) / (WM * FM * 32)), tn = (int)((g.N + WN * FN * 32 - 1) / (WN * FN * 32));
-  hipLaunchKernelGGL((gemm_i8<T, WM, WN, FM, FN, SK, GK, NSA, NSB, WPE>), dim3(tm * tn),
-                     dim3(WM * WN * SK * GK * 64), 0, st, g, how, tm, tn);
+static void run_i8(GemmI8 g, int how, hipStream_t st) {
+  constexpr int BM = WM * FM * 32, BN = WN * FN * 32, THREADS = WM * WN * SK * GK * 64;
+  const int64_t tm = (g.M + BM - 1) / BM;
+  // a grid holds less than 2^32 threads: more columns than that (2^30 of one row) take
+  // another launch
+  const int64_t most = std::max<int64_t>(((1ll << 32) - 1) / THREADS / tm, 1) * BN;
+  for (int64_t left = g.N;; left -= most) {
+    g.N = std::min(left, most);
+    const int64_t tn = (g.N + BN - 1) / BN;
+    hipLaunchKernelGGL((gemm_i8<T, WM, WN, FM, FN, SK, GK, NSA, NSB, WPE>), dim3((unsigned)(tm * tn)), dim3(THREADS),
+                       0, st, g, how, (int)tm, (int)tn);
+    if (left <= most) return;
+    g.b += most * g.ldb;
+    g.b_scale += most;
+    if (g.bias != nullptr) g.bias = (const T*)g.bias + most;
+    if (g.res != nullptr) g.res = (const T*)g.res + most;
+    if (g.gate != nullptr) g.gate += most;
+    g.c = (T*)g.c + most;
+  }
 }
 
 // Tiles, and the choice among them by modelled time: t0 + n (fill + step stages),
