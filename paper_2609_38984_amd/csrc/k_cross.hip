@@ -347,14 +347,14 @@ cross_bf16(const CrossArgs c, const Partial part) {
 // (requesting K and V before the mask is known: 128, hidden tiles are loaded too).
 template <int D>
 __global__ void __launch_bounds__(256)
-cross_f32(const CrossArgs c, const Partial part) {
+cross_f32(const CrossArgs c, const Partial part, int tile0) {
   constexpr int LD = D + 4;
   __shared__ float os[4][32][LD];
   __shared__ float ms[4][32], ls[4][32];
   const int group = c.heads / c.kv_heads;
   const int hk = blockIdx.x % c.kv_heads;
   TileAt ta;
-  if (!tile_at(c, group, 32, blockIdx.x / c.kv_heads, ta)) return;
+  if (!tile_at(c, group, 32, tile0 + blockIdx.x / c.kv_heads, ta)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, r31 = lane & 31;
   const int rr = min(ta.r0 + r31, ta.rows - 1);
   f32x4 qf[D / 8];
@@ -562,9 +562,15 @@ static void run_cross(int dtype, const CrossArgs& c, float* ws, int64_t ws_float
   const int64_t rows = (int64_t)c.n_q * c.heads;
   const int splits = cross_splits(wgs, tiles, rows, D, ws_floats);
   const Partial p{ws, ws + splits * rows * D, splits, __builtin_ctz(splits)};
-  const dim3 grid((unsigned)wgs, splits);
-  if (dtype == 1) hipLaunchKernelGGL((cross_bf16<D>), grid, dim3(256), 0, st, c, p);
-  else hipLaunchKernelGGL((cross_f32<D>), grid, dim3(256), 0, st, c, p);
+  if (dtype == 1) {                             // (fewer than 2^32 threads at n_q * heads = 2^30)
+    hipLaunchKernelGGL((cross_bf16<D>), dim3((unsigned)wgs, splits), dim3(256), 0, st, c, p);
+  } else {
+    // a grid holds less than 2^32 threads: more tiles than that (2^29 rows) take another launch
+    const int64_t most = ((1 << 24) - 1) / c.kv_heads, tiles = wgs / c.kv_heads;
+    for (int64_t t = 0; t < tiles; t += most)
+      hipLaunchKernelGGL((cross_f32<D>), dim3((unsigned)(std::min(tiles - t, most) * c.kv_heads), splits), dim3(256),
+                         0, st, c, p, (int)t);
+  }
   if (splits > 1) {
     const unsigned n = (unsigned)((rows + 3) / 4);
     if (dtype == 1) hipLaunchKernelGGL((cross_join<bf16_t, D>), dim3(n), dim3(256), 0, st, c, p);

@@ -39,3 +39,41 @@ def test_gemm_of_more_columns_than_a_grid_holds(contexts, dtype, epilogue):
                    None if gt is None else gt[at], False, c[:, at])
     del w, c, b, r, gt, sw
     torch.cuda.empty_cache()
+
+
+def test_attention_of_more_tiles_than_a_grid_holds(contexts):
+    """float32, 65,535 heads of their own: with one key to a head the output is its value, and
+    the normaliser the score."""
+    room(235)
+    g, heads, n_q, n_seqs, dim = gen(4), 65535, 6309, 64, 64
+    q = torch.empty((n_q, heads, dim), device="cuda")
+    for part in q.split(256):
+        part.uniform_(-1, 1, generator=g)
+    k, v = torch.empty((2, n_seqs, heads, dim), device="cuda").uniform_(-1, 1, generator=g)
+    o, lse = torch.empty_like(q), torch.empty((n_q, heads), device="cuda")
+    for part in o.split(256):
+        part.fill_(7.0)
+    # one query more than whole tiles of 32 in each sequence: 259 tiles of each head, of which
+    # one grid holds 256
+    lq = [1 + 32 * (5 * i % 7) for i in range(n_seqs - 1)]
+    lq.append(n_q - 5 - sum(lq))
+    assert sum((n + 31) // 32 for n in lq) == 259
+    cu_q = torch.tensor([0] + lq, device="cuda").cumsum(0).to(torch.int32)
+    cu_k = torch.arange(n_seqs + 1, device="cuda", dtype=torch.int32)
+    contexts["f32"].cross_attention(q, k, v, o, cu_q=cu_q, cu_k=cu_k, lse=lse)
+    at = 0
+    for i, n in enumerate(lq):
+        for lo in range(at, at + n, 200):
+            rows = slice(lo, min(lo + 200, at + n))
+            # p is exp2 of a difference of zero up to the rounding of a score below 8: 1 and a sum of
+            # itself, divided: 4 roundings of the value
+            assert bool(((o[rows] - v[i]).abs() <= 2.0 ** -22 * v[i].abs()).all()), (i, lo)
+        first = slice(at, at + 1)
+        want = (q[first].double() * k[i].double()).sum(2) / 8
+        size = (q[first].double() * k[i].double()).abs().sum(2) / 8
+        # 64 products and sums (twice 2^-24 for the matrix unit), the scale, the maximum, the logarithm
+        assert bool(((lse[first].double() - want).abs() <= 2 * 80 * 2.0 ** -24 * size + 2.0 ** -20).all()), i
+        at += n
+    assert bool((o[at:] == 7.0).all())
+    del q, o, k, v, lse
+    torch.cuda.empty_cache()
