@@ -227,32 +227,22 @@ gemm_i8(const GemmI8 g, int how, int tiles_m, int tiles_n) {
   // A stage's last operands are in registers before they are multiplied: the next
   // stage has to be there then, its first operands are read behind the MFMAs, and the
   // slots of this one are loaded again.
-  auto stage = [&](int it, auto first) {
-    constexpr int F = decltype(first)::value;
+  static_assert(KPW % 2 == 0, "a stage begins with the first operand set");
+  for (int it = 0; it < n_it; ++it) {
 #pragma unroll
     for (int q = 0; q < KPW; ++q) {
       if (q + 1 < KPW) {
-        read((F + q + 1) & 1, sa, sb, q + 1);
+        read((q + 1) & 1, sa, sb, q + 1);
       } else {
         sync(std::integral_constant<int, (NSA - 2) * A_INS + (NSB - 2) * B_INS>{});
         issue(rb, ring_b + sb * BN * 8, vb, it + NSB);
         issue(ra, ring_a + sa * BM * 8, va, it + NSA);
         sa = sa + 1 == NSA ? 0 : sa + 1;
         sb = sb + 1 == NSB ? 0 : sb + 1;
-        read((F + q + 1) & 1, sa, sb, 0);
+        read((q + 1) & 1, sa, sb, 0);
       }
-      multiply((F + q) & 1);
+      multiply(q & 1);
     }
-  };
-  if constexpr (KPW % 2 == 0) {
-    for (int it = 0; it < n_it; ++it) stage(it, std::integral_constant<int, 0>{});
-  } else {
-    int it = 0;
-    for (; it + 1 < n_it; it += 2) {
-      stage(it, std::integral_constant<int, 0>{});
-      stage(it + 1, std::integral_constant<int, 1>{});
-    }
-    if (it < n_it) stage(it, std::integral_constant<int, 0>{});
   }
   // Epilogue: each wave parks 32 rows of its tile, then the WK waves of one place
   // share its runs of 8 columns; a lane always has the same columns.  Everything it
