@@ -390,6 +390,10 @@ static void run_gemm_i8(const GemmI8& g, hipStream_t st) {
   }
 }
 
+extern "C" int swam_gemm_i8_tile(int64_t m, int64_t n, int64_t k) {
+  return m > 0 && n > 0 && k > 0 ? choose_i8(m, n, k) : -1;
+}
+
 hipError_t launch_gemm_i8(int dtype, const GemmI8& g, hipStream_t st) {
   if (g.M <= 0 || g.N <= 0) return hipSuccess;
   if (dtype == 1) run_gemm_i8<bf16_t>(g, st);

@@ -270,6 +270,9 @@ struct GemmI8 {
   bool gelu;
 };
 hipError_t launch_gemm_i8(int dtype, const GemmI8& g, hipStream_t st);
+// which of the product's nine tiles (0 to 8) these sizes run on; host only, for tests that
+// have to reach them all
+extern "C" int swam_gemm_i8_tile(int64_t m, int64_t n, int64_t k);
 
 // attention to an encoder's states (k_cross.hip); ws: workspace for the partial
 // results of split keys
