@@ -296,9 +296,11 @@ class Context:
         self.stream = stream or torch.cuda.current_stream()
         self.device = self.stream.device.index   # the GPU that the operators' tensors lie on
         h = C.c_void_p()
-        _check(self.lib, None, self.lib.swam_create(C.byref(self.c_cfg),
-                                                    C.c_void_p(self.stream.cuda_stream),
-                                                    C.byref(h)))
+        # the workspace comes from the current device: the stream's, whatever the caller's is
+        with torch.cuda.device(self.device):
+            _check(self.lib, None, self.lib.swam_create(C.byref(self.c_cfg),
+                                                        C.c_void_p(self.stream.cuda_stream),
+                                                        C.byref(h)))
         self.h = h
 
     def close(self):
@@ -313,8 +315,10 @@ class Context:
         _check(self.lib, self.h, rc)
 
     def set_stream(self, stream: torch.cuda.Stream):
-        """swam_set_stream: later calls run on `stream`, after the work already
-        queued on the previous one."""
+        """swam_set_stream: later calls run on `stream`, of the same GPU, after the
+        work already queued on the previous one."""
+        if stream.device.index != self.device:
+            raise ValueError(f"the stream is on GPU {stream.device.index}, the context on {self.device}")
         self._ok(self.lib.swam_set_stream(self.h, C.c_void_p(stream.cuda_stream)))
         self.stream = stream
 
