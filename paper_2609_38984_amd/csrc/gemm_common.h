@@ -1,5 +1,5 @@
-// Shared pieces of the bf16 projection kernels: the fused epilogue functions,
-// the workgroup-to-tile map and the buffer-to-LDS addressing helpers.
+// Shared pieces of the projection kernels: the fused epilogue functions, the
+// workgroup-to-tile map and the buffer-to-LDS loading helpers (cross attention's too).
 #pragma once
 #include "launchers.h"
 
@@ -120,6 +120,22 @@ __device__ __forceinline__ int vadd_sgpr(int v, int s) {
   int r;
   asm volatile("v_add_u32 %0, %1, %2" : "=v"(r) : "s"(s), "v"(v));
   return r;
+}
+
+// wait until at most V vector-memory operations and no LDS operation of this
+// wave are outstanding (vmcnt in bits 3:0 and 15:14, lgkmcnt in bits 11:8);
+// the empty asm statements keep the compiler's memory operations on their side
+template <int V>
+__device__ __forceinline__ void wait_stage() {
+  static_assert(V >= 0 && V < 64, "vmcnt is a 6-bit counter");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((V & 15) | (7 << 4) | ((V >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+
+// one DMA instruction: 16 bytes per lane from the buffer at `off` to a 1 KB LDS slab
+__device__ __forceinline__ void dma_slab(__amdgpu_buffer_rsrc_t r, uint4* slab, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)slab, 16, off, 0, 0, 0);
 }
 
 // Ring kernel (k_ring.hip): tiles, arguments and launcher.

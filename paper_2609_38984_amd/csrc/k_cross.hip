@@ -17,24 +17,18 @@
 // (10,160 rows of 24 heads on one tile 20 us for 62 MB, 4 us more for each further tile);
 // for single queries the bytes of K and V (8 x 10,160 keys of 24 heads 100 us, 499 MB at
 // 5.0 TB/s).  4,096 x 4,096 at head_dim 128 and 16 heads 138 us: 1,000 TFLOP/s.
-#include "launchers.h"
+#include "gemm_common.h"
 
 #include <algorithm>
 #include <cfloat>
 
 namespace swam {
 
-typedef __attribute__((address_space(3))) void lds_void_t;
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
 constexpr int CR_BK = 64;                      // keys per tile: one bit of a mask word each
-constexpr int CR_DWORD3 = 0x00020000;          // raw buffer descriptor, 32-bit data
 constexpr int CR_PAST_END = 0x7fffff00;        // an offset that no tile reaches
-// one DMA instruction: 16 bytes per lane at `off` to a 1 KB slab of LDS
-__device__ __forceinline__ void cr_slab(__amdgpu_buffer_rsrc_t r, uint4* slab, int off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)slab, 16, off, 0, 0, 0);
-}
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // The sequence that holds tile t of `bq` rows (rows are tokens x group): lane b
@@ -144,22 +138,22 @@ cross_bf16(const CrossArgs c, const Partial part) {
     const int64_t row = ta.s0 + (int64_t)t * CR_BK;
     const int rows = min(ta.s1 - (int)row, CR_BK);
     const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)((const bf16_t*)c.k + row * c.k_ld + hk * D), (short)0, ((rows - 1) * (int)c.k_ld + D) * 2, CR_DWORD3);
+        (void*)((const bf16_t*)c.k + row * c.k_ld + hk * D), (short)0, ((rows - 1) * (int)c.k_ld + D) * 2, SWAM_BUF_DWORD3);
     const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)((const bf16_t*)c.v + row * c.v_ld + hk * D), (short)0, ((rows - 1) * (int)c.v_ld + D) * 2, CR_DWORD3);
+        (void*)((const bf16_t*)c.v + row * c.v_ld + hk * D), (short)0, ((rows - 1) * (int)c.v_ld + D) * 2, SWAM_BUF_DWORD3);
     const int at = wave * (SLABS / NW) * 64;
     if (vis == ~(uint64_t)0) {
 #pragma unroll
       for (int j = 0; j < SLABS / NW; ++j) {
-        cr_slab(rk, &to[0][at + j * 64], off_k[j]);
-        cr_slab(rv, &to[1][at + j * 64], off_v[j]);
+        dma_slab(rk, &to[0][at + j * 64], off_k[j]);
+        dma_slab(rv, &to[1][at + j * 64], off_v[j]);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < SLABS / NW; ++j) {
         const bool see = (vis >> (8 * ((wave * (SLABS / NW) + j) & 7) + lrow)) & 1;
-        cr_slab(rk, &to[0][at + j * 64], see ? off_k[j] : CR_PAST_END);
-        cr_slab(rv, &to[1][at + j * 64], see ? off_v[j] : CR_PAST_END);
+        dma_slab(rk, &to[0][at + j * 64], see ? off_k[j] : CR_PAST_END);
+        dma_slab(rv, &to[1][at + j * 64], see ? off_v[j] : CR_PAST_END);
       }
     }
   };

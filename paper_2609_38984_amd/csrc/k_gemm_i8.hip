@@ -25,25 +25,10 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr int I8_BK = 128;            // codes of K per stage: a 128-byte row
 constexpr int I8_DEAD = 0x40000000;   // an offset past every tile (256 rows of less than 2^22 bytes)
 
-// wait until at most V vector-memory operations and no LDS operation of this wave
-// are outstanding
-template <int V>
-__device__ __forceinline__ void i8_wait() {
-  static_assert(V >= 0 && V < 64, "vmcnt is a 6-bit counter");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((V & 15) | (7 << 4) | ((V >> 4) << 14));
-  asm volatile("" ::: "memory");
-}
-
 // bytes of the operand from row r0 on, at most `rows` of them
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t i8_rows(const int8_t* p, int64_t ld, int r0, int rows, int K) {
   return __builtin_amdgcn_make_buffer_rsrc((void*)(p + r0 * ld), (short)0, (int)((rows - 1) * ld) + K,
                                            SWAM_BUF_DWORD3);
-}
-
-// one DMA instruction: 16 bytes per lane at `off` to a 1 KB slab of the ring
-__device__ __forceinline__ void i8_slab(__amdgpu_buffer_rsrc_t r, uint4* slab, int off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)slab, 16, off, 0, 0, 0);
 }
 
 // tanh-GELU u / (1 + exp(-2 sqrt(2/pi) (u + 0.044715 u^3))) with the cubic in Horner's
@@ -165,19 +150,19 @@ gemm_i8(const GemmI8 g, int how, int tiles_m, int tiles_n) {
     if (K - k0 >= I8_BK || k0 >= K) {
       const int k = k0 < K ? k0 : I8_DEAD;
 #pragma unroll
-      for (int j = 0; j < INS; ++j) i8_slab(rs, to + (wr * INS + j) * 64, vadd_sgpr(v[j], k));
+      for (int j = 0; j < INS; ++j) dma_slab(rs, to + (wr * INS + j) * 64, vadd_sgpr(v[j], k));
     } else {                                          // the last stage of a K off the stages
 #pragma unroll
       for (int j = 0; j < INS; ++j) {
         const int ch = (lane & 7) ^ lds_swz((wr * INS + j) * 8 + (lane >> 3));
-        i8_slab(rs, to + (wr * INS + j) * 64, v[j] + (k0 + 16 * ch < K ? k0 : I8_DEAD));
+        dma_slab(rs, to + (wr * INS + j) * 64, v[j] + (k0 + 16 * ch < K ? k0 : I8_DEAD));
       }
     }
   };
   // own loads but the `V` youngest have landed and own LDS reads are done; behind the
   // barrier so are those of every wave that shares the ring
   auto sync = [&](auto allow) {
-    i8_wait<decltype(allow)::value>();
+    wait_stage<decltype(allow)::value>();
     if constexpr (NR > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
@@ -273,7 +258,7 @@ gemm_i8(const GemmI8 g, int how, int tiles_m, int tiles_n) {
     }
   };
   load_res(0);
-  i8_wait<0>();
+  wait_stage<0>();
   if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   int* park = reinterpret_cast<int*>(lds) + wave * 32 * EP_LD;

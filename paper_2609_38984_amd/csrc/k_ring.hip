@@ -27,22 +27,6 @@
 
 namespace swam {
 
-// wait until at most V vector-memory operations and no LDS operation of this
-// wave are outstanding (vmcnt in bits 3:0 and 15:14, lgkmcnt in bits 11:8);
-// the empty asm statements keep the compiler's memory operations on their side
-template <int V>
-__device__ __forceinline__ void wait_stage() {
-  static_assert(V >= 0 && V < 64, "vmcnt is a 6-bit counter");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((V & 15) | (7 << 4) | ((V >> 4) << 14));
-  asm volatile("" ::: "memory");
-}
-
-// one DMA instruction: 16 bytes per lane from the buffer at `off` to a 1 KB LDS slab
-__device__ __forceinline__ void dma_slab(__amdgpu_buffer_rsrc_t r, uint4* slab, int off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)slab, 16, off, 0, 0, 0);
-}
-
 // acc += A B^T for one 16-byte chunk per lane of a 32-row A and B fragment.  The
 // fragments are values of the vector type: read through a pointer to the LDS
 // words the compiler waits for every DMA load in flight before each stage.
