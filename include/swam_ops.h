@@ -95,8 +95,10 @@ int swam_gemm_i8(swam_ctx* ctx, const int8_t* a, int64_t lda, const float* a_sca
  *   o_h(i) = sum_j p_ij v_h'(j),  p_ij = softmax_j(scale q_h(i) . k_h'(j))
  * over the visible keys j of the key sequence that i's sequence attends, with
  * h' = h / (n_heads / n_kv_heads).  lse (optional) receives the natural-log
- * normaliser of every row and head.  A row without a visible key gets zeros and
- * minus infinity.
+ * normaliser of every row and head.  A row without a visible key, or whose visible
+ * scores are all minus infinity, gets zeros and minus infinity.  Scores, weights and
+ * sums are float32; a bf16 context rounds the weights to bf16 in front of the product
+ * with v (an error of 0.0016 of the output's size beside the 0.0017 of its own rounding).
  *   q, o : act, token i, head h at q + i q_stride + h head_dim (n_q tokens)
  *   k, v : act, token j, head h' at k + j k_stride + h' head_dim (n_k tokens)
  *   key_mask : bytes [n_k], 0 hides a key (padding), or NULL.  What hidden keys

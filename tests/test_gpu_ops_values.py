@@ -140,6 +140,25 @@ def test_visible_values_that_are_not_finite_stay_in_their_rows(contexts, dtype, 
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n_q,n_k", [(1, 2500), (70, 300), (300, 1000)])
+@pytest.mark.parametrize("part", ["first", "last", "all"])
+def test_visible_scores_of_minus_infinity_are_as_hidden(contexts, dtype, dim, n_q, n_k, part):
+    dt, g, heads = TYPES[dtype], gen(23 + dim), 4
+    q, _ = rows_of((n_q, heads, dim), dt, g)
+    q[:, :, 0] = 1.0
+    k, _ = rows_of((n_k, heads, dim), dt, g)
+    v, _ = rows_of((n_k, heads, dim), dt, g)
+    seen = torch.ones(n_k, dtype=torch.bool, device="cuda")
+    seen[{"first": slice(0, 2 * n_k // 3), "last": slice(n_k // 3, n_k), "all": slice(0, n_k)}[part]] = False
+    clean = k.clone()
+    k[~seen, :, 0] = -math.inf
+    o, lse = torch.full_like(q, 7.0), torch.full((n_q, heads), 7.0, device="cuda")
+    contexts[dtype].cross_attention(q, k, v, o, lse=lse)
+    check_attention(q, clean, v, o, lse, [n_q], [n_k], [0], seen, dim ** -0.5, o, lse)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("m,n,k", [(1, 40, 48), (130, 264, 272), (700, 1540, 528)])
 def test_infinities_through_the_epilogue(contexts, dtype, m, n, k):
     """A bias or residual that is not finite goes through the formula into its own column or
