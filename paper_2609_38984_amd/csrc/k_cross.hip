@@ -12,11 +12,14 @@
 // Softmax in one pass with a running maximum (base 2, float32).
 //
 // What bounds it: for many rows the instructions of a score (head_dim 64, per wave and
-// tile: 16 MFMAs of 32 cycles, 32 exponentials of 8, 81 other vector operations; MFMA and
-// vector work of different waves hardly overlap) and, on few keys, the queries and outputs
-// (10,160 rows of 24 heads on one tile 20 us for 62 MB, 4 us more for each further tile);
-// for single queries the bytes of K and V (8 x 10,160 keys of 24 heads 100 us, 499 MB at
-// 5.0 TB/s).  4,096 x 4,096 at head_dim 128 and 16 heads 138 us: 1,000 TFLOP/s.
+// tile: 16 MFMAs of 32 cycles, 32 exponentials of 8, 81 other vector operations, which
+// overlap with other waves' MFMAs in part: two waves of each take 83 cycles (exponentials,
+// products) to 113 (fused, conversions) where either kind alone takes 64 to 69; additions,
+// 35 alone, come on top in full)
+// and, on few keys, the queries and outputs (10,160 rows of 24 heads on one tile 20 us for
+// 62 MB, 4 us more for each further tile); for single queries the bytes of K and V (8 x
+// 10,160 keys of 24 heads 100 us, 499 MB at 5.0 TB/s).  4,096 x 4,096 at head_dim 128 and
+// 16 heads 138 us: 1,000 TFLOP/s.
 #include "gemm_common.h"
 
 #include <algorithm>
@@ -219,7 +222,10 @@ cross_bf16(const CrossArgs c, const Partial part) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(st[t][8 * u + mm], sc, -m_run));
             const float p1 = __builtin_amdgcn_exp2f(fmaf(st[t][8 * u + mm + 1], sc, -m_run));
             ps0 += p0; ps1 += p1;
-            // P in bf16, the other operand's type; the sum keeps float32
+            // P in bf16, the other operand's type; the sum keeps float32.  Outputs are off by
+            // 0.0023 of their size where bf16 itself makes 0.0017; the rest of P as a second
+            // operand gives the 0.0017 and takes 80 us for 71 (8 sequences of up to 3,360, 12
+            // heads of 128), 61 for 45 (10,160 x 24 heads on 512), 133 for 106 (8 x 1 on 10,160)
             pf[t][u][mm] = (__bf16)p0; pf[t][u][mm + 1] = (__bf16)p1;
           }
     };
@@ -337,8 +343,9 @@ cross_bf16(const CrossArgs c, const Partial part) {
 // memory (an MFMA takes 64 cycles for 4 to 16 bytes per lane).  Four waves take
 // every fourth tile of 32 keys of the same 32 rows and meet in LDS.  326 rows of 24
 // heads on 77 keys 9.3 us: one tile to a wave, the chain of its loads (offsets, mask,
-// K and V, merge) around 2 us of MFMAs.  3,000 x 12 heads of 128 on 512 keys 96 us
-// (requesting K and V before the mask is known: 128, hidden tiles are loaded too).
+// K and V, merge) around 2 us of MFMAs.  3,000 x 12 heads of 128 on 512 keys 110 us for
+// 62 of MFMAs (requesting K and V before the mask is known: a third more, hidden tiles are
+// loaded too); 8 x 1 query of 24 heads on 10,160 keys 250 us (998 MB), 1 x 1 47.
 template <int D>
 __global__ void __launch_bounds__(256)
 cross_f32(const CrossArgs c, const Partial part, int tile0) {
@@ -469,7 +476,8 @@ cross_f32(const CrossArgs c, const Partial part, int tile0) {
 
 // One wave per token and head adds up the slices, in a fixed order.  Lane s weighs slice
 // s; D / 4 lanes hold a slice's row, so a wave reads several at once and eight such
-// loads are in flight (32 slices of 32 rows 4 us; one slice after the other 12).  Rows outside every sequence have none and are left as they are.
+// loads are in flight (32 slices of 32 rows 4 us; one slice after the other 12).  Rows
+// outside every sequence have none and are left as they are.
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
 cross_join(const CrossArgs c, const Partial part) {
@@ -532,10 +540,18 @@ static int64_t cross_slots(const CrossArgs& c, int64_t bq) {
 // tile, so the keys are split, as far as the workspace holds the partial results.  Chosen
 // by modelled time (us): tiles per slice, each `lone` for a workgroup by itself and
 // `share` per workgroup where several share a CU, plus the pass that joins the
-// slices and what they write and read.  us without | with the chosen split: 8 x 1 query
-// of 24 heads on 10,160 keys 240 | 118 (4 slices), 1 x 32 of 128 on 10,160 229 | 18.7 (64),
-// 32 x 24 on 2,048 39 | 12.7 (16), 300 x 16 on 4,096 70 | 25 (8), 326 x 24 on 2,048 38 | 24
-// (4); 512 x 24 on 512 11 | 19 (2, not chosen), 4,096 x 12 of 128 on 512 25 | 58 (2, not chosen).
+// slices and what they write and read.  bf16, us without | with the chosen split: 8 x 1
+// query of 24 heads on 10,160 keys 245 | 100 (4 slices), 1 query of 32 heads of 128 on 8 on
+// 10,160 233 | 19 (64), 32 x 24 on 2,048 40 | 13 (16), 300 x 16 on 4,096 69 | 25 (8), 326 x
+// 24 on 2,048 37 | 24 (4); 512 x 24 on 512 11 | 19 (2, not chosen), 4,096 x 12 of 128 on 512
+// 23 | 54 (2, not chosen).
+// The constants are the bf16 kernel's.  For float32 they are within 4% of the best split for
+// single queries (the same three 379 | 250, 458 | 31, 61 | 18) and up to a quarter off for
+// many rows: 300 x 16 114 | 80 (4; 8: 70), 326 x 24 92 | 80 (2; 8: 71), 1,000 x 12 of 128 on
+// 4,096 330 (none; 4: 262).
+// The lengths are on the device, so the mean one counts: beside 63 prompts of 16 states one
+// of 10,160 is not split (64 x 1 query of 24 heads 186 us, with 8 slices 60), beside 7 of 512
+// into 4 (57, with 16 slices 34).
 static int cross_splits(int64_t wgs, int64_t tiles, int64_t rows, int D, int64_t ws_floats) {
   const double lone = D == 64 ? 1.2 : 1.6, share = D == 64 ? 0.64 : 1.0;
   int best = 1;

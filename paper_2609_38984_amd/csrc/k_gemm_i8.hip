@@ -10,7 +10,7 @@
 // The descriptors of the loads end with the operand, so rows past M or N read as
 // zeros; chunks past K get an offset past the end.
 // 8,192^3: 2,200-2,400 TOP/s by box (the library's product there: 2,150), at which
-// the chip runs at 1.76 of its 2.4 GHz and the matrix units are 58% busy.
+// the chip runs at 1.7 of its 2.4 GHz and the matrix units are busy for 65% of the cycles.
 #include "gemm_common.h"
 
 #include <algorithm>
@@ -32,7 +32,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t i8_rows(const int8_t* p, int64
 }
 
 // tanh-GELU u / (1 + exp(-2 sqrt(2/pi) (u + 0.044715 u^3))) with the cubic in Horner's
-// form, on the hardware exp2 and reciprocal (about 1 ulp each)
+// form (fewer operations than gelu_tanh of the bf16 projections: GELU is 25 of 310 us at
+// 17,472 x 8,192 x 2,048), on the hardware exp2 and reciprocal (about 1 ulp each)
 __device__ __forceinline__ float i8_gelu(float u) {
   constexpr float c = -2.0f * 1.4426950408889634f * 0.7978845608028654f;
   return u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * fmaf(u * u, c * 0.044715f, c)));
@@ -50,8 +51,8 @@ __device__ __forceinline__ void i8_load8(const T* p, bool whole, int n, float fi
 }
 
 // how the output is stored: whole, 16-byte aligned runs of 8 columns in every operand of
-// the epilogue; larger than the 256 MB cache behind the L2 (stored past the caches, which
-// then keep A and B: 17,472 x 8,192 x 2,048 317 us, through them 325)
+// the epilogue; larger than the 256 MB cache behind the L2 (bf16 runs are then stored past
+// the caches, which keep A and B: 17,472 x 8,192 x 2,048 317 us, through them 325)
 enum { I8_ALIGNED = 1, I8_PAST_CACHE = 2 };
 constexpr int64_t I8_CACHE_BYTES = 256 << 20;
 
@@ -326,11 +327,14 @@ static void run_i8(GemmI8 g, int how, hipStream_t st) {
 // their rounds count in halves once the grid spills past one per CU (smoothly past
 // eight), and a lone one per CU takes `lone` of a shared round.  The constants (us)
 // are a fit to 17 row counts from 1 to 17,472 of 12 projections with N and K from 512
-// to 8,192; choosing by it runs 1.7% above the best of thirteen tiles on average.
-// E.g. 1 x 1,536 x 1,536 4.0 us on 32x32 (64x64 5.8, 256x256 19), 512 x 1,536 x 4,096
-// 11.1 on 64x64 (128x128 19), 3,472 x 1,536 x 6,144 38.4 on 192x128 with the k-steps
-// of a stage shared by two groups of waves (44.9 with one), 17,472 x 8,192 x 2,048 303
-// on 256x256 (192x128 319).
+// to 8,192, by relative error; choosing by it runs 1.7% above the best of thirteen tiles
+// on average.  It ranks tiles and is no forecast: large products take up to 1.4 times what
+// it says (8,192^3 485 for 334), for the clock falls under their load.
+// Measured (the model's figure behind it): 1 x 1,536 x 1,536 4.0 us (4.4) on 32x32 (64x64
+// 5.8 (6.4), 256x256 19 (22)), 512 x 1,536 x 4,096 11.1 (10.3) on 64x64 (128x128 19 (19)),
+// 3,472 x 1,536 x 6,144 38.4 (32.6) on 192x128 with the k-steps of a stage shared by two
+// groups of waves (44.9 (36.8) with one), 17,472 x 8,192 x 2,048 303 (244) on 256x256
+// (192x128 319 (300)).
 struct I8Tile {
   int bm, bn, pair;
   double lone, t0, fill, step;
