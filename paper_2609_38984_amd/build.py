@@ -27,6 +27,7 @@ HIPCC_FLAGS = [
 EXTRA_DEVICE_FLAGS = {
     "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
     "k_cross.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "k_cache.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

@@ -288,4 +288,49 @@ struct CrossArgs {
 };
 hipError_t launch_cross(int dtype, const CrossArgs& a, float* ws, int64_t ws_floats, hipStream_t st);
 
+// ---------------------------------------------------------------------------
+// streaming block on a paged cache (swam_cache.h)
+// ---------------------------------------------------------------------------
+// the cache and the chunk behind it: token j of sequence s is slot j & (2^lg_page - 1) of
+// page table[s][j >> lg_page]
+struct Paged {
+  void *k, *v;
+  int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+  const int32_t* table;
+  const int32_t* length;
+  const int32_t* cu;                   // [n_seqs + 1] or NULL: one sequence of all rows
+  int64_t table_ld;
+  int n_pages, lg_page, max_pages, n_seqs, kv_heads;
+};
+// norm and rotation of head vectors (k_head.hip), to rows or, with cache, k and v to
+// their pages
+struct HeadPost {
+  const void *q, *k, *v;               // v with a cache only
+  int64_t q_ld, k_ld, v_ld;
+  void *q_out, *k_out;                 // k_out without a cache only
+  int64_t qo_ld, ko_ld;
+  const void *q_gain, *k_gain;
+  const double* freq;
+  const int32_t* pos;
+  int64_t rows;
+  int heads, kv_heads, dim;
+  int norm, rot, half;                 // rot: rotated elements, half: their layout
+  float eps, mag;
+};
+hipError_t launch_head_post(int dtype, const HeadPost& a, const Paged* cache, hipStream_t st);
+
+// attention of a chunk to its cache (k_cache.hip); ws: workspace for the partial
+// results of split keys
+struct CacheArgs {
+  Paged pg;
+  const void* q;
+  void* o;
+  float* lse;
+  int64_t q_ld, o_ld;
+  int n_q, heads, dim;
+  int causal, window;
+  float scale;
+};
+hipError_t launch_cache_attention(int dtype, const CacheArgs& a, float* ws, int64_t ws_floats, hipStream_t st);
+
 }  // namespace swam

@@ -15,6 +15,7 @@
 
 #include "../../include/swam.h"
 #include "../../include/swam_ops.h"
+#include "../../include/swam_cache.h"
 #include "launchers.h"
 
 #include <cmath>
@@ -348,6 +349,95 @@ struct OnDevice {
     if (prev >= 0) (void)hipSetDevice(prev);
   }
 };
+
+// ---- arguments of the operators of swam_cache.h
+
+int check_post(swam_ctx* c, const swam_qk_post* p, int32_t head_dim) {
+  if (p->norm != 0 && p->norm != 1) return set_err(c, SWAM_E_INVALID, "norm must be 0 or 1");
+  if (p->norm && (!(p->eps >= 0.0f) || !std::isfinite(p->eps)))
+    return set_err(c, SWAM_E_INVALID, "eps must be finite and >= 0");
+  if (!p->norm && (p->q_gain || p->k_gain)) return set_err(c, SWAM_E_INVALID, "a gain needs the norm");
+  if (!aligned16(p->q_gain) || !aligned16(p->k_gain)) return set_err(c, SWAM_E_INVALID, "gains must be 16-byte aligned");
+  if (p->rope_dims < 0 || p->rope_dims > head_dim || p->rope_dims % 2)
+    return set_err(c, SWAM_E_SHAPE, "rope_dims must be even, 0 to head_dim");
+  if (p->rope_dims == 0) return SWAM_OK;
+  if (p->rope_layout != SWAM_ROPE_INTERLEAVED && p->rope_layout != SWAM_ROPE_HALF)
+    return set_err(c, SWAM_E_INVALID, "unknown rope_layout");
+  if (!p->rope_freq) return set_err(c, SWAM_E_INVALID, "rope_freq required");
+  if (!typed(p->rope_freq, 8)) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  if (!std::isfinite(p->rope_magnitude)) return set_err(c, SWAM_E_INVALID, "rope_magnitude must be finite");
+  return SWAM_OK;
+}
+
+// head rows of an act tensor: NULL where there are no heads
+int check_heads(swam_ctx* c, const void* p, int64_t ld, int64_t rows, int64_t width, const char* name) {
+  if (width == 0) return p ? set_err(c, SWAM_E_INVALID, std::string(name) + " without heads") : SWAM_OK;
+  if (rows > 0 && !p) return set_err(c, SWAM_E_INVALID, std::string(name) + " required");
+  if (ld < width) return set_err(c, SWAM_E_INVALID, std::string(name) + ": row stride is smaller than its row");
+  if (far_apart(rows, ld)) return set_err(c, SWAM_E_SHAPE, "rows times row stride below 2^48");
+  if (!aligned16(p) || (rows > 1 && ld * ops_esz(c) % 16))
+    return set_err(c, SWAM_E_INVALID, std::string(name) + " and its rows must be 16-byte aligned");
+  return SWAM_OK;
+}
+
+// K or V of a cache: strides whose elements do not meet, and the bytes they span
+int check_pages(swam_ctx* c, const void* p, int64_t page, int64_t token, int64_t head, const swam_kv_cache* k, Span* out) {
+  const int64_t es = ops_esz(c);
+  *out = Span{0, 0, 0, 0};
+  if (k->n_pages == 0) return SWAM_OK;
+  if (!p) return set_err(c, SWAM_E_INVALID, "the cache's k and v required");
+  struct Dim { int64_t step, n; } d[3] = {{page, k->n_pages}, {token, k->page_size}, {head, k->n_kv_heads}};
+  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.step < b.step; });
+  int64_t extent = k->head_dim;                 // elements of what lies inside
+  for (const Dim& x : d) {
+    if (x.n == 1) continue;
+    if (x.step < extent) return set_err(c, SWAM_E_INVALID, "the cache's strides let elements meet");
+    if (x.step > (1ll << 48) / x.n) return set_err(c, SWAM_E_SHAPE, "a cache's dimension times its stride below 2^48");
+    extent += x.step * (x.n - 1);
+  }
+  if (token > OPS_MAX_STRIDE) return set_err(c, SWAM_E_SHAPE, "the cache's token strides below 2^22");
+  if (!aligned16(p) || page * es % 16 || token * es % 16 || head * es % 16)
+    return set_err(c, SWAM_E_INVALID, "the cache's k, v and strides must be 16-byte aligned");
+  *out = Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)(extent * es), 0, 0};
+  return SWAM_OK;
+}
+
+int check_cache(swam_ctx* c, const swam_kv_cache* k, const int32_t* cu, Span* ks, Span* vs) {
+  if (!k) return set_err(c, SWAM_E_INVALID, "cache is NULL");
+  if (k->head_dim != 64 && k->head_dim != 128) return set_err(c, SWAM_E_SHAPE, "head_dim must be 64 or 128");
+  if (k->n_kv_heads < 1 || k->n_kv_heads >= (1 << 16)) return set_err(c, SWAM_E_SHAPE, "1 to 2^16 - 1 K/V heads");
+  if (k->page_size < 8 || k->page_size > SWAM_CACHE_MAX_PAGE || (k->page_size & (k->page_size - 1)))
+    return set_err(c, SWAM_E_SHAPE, "page_size must be a power of two, 8 to SWAM_CACHE_MAX_PAGE");
+  if (k->n_seqs < 1 || k->n_seqs > SWAM_CACHE_MAX_SEQS)
+    return set_err(c, SWAM_E_SHAPE, "1 to SWAM_CACHE_MAX_SEQS sequences");
+  if (k->n_pages < 0 || k->max_pages < 0) return set_err(c, SWAM_E_INVALID, "n_pages and max_pages must be >= 0");
+  if ((int64_t)k->max_pages * k->page_size >= (1ll << 30))
+    return set_err(c, SWAM_E_SHAPE, "max_pages * page_size below 2^30");
+  if (!cu && k->n_seqs != 1) return set_err(c, SWAM_E_INVALID, "several sequences need cu");
+  if (!k->length || (k->max_pages > 0 && !k->table)) return set_err(c, SWAM_E_INVALID, "table and length required");
+  if (k->table_stride < k->max_pages) return set_err(c, SWAM_E_INVALID, "table_stride < max_pages");
+  if (far_apart(k->n_seqs, k->table_stride)) return set_err(c, SWAM_E_SHAPE, "n_seqs times table_stride below 2^48");
+  if (!typed(k->table, 4) || !typed(k->length, 4) || !typed(cu, 4))
+    return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  if (int rc = check_pages(c, k->k, k->k_page, k->k_token, k->k_head, k, ks)) return rc;
+  if (int rc = check_pages(c, k->v, k->v_page, k->v_token, k->v_head, k, vs)) return rc;
+  if (k->n_pages > 0 && k->k == k->v) return set_err(c, SWAM_E_INVALID, "the cache's k and v are one tensor");
+  return SWAM_OK;
+}
+
+Paged paged(const swam_kv_cache* k, const int32_t* cu) {
+  return Paged{k->k, k->v, k->k_page, k->k_token, k->k_head, k->v_page, k->v_token, k->v_head, k->table, k->length,
+               cu, k->table_stride, (int)std::min<int64_t>(k->n_pages, INT32_MAX), __builtin_ctz(k->page_size),
+               k->max_pages, k->n_seqs, k->n_kv_heads};
+}
+
+void put_post(HeadPost& a, const swam_qk_post* p) {
+  if (!p) return;
+  a.norm = p->norm; a.eps = p->eps;
+  a.q_gain = p->q_gain; a.k_gain = p->k_gain;
+  a.rot = p->rope_dims; a.half = p->rope_layout == SWAM_ROPE_HALF;
+  a.freq = p->rope_freq; a.mag = p->rope_magnitude;
+}
 
 // one block in place on x [n_rows][d]; mod = this block's [6][d] modulation
 // pos_mode (rope only): 0 = dense layout, 1 = packed rows of the cached
@@ -1593,6 +1683,158 @@ int swam_cross_attention(swam_ctx* c, const void* q, int64_t q_stride, const voi
   Timed t(c, SWAM_T_CROSS);
   SWAM_HIP(c, launch_cross(c->cfg.dtype, a, c->ptr<float>(c->lay.splitk), c->dv.splitk_floats, c->st),
            "cross_attention");
+  return SWAM_OK;
+}
+
+// ------------------------------------------------ streaming block on a paged cache
+
+int swam_rope_frequencies(int32_t dims, double base, int32_t scaling, double factor, double trained,
+                          double* freq, float* magnitude) {
+  if (dims < 2 || dims % 2 || dims > SWAM_QK_MAX_DIM)
+    return set_err(nullptr, SWAM_E_SHAPE, "dims must be even, 2 to SWAM_QK_MAX_DIM");
+  if (!freq || !magnitude) return set_err(nullptr, SWAM_E_INVALID, "freq and magnitude required");
+  if (scaling < SWAM_ROPE_PLAIN || scaling > SWAM_ROPE_YARN) return set_err(nullptr, SWAM_E_INVALID, "unknown scaling");
+  if (!std::isfinite(base) || !(base > 1.0) || !std::isfinite(factor) || !(factor >= 1.0))
+    return set_err(nullptr, SWAM_E_INVALID, "need a finite base > 1 and a finite factor >= 1");
+  if (scaling == SWAM_ROPE_YARN && (!std::isfinite(trained) || !(trained > 0.0)))
+    return set_err(nullptr, SWAM_E_INVALID, "YARN needs the positions that the model was trained on");
+  if (scaling == SWAM_ROPE_NTK) {
+    if (dims == 2) return set_err(nullptr, SWAM_E_SHAPE, "NTK needs dims > 2");
+    base *= std::pow(factor, (double)dims / (dims - 2));
+  }
+  for (int32_t i = 0; i < dims / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / dims);
+    if (scaling == SWAM_ROPE_LINEAR) f /= factor;
+    if (scaling == SWAM_ROPE_YARN) {
+      const double turns = trained * f / (2.0 * M_PI);
+      const double g = std::min(1.0, std::max(0.0, (turns - 1.0) / 31.0));
+      f *= g + (1.0 - g) / factor;
+    }
+    freq[i] = f;
+  }
+  *magnitude = scaling == SWAM_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return SWAM_OK;
+}
+
+int swam_qk_norm_rope(swam_ctx* c, const swam_qk_post* post, const int32_t* pos, const void* q,
+                      int64_t q_stride, const void* k, int64_t k_stride, int64_t rows,
+                      int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void* q_out,
+                      int64_t qo_stride, void* k_out, int64_t ko_stride) {
+  if (!post) return set_err(c, SWAM_E_INVALID, "post is NULL");
+  if (head_dim < 8 || head_dim % 8 || head_dim > SWAM_QK_MAX_DIM)
+    return set_err(c, SWAM_E_SHAPE, "head_dim must be a multiple of 8 up to SWAM_QK_MAX_DIM");
+  if (n_heads < 0 || n_kv_heads < 0) return set_err(c, SWAM_E_INVALID, "n_heads and n_kv_heads must be >= 0");
+  if ((int64_t)n_heads + n_kv_heads >= (1 << 16)) return set_err(c, SWAM_E_SHAPE, "heads below 2^16");
+  if (rows < 0) return set_err(c, SWAM_E_INVALID, "rows must be >= 0");
+  if (rows >= (1ll << 31)) return set_err(c, SWAM_E_SHAPE, "rows below 2^31");
+  if (int rc = check_post(c, post, head_dim)) return rc;
+  const int64_t qw = (int64_t)n_heads * head_dim, kw = (int64_t)n_kv_heads * head_dim, es = ops_esz(c);
+  if (int rc = check_heads(c, q, q_stride, rows, qw, "q")) return rc;
+  if (int rc = check_heads(c, k, k_stride, rows, kw, "k")) return rc;
+  if (int rc = check_heads(c, q_out, qo_stride, rows, qw, "q_out")) return rc;
+  if (int rc = check_heads(c, k_out, ko_stride, rows, kw, "k_out")) return rc;
+  if (!typed(pos, 4)) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  const Span qs = span(q, q_stride, rows, qw, es), ks = span(k, k_stride, rows, kw, es);
+  const Span qo = span(q_out, qo_stride, rows, qw, es), ko = span(k_out, ko_stride, rows, kw, es);
+  const bool q_in = q_out == q && qo_stride == q_stride, k_in = k_out == k && ko_stride == k_stride;
+  if ((!q_in && meet(qo, qs)) || meet(qo, ks) || (!k_in && meet(ko, ks)) || meet(ko, qs) || meet(qo, ko))
+    return set_err(c, SWAM_E_INVALID, "an output overlaps another tensor (it may only be its input)");
+  for (const Span& in : {span(pos, 1, rows, 1, 4), span(post->q_gain, 1, head_dim, 1, es),
+                         span(post->k_gain, 1, head_dim, 1, es), span(post->rope_freq, 1, post->rope_dims / 2, 1, 8)})
+    if (meet(qo, in) || meet(ko, in)) return set_err(c, SWAM_E_INVALID, "an output overlaps an input");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (rows == 0 || n_heads + n_kv_heads == 0) return SWAM_OK;
+  HeadPost a{};
+  put_post(a, post);
+  a.q = q; a.q_ld = q_stride; a.k = k; a.k_ld = k_stride;
+  a.q_out = q_out; a.qo_ld = qo_stride; a.k_out = k_out; a.ko_ld = ko_stride;
+  a.pos = pos; a.rows = rows;
+  a.heads = n_heads; a.kv_heads = n_kv_heads; a.dim = head_dim;
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_HEAD_POST);
+  SWAM_HIP(c, launch_head_post(c->cfg.dtype, a, nullptr, c->st), "qk_norm_rope");
+  return SWAM_OK;
+}
+
+int swam_cache_append(swam_ctx* c, const swam_kv_cache* cache, const swam_qk_post* post,
+                      const int32_t* pos, const int32_t* cu, const void* q, int64_t q_stride,
+                      const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t rows,
+                      int32_t n_heads, void* q_out, int64_t qo_stride) {
+  Span kc, vc;
+  if (int rc = check_cache(c, cache, cu, &kc, &vc)) return rc;
+  const int64_t dim = cache->head_dim, es = ops_esz(c);
+  if (n_heads < 0) return set_err(c, SWAM_E_INVALID, "n_heads must be >= 0");
+  if (n_heads + 2ll * cache->n_kv_heads >= (1 << 16)) return set_err(c, SWAM_E_SHAPE, "heads of q, k and v below 2^16");
+  if (rows < 0) return set_err(c, SWAM_E_INVALID, "rows must be >= 0");
+  if (rows >= (1ll << 31)) return set_err(c, SWAM_E_SHAPE, "rows below 2^31");
+  if (post)
+    if (int rc = check_post(c, post, cache->head_dim)) return rc;
+  const int64_t qw = n_heads * dim, kw = cache->n_kv_heads * dim;
+  if (int rc = check_heads(c, q, q_stride, rows, qw, "q")) return rc;
+  if (int rc = check_heads(c, k, k_stride, rows, kw, "k")) return rc;
+  if (int rc = check_heads(c, v, v_stride, rows, kw, "v")) return rc;
+  if (int rc = check_heads(c, q_out, qo_stride, rows, qw, "q_out")) return rc;
+  if (!typed(pos, 4)) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  const Span qs = span(q, q_stride, rows, qw, es), qo = span(q_out, qo_stride, rows, qw, es);
+  if (!(q_out == q && qo_stride == q_stride) && meet(qo, qs))
+    return set_err(c, SWAM_E_INVALID, "q_out overlaps q (it may only be it)");
+  for (const Span& in : {span(k, k_stride, rows, kw, es), span(v, v_stride, rows, kw, es), span(pos, 1, rows, 1, 4),
+                         span(cu, 1, cache->n_seqs + 1, 1, 4), span(cache->length, 1, cache->n_seqs, 1, 4),
+                         span(cache->table, cache->table_stride, cache->n_seqs, cache->max_pages, 4),
+                         span(post ? post->q_gain : nullptr, 1, dim, 1, es),
+                         span(post ? post->k_gain : nullptr, 1, dim, 1, es),
+                         span(post ? post->rope_freq : nullptr, 1, post ? post->rope_dims / 2 : 0, 1, 8)}) {
+    if (meet(qo, in)) return set_err(c, SWAM_E_INVALID, "q_out overlaps an input");
+    if (meet(kc, in) || meet(vc, in)) return set_err(c, SWAM_E_INVALID, "the cache overlaps an input");
+  }
+  if (meet(kc, qs) || meet(vc, qs) || meet(kc, qo) || meet(vc, qo))
+    return set_err(c, SWAM_E_INVALID, "the cache overlaps q or q_out");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (rows == 0) return SWAM_OK;
+  HeadPost a{};
+  put_post(a, post);
+  a.q = q; a.q_ld = q_stride; a.k = k; a.k_ld = k_stride; a.v = v; a.v_ld = v_stride;
+  a.q_out = q_out; a.qo_ld = qo_stride;
+  a.pos = pos; a.rows = rows;
+  a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.dim = cache->head_dim;
+  const Paged pg = paged(cache, cu);
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_APPEND);
+  SWAM_HIP(c, launch_head_post(c->cfg.dtype, a, &pg, c->st), "cache_append");
+  return SWAM_OK;
+}
+
+int swam_cache_attention(swam_ctx* c, const swam_kv_cache* cache, const int32_t* cu, const void* q,
+                         int64_t q_stride, int64_t rows, int32_t n_heads, int32_t causal,
+                         int32_t window, float scale, void* o, int64_t o_stride, float* lse) {
+  Span kc, vc;
+  if (int rc = check_cache(c, cache, cu, &kc, &vc)) return rc;
+  if (n_heads < 1 || n_heads % cache->n_kv_heads)
+    return set_err(c, SWAM_E_INVALID, "n_heads must be a positive multiple of the K/V heads");
+  if (causal != 0 && causal != 1) return set_err(c, SWAM_E_INVALID, "causal must be 0 or 1");
+  if (window < 0) return set_err(c, SWAM_E_INVALID, "window must be >= 0");
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return set_err(c, SWAM_E_INVALID, "scale must be finite and > 0");
+  if (rows < 0) return set_err(c, SWAM_E_INVALID, "rows must be >= 0");
+  if (n_heads > 4096 || rows >= (1ll << 30) || rows * n_heads >= (1ll << 30))
+    return set_err(c, SWAM_E_SHAPE, "rows * n_heads below 2^30, n_heads up to 4096");
+  const int64_t dim = cache->head_dim, qw = n_heads * dim, es = ops_esz(c);
+  if (int rc = check_heads(c, q, q_stride, rows, qw, "q")) return rc;
+  if (int rc = check_heads(c, o, o_stride, rows, qw, "o")) return rc;
+  if (std::max(q_stride, o_stride) > OPS_MAX_STRIDE) return set_err(c, SWAM_E_SHAPE, "row strides below 2^22");
+  if (!typed(lse, 4)) return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
+  const Span os = span(o, o_stride, rows, qw, es), ls = span(lse, n_heads, rows, n_heads, 4);
+  for (const Span& in : {span(q, q_stride, rows, qw, es), kc, vc, span(cu, 1, cache->n_seqs + 1, 1, 4),
+                         span(cache->length, 1, cache->n_seqs, 1, 4),
+                         span(cache->table, cache->table_stride, cache->n_seqs, cache->max_pages, 4)})
+    if (meet(os, in) || meet(ls, in)) return set_err(c, SWAM_E_INVALID, "o or lse overlaps an input");
+  if (meet(os, ls)) return set_err(c, SWAM_E_INVALID, "o overlaps lse");
+  if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
+  if (rows == 0) return SWAM_OK;
+  CacheArgs a{paged(cache, cu), q, o, lse, q_stride, o_stride, (int)rows, n_heads, cache->head_dim, causal, window, scale};
+  OnDevice dev(c);
+  Timed t(c, SWAM_T_CACHE_ATTN);
+  SWAM_HIP(c, launch_cache_attention(c->cfg.dtype, a, c->ptr<float>(c->lay.splitk), c->dv.splitk_floats, c->st),
+           "cache_attention");
   return SWAM_OK;
 }
 

@@ -23,7 +23,7 @@ KIND_DENSE, KIND_REFRESH, KIND_SPARSE = 0, 1, 2
 KIND_NONE, KIND_ANY = -1, -2   # timer slots outside any step / every slot
 TIMERS = ["ADALN", "LNMOD", "GEMM_QKV", "ATTN", "GEMM_OUT", "GEMM_UP", "GEMM_DOWN", "SCORE",
           "REDUCE", "SELECT", "PACK", "UNPACK", "COPY", "SAMPLE", "QK_POST", "QUANT", "GEMM_I8",
-          "CROSS"]
+          "CROSS", "HEAD_POST", "APPEND", "CACHE_ATTN"]
 T = {name: i for i, name in enumerate(TIMERS)}
 
 EXPORTS = ["swam_create", "swam_destroy", "swam_set_stream", "swam_plan", "swam_status_str",
@@ -40,6 +40,12 @@ OP_EXPORTS = ["swam_rms_norm_i8", "swam_quantize_i8", "swam_gemm_i8", "swam_cros
 I8_MAX_WIDTH, I8_MAX_K = 32768, 131056   # SWAM_I8_MAX_WIDTH, SWAM_I8_MAX_K
 GEMM_GELU = 1                            # SWAM_GEMM_GELU
 
+# include/swam_cache.h
+CACHE_EXPORTS = ["swam_rope_frequencies", "swam_qk_norm_rope", "swam_cache_append", "swam_cache_attention"]
+CACHE_MAX_SEQS, CACHE_MAX_PAGE, QK_MAX_DIM = 1024, 4096, 512   # SWAM_CACHE_MAX_SEQS, ...
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}                     # SWAM_ROPE_INTERLEAVED, ...
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3}   # SWAM_ROPE_PLAIN, ...
+
 # the flow-schedule shift of the paper's backbones (App. B.2)
 SCHEDULE_SHIFT = 5.0
 
@@ -51,6 +57,21 @@ def flow_sigmas(n_steps: int, shift: float = SCHEDULE_SHIFT) -> list[float]:
     out = (C.c_double * (n_steps + 1))()
     _check(lib, None, lib.swam_flow_sigmas(int(n_steps), float(shift), out))
     return list(out)
+
+
+def rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                     trained: float = 0.0) -> tuple[list[float], float]:
+    """The dims / 2 frequencies of a rotation (radians per position) and the factor of the rotated
+    elements, for a context `factor` times longer than the `trained` positions by the rule
+    `scaling`: "plain" (none), "linear", "ntk" or "yarn".  Computed by swam_rope_frequencies in
+    the library (a host call, no GPU needed)."""
+    lib = load_library()
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {list(ROPE_SCALINGS)}, got {scaling!r}")
+    out, m = (C.c_double * max(1, int(dims) // 2))(), C.c_float()
+    _check(lib, None, lib.swam_rope_frequencies(int(dims), float(base), ROPE_SCALINGS[scaling], float(factor),
+                                                float(trained), out, C.byref(m)))
+    return list(out), m.value
 
 
 class SwamError(RuntimeError):
@@ -106,6 +127,19 @@ class LatentIOStruct(C.Structure):
     _fields_ = [("d_latent", C.c_int32)] + [(n, C.c_void_p) for n in LATENT_NAMES]
 
 
+class QkPostStruct(C.Structure):
+    _fields_ = [("norm", C.c_int32), ("eps", C.c_float), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p),
+                ("rope_dims", C.c_int32), ("rope_layout", C.c_int32), ("rope_freq", C.c_void_p),
+                ("rope_magnitude", C.c_float)]
+
+
+class CacheStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v")] + [(n, C.c_int64) for n in (
+        "k_page", "k_token", "k_head", "v_page", "v_token", "v_head", "n_pages")] + [(n, C.c_int32) for n in (
+            "page_size", "n_kv_heads", "head_dim", "n_seqs", "max_pages")] + [
+        ("table_stride", C.c_int64), ("table", C.c_void_p), ("length", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -152,6 +186,12 @@ def load_library(path: str = LIB_PATH):
         "swam_gemm_i8": [P, P, I64, P, P, I64, P, P, P, I64, P, I32, P, I64, I64, I64, I64],
         "swam_cross_attention": [P, P, I64, P, I64, P, I64, P, P, P, P, I32, I32, I64, I64, I32, I32,
                                  I32, F, P, I64, P],
+        "swam_rope_frequencies": [I32, C.c_double, I32, C.c_double, C.c_double, C.POINTER(C.c_double),
+                                  C.POINTER(C.c_float)],
+        "swam_qk_norm_rope": [P, C.POINTER(QkPostStruct), P, P, I64, P, I64, I64, I32, I32, I32, P, I64, P, I64],
+        "swam_cache_append": [P, C.POINTER(CacheStruct), C.POINTER(QkPostStruct), P, P, P, I64, P, I64, P, I64, I64,
+                              I32, P, I64],
+        "swam_cache_attention": [P, C.POINTER(CacheStruct), P, P, I64, I64, I32, I32, I32, F, P, I64, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -256,6 +296,88 @@ class LatentIO:
         self.d_latent = int(weights["w_in"].shape[1])
         self.struct = LatentIOStruct(self.d_latent, *[_ptr(weights[n], act_dtype, name=n)
                                                       for n in LATENT_NAMES])
+
+
+class Rope:
+    """Rotation of the first 2 len(freq) elements of a head by position times freq (float64 GPU
+    tensor, radians per position; rope_frequencies makes them).  layout "interleaved": pairs
+    (2i, 2i + 1), "half": (i, i + len(freq)); magnitude: factor of the rotated elements."""
+
+    def __init__(self, freq: torch.Tensor, layout: str = "interleaved", magnitude: float = 1.0):
+        if layout not in ROPE_LAYOUTS:
+            raise ValueError(f"layout must be one of {list(ROPE_LAYOUTS)}, got {layout!r}")
+        _ptr(freq, torch.float64, name="freq")
+        self.freq, self.layout, self.magnitude = freq, layout, float(magnitude)
+
+
+class QkPost:
+    """What is done to query and key heads: RMS norm (norm, eps, gains [head_dim] in the context's
+    dtype or None) and rotation (rope, or None), with the C descriptor."""
+
+    def __init__(self, norm: bool = True, eps: float = 1e-6, q_gain=None, k_gain=None, rope: Rope | None = None):
+        self.q_gain, self.k_gain, self.rope = q_gain, k_gain, rope
+        held = [t for t in (q_gain, k_gain, None if rope is None else rope.freq) if t is not None]
+        self.devices = {t.get_device() for t in held if isinstance(t, torch.Tensor)}
+        self.act_dtypes = {t.dtype for t in (q_gain, k_gain) if isinstance(t, torch.Tensor)}
+        self.gain_dims = {t.numel() for t in (q_gain, k_gain) if isinstance(t, torch.Tensor)}
+        self.struct = QkPostStruct(int(bool(norm)), float(eps), _ptr(q_gain, name="q_gain"), _ptr(k_gain, name="k_gain"))
+        if rope is not None:
+            self.struct.rope_dims = 2 * rope.freq.numel()
+            self.struct.rope_layout = ROPE_LAYOUTS[rope.layout]
+            self.struct.rope_freq = rope.freq.data_ptr()
+            self.struct.rope_magnitude = rope.magnitude
+
+    def _for(self, act, dim, device):
+        """The descriptor, once its tensors fit the call."""
+        if any(d != device for d in self.devices):
+            raise ValueError(f"post is on GPU {self.devices}, the context on {device}")
+        if any(t is not act for t in self.act_dtypes):
+            raise TypeError(f"gains must be {act}, got {self.act_dtypes}")
+        if any(n != dim for n in self.gain_dims):
+            raise ValueError(f"gains have {self.gain_dims} elements, need {dim}")
+        return C.byref(self.struct)
+
+
+class Cache:
+    """A paged cache with its C descriptor.  k, v [n_pages][page_size][kv_heads][head_dim] in the
+    context's dtype, any strides with contiguous heads; table int32 [n_seqs][max_pages]: the
+    pages of each sequence (outside [0, n_pages): none); length int32 [n_seqs]: tokens before the
+    chunk.  The caller keeps and updates table and length in place."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be a tensor [n_pages][page_size][kv_heads][head_dim]")
+        self.device, self.act_dtype = k.get_device(), k.dtype
+        n_pages, page, self.kv_heads, self.head_dim = k.shape
+        for name, t in (("k", k), ("v", v)):
+            if not isinstance(t, torch.Tensor) or t.dtype is not k.dtype or t.get_device() != self.device or self.device < 0:
+                _refuse(t, k.dtype, name, self.device)
+            if t.shape != k.shape:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {tuple(k.shape)}")
+            if t.numel() and t.stride(3) != 1:
+                raise ValueError(f"{name} must have contiguous heads")
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise ValueError("table must be a tensor [n_seqs][max_pages]")
+        n_seqs, max_pages = table.shape
+        tp, ts = _rows(table, torch.int32, table.shape, "table", self.device)
+        lp = _vec(length, torch.int32, n_seqs, "length", self.device)
+        if length.numel() != n_seqs:
+            raise ValueError(f"length has {length.numel()} elements, needs {n_seqs}")
+        self.k, self.v, self.table, self.length, self.n_seqs = k, v, table, length, n_seqs
+        # (a dimension of one has no second element to reach)
+        ks, vs = ([st if n > 1 else 0 for n, st in zip(t.shape, t.stride())] for t in (k, v))
+        self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), *ks[:3], *vs[:3], n_pages, page, self.kv_heads,
+                                  self.head_dim, n_seqs, max_pages, ts, tp, lp)
+
+    def _for(self, act, device, cu):
+        """The descriptor, once the cache and the offsets fit the call."""
+        if self.act_dtype is not act:
+            raise TypeError(f"the cache must be {act}, got {self.act_dtype}")
+        if self.device != device:
+            raise ValueError(f"the cache is on GPU {self.device}, the context on {device}")
+        if cu is not None and cu.numel() != self.n_seqs + 1:
+            raise ValueError(f"cu has {cu.numel()} elements, needs {self.n_seqs + 1}")
+        return C.byref(self.struct)
 
 
 NOALLOC_SCRATCH_BYTES = 1 << 20   # SWAM_NOALLOC_SCRATCH_BYTES
@@ -596,6 +718,64 @@ class Context:
             self.h, qp, qs, kp, ks, vp, vs, mp, _vec(cu_q, i32, 0, "cu_q", dev), _vec(cu_k, i32, 0, "cu_k", dev),
             _vec(kv_seq, i32, 0, "kv_seq", dev), n_seqs, n_kv, n_q, n_k, heads, kv_heads, dim,
             dim ** -0.5 if scale is None else scale, op, os_, _vec(lse, torch.float32, n_q * heads, "lse", dev))
+        if rc:
+            self._ok(rc)
+
+    # -- streaming block on a paged cache (include/swam_cache.h) -----------------------
+    def qk_norm_rope(self, q, k, post: QkPost, pos=None, q_out=None, k_out=None):
+        """Norm and rotation (post) of the heads of q [rows][heads][head_dim] and k
+        [rows][kv_heads][head_dim] (either may be None), in place or to q_out, k_out.  pos int32
+        [rows]: positions (None: the row's index)."""
+        act, dev = self.act_dtype, self.device
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("q or k required")
+        rows, _, dim = some.shape
+        heads, kv_heads = (0 if t is None else t.shape[1] for t in (q, k))
+        qp, qs = _rows(q, act, (rows, heads, dim), "q", dev)
+        kp, ks = _rows(k, act, (rows, kv_heads, dim), "k", dev)
+        qo, qos = (qp, qs) if q_out is None else _rows(q_out, act, (rows, heads, dim), "q_out", dev)
+        ko, kos = (kp, ks) if k_out is None else _rows(k_out, act, (rows, kv_heads, dim), "k_out", dev)
+        rc = self.lib.swam_qk_norm_rope(self.h, post._for(act, dim, dev), _vec(pos, torch.int32, rows, "pos", dev), qp, qs,
+                                        kp, ks, rows, heads, kv_heads, dim, qo, qos, ko, kos)
+        if rc:
+            self._ok(rc)
+
+    def cache_append(self, cache: Cache, k, v, cu=None, q=None, q_out=None, post: QkPost | None = None, pos=None):
+        """Append a chunk to the cache: k (after norm and rotation, post) and v [rows][kv_heads][head_dim]
+        of token i of sequence s at cache.length[s] + i.  cu int32 [n_seqs + 1]: row offsets of the
+        sequences (None: one sequence); q [rows][heads][head_dim] gets the same norm and rotation, in
+        place or to q_out; pos int32 [rows]: positions of the rotation (None: the token's in its
+        sequence)."""
+        act, dev, dim = self.act_dtype, self.device, cache.head_dim
+        rows = k.shape[0]
+        heads = 0 if q is None else q.shape[1]
+        keys = (rows, cache.kv_heads, dim)
+        kp, ks = _rows(k, act, keys, "k", dev)
+        vp, vs = _rows(v, act, keys, "v", dev)
+        qp, qs = _rows(q, act, (rows, heads, dim), "q", dev)
+        qo, qos = (qp, qs) if q_out is None else _rows(q_out, act, (rows, heads, dim), "q_out", dev)
+        rc = self.lib.swam_cache_append(
+            self.h, cache._for(act, dev, cu), None if post is None else post._for(act, dim, dev),
+            _vec(pos, torch.int32, rows, "pos", dev), _vec(cu, torch.int32, 0, "cu", dev), qp, qs, kp, ks, vp, vs, rows,
+            heads, qo, qos)
+        if rc:
+            self._ok(rc)
+
+    def cache_attention(self, cache: Cache, q, o, cu=None, causal: bool = True, window: int = 0,
+                        scale: float | None = None, lse=None):
+        """o [rows][heads][head_dim] = attention of a chunk's tokens q to everything in the cache, the
+        appended chunk included.  cu as for cache_append; causal: a token sees the chunk up to
+        itself (else all of it); window: keys up to its own that a token sees at most (0: all); scale:
+        1 / sqrt(head_dim) by default; lse float [rows][heads] receives the normalisers."""
+        act, dev, dim = self.act_dtype, self.device, cache.head_dim
+        rows, heads = q.shape[:2]
+        qp, qs = _rows(q, act, (rows, heads, dim), "q", dev)
+        op, os_ = _rows(o, act, (rows, heads, dim), "o", dev)
+        rc = self.lib.swam_cache_attention(
+            self.h, cache._for(act, dev, cu), _vec(cu, torch.int32, 0, "cu", dev), qp, qs, rows, heads,
+            1 if causal else 0, window, dim ** -0.5 if scale is None else scale, op, os_,
+            _vec(lse, torch.float32, rows * heads, "lse", dev))
         if rc:
             self._ok(rc)
 
