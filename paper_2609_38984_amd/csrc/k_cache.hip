@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 namespace swam {
 
@@ -29,10 +30,11 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 struct Split {
   float* o;
   float* ml;
-  int* plan;          // [0]: tiles of a slice, written by workgroup 0 for the joining pass
-  int budget;         // slices beyond the first of every tile, 0: keys are not split
+  int* plan;          // [0]: log2 of a slice's tiles, written by workgroup 0 for the joining pass
+  int budget;         // slices beyond the first of every row tile, 0: keys are not split
   int slot_rows;
 };
+constexpr int NO_SPLIT = 30;                   // log2 of more tiles than any sequence has
 
 // Sequence s as the kernels see it.
 struct Seq {
@@ -41,7 +43,7 @@ struct Seq {
   int qt, nk;         // row tiles, key tiles that a row tile reads at most
 };
 template <int BQ, int BK>
-__device__ __forceinline__ Seq seq_at(const CacheArgs& c, int group, int s) {
+__device__ __forceinline__ Seq seq_at(const CacheArgs& c, int s) {
   Seq q{};
   if (s >= c.pg.n_seqs) return q;
   int e;
@@ -49,42 +51,45 @@ __device__ __forceinline__ Seq seq_at(const CacheArgs& c, int group, int s) {
   q.n = e - q.a;
   q.old = held(c.pg, s);
   q.total = (int)min((int64_t)q.old + q.n, (int64_t)c.pg.max_pages << c.pg.lg_page);
-  q.qt = (q.n * group + BQ - 1) / BQ;
+  q.qt = (q.n * c.group + BQ - 1) / BQ;
   q.nk = (q.total + BK - 1) / BK;
-  // a causal window bounds what a row tile reads: its own tokens and the window before them
-  if (c.window && c.causal) q.nk = min(q.nk, (min(c.window, 1 << 30) + BQ / group + 1) / BK + 2);
+  // a causal window bounds what a row tile reads: its own tokens (BQ + 1 at most) and the
+  // window before them
+  if (c.window && c.causal) q.nk = min(q.nk, (min(c.window, 1 << 30) + BQ + 1) / BK + 2);
   return q;
 }
 
+// inclusive sums over the first `n` lanes
 template <typename T>
-__device__ __forceinline__ T wave_scan(T v) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
+__device__ __forceinline__ T wave_scan(T v, int n) {
+  for (int s = 1; s < n; s <<= 1) {
     const T u = __shfl_up(v, s);
     if ((int)(threadIdx.x & 63) >= s) v += u;
   }
   return v;
 }
 
-// Tiles of a slice, from the key tiles of all row tiles (`all`, over all K/V heads) and the most of
-// one: modelled time of a workgroup by itself (`lone` ns a tile) and of several that
-// share a CU, and of the pass that joins the slices.
+// log2 of the tiles of a slice, from the key tiles of all row tiles (`all`, over all K/V heads) and
+// the most of one: modelled time (us) of a workgroup by itself (`lone` a tile) and of several that
+// share a CU, and of the pass that joins the slices.  all / 2^lg slices beyond the first
+// are within the budget; a row tile of more than 2^lg tiles has fewer than 2 all / 2^lg.
 template <int D>
-__device__ __forceinline__ int slice_tiles(int64_t all, int most, const Split& sp) {
-  if (sp.budget == 0) return max(most, 1);
-  const float lone = D == 64 ? 1.2f : 1.6f, share = (D == 64 ? 0.64f : 1.0f) / 256.0f * (float)all;
-  const int least = max((int)((all + sp.budget - 1) / sp.budget), 2);
-  int best = max(most, 1);
+__device__ __forceinline__ int slice_tiles(float all, int most, const Split& sp) {
+  if (sp.budget == 0) return NO_SPLIT;
+  const float lone = D == 64 ? 1.2f : 1.6f, share = (D == 64 ? 0.64f : 1.0f) / 256.0f * all;
+  const float join = 2.0f * all * (float)sp.slot_rows * (D + 2) * (4.0f / 3.0e6f);
+  int best = NO_SPLIT;
   float best_us = fmaxf(lone * (float)most, share);
-  for (int k = 1; k < 16; ++k) {
-    const int t = (most + (1 << k) - 1) >> k;
-    if (t < least) break;
-    const float us = fmaxf(lone * (float)t, share) + 4.5f +
-                     2.0f * (float)all / (float)t * (float)sp.slot_rows * (D + 2) * (4.0f / 3.0e6f);
-    if (us < best_us) { best_us = us; best = t; }
+#pragma unroll 1
+  for (int lg = 1; (1 << lg) < most; ++lg) {
+    const float t = (float)(1 << lg);
+    if (t * (float)sp.budget < all * 1.0001f + 1.0f) continue;
+    const float us = fmaxf(lone * t, share) + 4.5f + join * __builtin_amdgcn_rcpf(t);
+    if (us < best_us) { best_us = us; best = lg; }
   }
   return best;
 }
+__device__ __forceinline__ int slices(int nk, int lg) { return max((nk + (1 << lg) - 1) >> lg, 1); }
 
 // What a workgroup does: slice y of ch of the keys of row tile qi of sequence s, its
 // partial results in `slot` (units before it in split sequences).
@@ -92,51 +97,54 @@ struct Work {
   Seq q;
   int s, qi, y, ch, slot;
 };
-// The lanes hold the sequences in order, `per` to a lane; three passes over them find the
+// The lanes hold the sequences in order, `per` to a lane; passes over them find the
 // slices' length, the units in front of each, and the one that holds `unit`.
 template <int D, int BQ, int BK>
 __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int unit, Work& w) {
-  const int lane = threadIdx.x & 63, group = c.heads / c.pg.kv_heads;
-  const int per = (c.pg.n_seqs + 63) >> 6;
-  const Seq first = seq_at<BQ, BK>(c, group, lane * per);
-  int64_t all = 0;
-  int most = 0;
-  for (int i = 0; i < per; ++i) {
-    const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, group, lane * per + i);
-    all += (int64_t)q.qt * q.nk;
-    most = max(most, q.nk);
+  const int lane = threadIdx.x & 63;
+  const int per = (c.pg.n_seqs + 63) >> 6, lanes = min(c.pg.n_seqs, 64);
+  const Seq first = seq_at<BQ, BK>(c, lane * per);
+  int lg = NO_SPLIT;
+  if (sp.budget) {
+    float all = (float)first.qt * (float)first.nk;
+    int most = first.nk;
+    for (int i = 1; i < per; ++i) {
+      const Seq q = seq_at<BQ, BK>(c, lane * per + i);
+      all += (float)q.qt * (float)q.nk;
+      most = max(most, q.nk);
+    }
+    for (int o = 1; o < lanes; o <<= 1) {
+      all += __shfl_xor(all, o);
+      most = max(most, __shfl_xor(most, o));
+    }
+    all = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, all)));
+    lg = __builtin_amdgcn_readfirstlane(
+        slice_tiles<D>(all * (float)c.pg.kv_heads, __builtin_amdgcn_readfirstlane(most), sp));
+    if (blockIdx.x == 0 && threadIdx.x == 0) sp.plan[0] = lg;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    all += __shfl_xor(all, o);
-    most = max(most, __shfl_xor(most, o));
-  }
-  const int tiles = slice_tiles<D>(all * c.pg.kv_heads, most, sp);
-  if (blockIdx.x == 0 && threadIdx.x == 0 && sp.budget) sp.plan[0] = tiles < most ? tiles : 0;
   int units = 0, split = 0;
   for (int i = 0; i < per; ++i) {
-    const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, group, lane * per + i);
-    const int ch = max((q.nk + tiles - 1) / tiles, 1);
+    const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, lane * per + i);
+    const int ch = slices(q.nk, lg);
     units += q.qt * ch;
     split += ch > 1 ? q.qt * ch : 0;
   }
-  int at = wave_scan(units), slot = wave_scan(split);
+  int at = wave_scan(units, lanes), slot = sp.budget ? wave_scan(split, lanes) : 0;
   const uint64_t past = __ballot(at > unit);
   if (past == 0) return false;
   at -= units;
   slot -= split;
   w = Work{};
+  int r = 0;
   for (int i = 0; i < per; ++i) {
-    const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, group, lane * per + i);
-    const int ch = max((q.nk + tiles - 1) / tiles, 1), n = q.qt * ch;
+    const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, lane * per + i);
+    const int ch = slices(q.nk, lg), n = q.qt * ch;
     if (unit >= at && unit < at + n) {
       w.q = q;
       w.s = lane * per + i;
       w.ch = ch;
-      // the last rows of a causal chunk see most: they come first
-      w.qi = q.qt - 1 - (unit - at) / ch;
-      w.y = (unit - at) % ch;
       w.slot = slot + unit - at;
+      r = unit - at;
     }
     at += n;
     slot += ch > 1 ? n : 0;
@@ -144,21 +152,58 @@ __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int
   const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
   auto bcast = [&](int& v) { v = __builtin_amdgcn_readlane(v, b); };
   bcast(w.q.a); bcast(w.q.n); bcast(w.q.old); bcast(w.q.total); bcast(w.q.qt); bcast(w.q.nk);
-  bcast(w.s); bcast(w.qi); bcast(w.y); bcast(w.ch); bcast(w.slot);
+  bcast(w.s); bcast(w.ch); bcast(w.slot); bcast(r);
+  // the last rows of a causal chunk see most: they come first
+  const int qi = w.ch == 1 ? r : r / w.ch;
+  w.qi = w.q.qt - 1 - qi;
+  w.y = r - qi * w.ch;
   return true;
 }
 
-// the keys [lo, hi) that rows [r0, r1] of a sequence see, as far as one range holds them
-__device__ __forceinline__ void key_range(const CacheArgs& c, const Seq& q, int group, int r0, int r1, int& lo, int& hi) {
-  hi = c.causal ? min(q.old + r1 / group + 1, q.total) : q.total;
-  lo = c.window ? min(max(q.old + r0 / group - c.window + 1, 0), hi) : 0;
+// Row r of a sequence is head r % group of token r / group: for rows near the tile's first,
+// whose token and remainder are known (x below group + BQ).
+struct Rows {
+  int tok, rem, group;
+  uint32_t magic;                              // ceil(2^32 / group), exact for x (group - 1) < 2^32
+  __device__ __forceinline__ Rows(int r0, const CacheArgs& c) : group(c.group), magic(c.group_magic) {
+    tok = group == 1 ? r0 : r0 / group;
+    rem = r0 - tok * group;
+  }
+  __device__ __forceinline__ int token(int i) const { return tok + (group == 1 ? i : (int)__umulhi(rem + i, magic)); }
+  __device__ __forceinline__ int head(int i) const {
+    return group == 1 ? 0 : rem + i - (int)__umulhi(rem + i, magic) * group;
+  }
+};
+
+// the keys [lo, hi) that tokens [t0, t1] of a sequence see, as far as one range holds them
+__device__ __forceinline__ void key_range(const CacheArgs& c, const Seq& q, int t0, int t1, int& lo, int& hi) {
+  hi = c.causal ? min(q.old + t1 + 1, q.total) : q.total;
+  lo = c.window ? min(max(q.old + t0 - c.window + 1, 0), hi) : 0;
 }
 
 // tiles [t0, t1) of slice y of ch
 __device__ __forceinline__ void slice_of(int lo, int hi, int bk, int y, int ch, int& t0, int& t1) {
   const int a = lo / bk, n = (hi + bk - 1) / bk - a;
-  t0 = a + (int)((int64_t)n * y / ch);
-  t1 = a + (int)((int64_t)n * (y + 1) / ch);
+  if (ch == 1) { t0 = a; t1 = a + n; return; }
+  const int each = n / ch, more = n - each * ch;
+  t0 = a + each * y + min(y, more);
+  t1 = t0 + each + (y < more);
+}
+
+// Values that are not finite (bf16, exponent all ones): a weight of zero does not hide them, so
+// where rows see different keys they are left out of the products and added by hand.
+__device__ __forceinline__ uint4 without_odd(uint4 x) {
+  auto f = [](uint32_t y) {
+    if ((y & 0x7f80u) == 0x7f80u) y &= 0xffff0000u;
+    return (y & 0x7f800000u) == 0x7f800000u ? y & 0xffffu : y;
+  };
+  return make_uint4(f(x.x), f(x.y), f(x.z), f(x.w));
+}
+__device__ __forceinline__ void add_odd(f32x16& o, int q4, bool sees, uint2 x) {
+  const float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u),
+                      __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u)};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[4 * q4 + e] += sees && !(fabsf(f[e]) <= FLT_MAX) ? f[e] : 0.0f;
 }
 
 template <int D>
@@ -168,7 +213,7 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   constexpr int NW = 4, BQ = 32 * NW;
   constexpr int TILE = CA_BK * 8 * H2;           // uint4 of a K or V tile
   __shared__ uint4 kv[2][2][TILE];               // [stage][K | V][half][key][8 chunks]
-  const int group = c.heads / c.pg.kv_heads;
+  const int group = c.group;
   // neighbouring workgroups take the K/V heads in turn: with a multiple of 8 of them a
   // head stays on one XCD
   const int hk = blockIdx.x % c.pg.kv_heads;
@@ -177,32 +222,31 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r31 = lane & 31;
-  const int rows = w.q.n * group, r0 = w.qi * BQ, total = w.q.total;
+  const int r0 = w.qi * BQ, left = w.q.n * group - r0, total = w.q.total;   // rows of the sequence from r0 on
+  const Rows row_of(r0, c);
   int lo, hi, t0, t1;
-  key_range(c, w.q, group, r0, min(r0 + BQ, rows) - 1, lo, hi);
+  key_range(c, w.q, row_of.tok, row_of.token(min(BQ, left) - 1), lo, hi);
   slice_of(lo, hi, CA_BK, w.y, w.ch, t0, t1);
   // the keys that all rows of this wave see lie in [low_last, lim_first], those that any
   // sees in [low_first, lim_last]; a wave behind the last row sees none
-  const int wr = r0 + wave * 32;
-  int lim_first = total - 1, lim_last = wr < rows ? total - 1 : -1, low_first = 0, low_last = 0;
-  const int tok_first = min(wr, rows - 1) / group, tok_last = min(wr + 31, rows - 1) / group;
+  const int wr = wave * 32;
+  int lim_first = total - 1, lim_last = wr < left ? total - 1 : -1, low_first = 0, low_last = 0;
+  const int p_first = w.q.old + row_of.token(min(wr, left - 1)), p_last = w.q.old + row_of.token(min(wr + 31, left - 1));
   if (c.causal) {
-    lim_first = min(lim_first, w.q.old + tok_first);
-    lim_last = min(lim_last, w.q.old + tok_last);
+    lim_first = min(lim_first, p_first);
+    lim_last = min(lim_last, p_last);
   }
   if (c.window) {
-    low_first = max(w.q.old + tok_first - c.window + 1, 0);
-    low_last = max(w.q.old + tok_last - c.window + 1, 0);
+    low_first = max(p_first - c.window + 1, 0);
+    low_last = max(p_last - c.window + 1, 0);
   }
   bf16x8 qf[D / 16];
   int lim = total - 1, low = 0;                  // of this lane's row
   {
-    const int rr = min(wr + r31, rows - 1);
-    const int64_t tok = w.q.a + rr / group;
-    const int head = hk * group + rr % group;
-    if (c.causal) lim = min(lim, w.q.old + rr / group);
-    if (c.window) low = max(w.q.old + rr / group - c.window + 1, 0);
-    const bf16_t* qp = (const bf16_t*)c.q + tok * c.q_ld + head * D;
+    const int i = min(wr + r31, left - 1), tok = row_of.token(i);
+    if (c.causal) lim = min(lim, w.q.old + tok);
+    if (c.window) low = max(w.q.old + tok - c.window + 1, 0);
+    const bf16_t* qp = (const bf16_t*)c.q + (int64_t)(w.q.a + tok) * c.q_ld + (hk * group + row_of.head(i)) * D;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
       qf[s] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 8 * (2 * s + g)));
@@ -218,30 +262,44 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   };
   const int lrow = lane >> 3;
   constexpr int SL = 8 * H2 / NW;                // 8-key slabs of a tile that a wave stages
+  const int slab0 = wave * SL, key0 = (slab0 & 7) * 8, half = slab0 >> 3;
   int off_k[2], off_v[2];                        // of even and odd slabs
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int r = j * 8 + lrow, col = 8 * ((lane & 7) ^ lds_swz(r));
-    off_k[j] = (lrow * (int)c.pg.k_token + col) * 2;
-    off_v[j] = (lrow * (int)c.pg.v_token + col) * 2;
+    off_k[j] = (r * (int)c.pg.k_token + col) * 2;
+    off_v[j] = (r * (int)c.pg.v_token + col) * 2;
   }
-  // K and V of tile t into LDS, `pages` of its keys in the lanes
-  auto issue = [&](uint4 (&to)[2][TILE], int t, int pages) {
+  const bf16_t* k_head = (const bf16_t*)c.pg.k + hk * c.pg.k_head + 64 * half;
+  const bf16_t* v_head = (const bf16_t*)c.pg.v + hk * c.pg.v_head + 64 * half;
+  // K and V of tile t into LDS, `pages` of its keys in the lanes; RUN slabs share a page
+  auto issue_runs = [&](uint4 (&to)[2][TILE], int t, int pages, auto run) {
+    constexpr int RUN = decltype(run)::value;
 #pragma unroll
-    for (int j = 0; j < SL; ++j) {
-      const int slab = wave * SL + j, r = (slab & 7) * 8, half = slab >> 3;
-      const int page = __builtin_amdgcn_readlane(pages, r);
-      const int key = t * CA_BK + r, n = page < 0 ? 0 : min(total - key, 8);
-      const int64_t p = max(page, 0), at = key & ((1 << c.pg.lg_page) - 1);
-      const bf16_t* kb = (const bf16_t*)c.pg.k + p * c.pg.k_page + at * c.pg.k_token + hk * c.pg.k_head + 64 * half;
-      const bf16_t* vb = (const bf16_t*)c.pg.v + p * c.pg.v_page + at * c.pg.v_token + hk * c.pg.v_head + 64 * half;
+    for (int j = 0; j < SL; j += RUN) {
+      const int page = __builtin_amdgcn_readlane(pages, key0 + 8 * j);
+      const int key = t * CA_BK + key0 + 8 * j, n = page < 0 ? 0 : min(total - key, 8 * RUN);
+      const int64_t p = max(page, 0);
+      const int64_t at = key & ((1 << c.pg.lg_page) - 1);
+      const bf16_t* kb = k_head + p * c.pg.k_page + at * c.pg.k_token;
+      const bf16_t* vb = v_head + p * c.pg.v_page + at * c.pg.v_token;
       const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
           (void*)kb, (short)0, n ? ((n - 1) * (int)c.pg.k_token + 64) * 2 : 0, SWAM_BUF_DWORD3);
       const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
           (void*)vb, (short)0, n ? ((n - 1) * (int)c.pg.v_token + 64) * 2 : 0, SWAM_BUF_DWORD3);
-      dma_slab(rk, &to[0][slab * 64], off_k[j & 1]);
-      dma_slab(rv, &to[1][slab * 64], off_v[j & 1]);
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const int slab = slab0 + j + i, e = RUN == 1 ? 8 * ((j + i) & 1) : -16 * (i >> 1);   // (rows that off_* has beyond the slab's)
+        dma_slab(rk, &to[0][slab * 64], off_k[(j + i) & 1] - e * (int)c.pg.k_token * 2);
+        dma_slab(rv, &to[1][slab * 64], off_v[(j + i) & 1] - e * (int)c.pg.v_token * 2);
+      }
     }
+  };
+  auto issue = [&](uint4 (&to)[2][TILE], int t, int pages) {
+    const int run = 1 << c.pg.lg_page >> 3;
+    if (run >= SL) issue_runs(to, t, pages, std::integral_constant<int, SL>{});
+    else if (SL > 2 && run == 2) issue_runs(to, t, pages, std::integral_constant<int, 2>{});
+    else issue_runs(to, t, pages, std::integral_constant<int, 1>{});
   };
   // V^T operand by transposed LDS reads: in each 16-lane group lane a addresses
   // V[key0 + (a >> 2)][col0 + 4 (a & 3)] and lane i receives keys key0..key0+3 of
@@ -272,12 +330,12 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     uint64_t m = h < 0 ? 0 : h >= 63 ? vis : vis & ((2ull << h) - 1);
     return l > 63 ? 0 : l > 0 ? m & (~0ull << l) : m;
   };
-  auto v_operand = [&](const unsigned short* vs, int ht, int t, int u) -> bf16x8 {
+  auto v_operand = [&](const unsigned short* vs, int ht, int t, int u) -> uint4 {
     const int base = (ht >> 1) * CA_BK * 64 + (32 * t + 16 * u) * 64;
     const v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1] + base));
     const v4i16 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[(ht & 1) ^ 1] + 8 * 64 + base));
     const uint2 w1 = __builtin_bit_cast(uint2, x1), w2 = __builtin_bit_cast(uint2, x2);
-    return __builtin_bit_cast(bf16x8, make_uint4(w1.x, w1.y, w2.x, w2.y));
+    return make_uint4(w1.x, w1.y, w2.x, w2.y);
   };
 
   // one tile of keys; `part`: some row sees some of its keys only; `mixed`: of those that
@@ -296,17 +354,18 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
         }
       }
       if (part) {
-        // register r holds key 8 (r >> 2) + 4 g + (r & 3) of its half
+        // register r holds key 8 (r >> 2) + 4 g + (r & 3) of its half.  (A branch: no tile
+        // but the first and last of a row needs these)
         const uint64_t m = seen(at, vis) >> (4 * g);
+        uint32_t bits[2] = {(uint32_t)m, (uint32_t)(m >> 32)};
+        asm volatile("" : "+v"(bits[0]), "+v"(bits[1]));
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint32_t bits = (uint32_t)(m >> (32 * t));
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (r >> 2) + (r & 3), 1);
+            const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits[t], 8 * (r >> 2) + (r & 3), 1);
             st[t][r] = __uint_as_float((__float_as_uint(st[t][r]) & keep) | (0xff800000u & ~keep));
           }
-        }
       }
     };
     bf16x8 pf[2][2];
@@ -371,41 +430,33 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
       odd = __any(top[0] >= 0x7f80 || top[1] >= 0x7f80);
     }
     if (odd) {
-      // key by key: every product keeps one, and only the rows that see it take it
+      // such values are left out of the products, and the rows that see them add them
       const uint64_t m = seen(at, vis);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
 #pragma unroll 1
-          for (int key = 0; key < 16; ++key) {
-            const int e = 4 * (key >> 3) + (key & 3);
-            const bool mine = ((key >> 2) & 1) == g, sees = (m >> (32 * t + 16 * u + key)) & 1;
-            uint32_t keep[4];
+      for (int key = 0; key < CA_BK; ++key) {
+        const bool sees = (m >> key) & 1;
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
-              keep[d] = mine && (e >> 1) == d ? ((e & 1) ? 0xffff0000u : 0xffffu) : 0u;
-            auto only = [&](bf16x8 x) -> bf16x8 {
-              const uint4 y = __builtin_bit_cast(uint4, x);
-              return __builtin_bit_cast(bf16x8, make_uint4(y.x & keep[0], y.y & keep[1], y.z & keep[2], y.w & keep[3]));
-            };
-            const bf16x8 pk = only(pf[t][u]);
+        for (int ht = 0; ht < D / 32; ++ht)
 #pragma unroll
-            for (int ht = 0; ht < D / 32; ++ht) {
-              const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(only(v_operand(vs, ht, t, u)), pk, o[ht], 0, 0, 0);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) o[ht][r] = sees ? x[r] : o[ht][r];
-            }
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const int chunk = (4 * (ht & 1) + q4) ^ lds_swz(key);
+            add_odd(o[ht], q4, sees, *reinterpret_cast<const uint2*>(vs + (ht >> 1) * CA_BK * 64 + key * 64 + 8 * chunk + 4 * g));
           }
-      return;
+      }
     }
+    auto products = [&](auto clean) {
 #pragma unroll
-    for (int ht = 0; ht < D / 32; ++ht)
+      for (int ht = 0; ht < D / 32; ++ht)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          o[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vs, ht, t, u), pf[t][u], o[ht], 0, 0, 0);
+          for (int u = 0; u < 2; ++u) {
+            const uint4 x = clean(v_operand(vs, ht, t, u));
+            o[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf[t][u], o[ht], 0, 0, 0);
+          }
+    };
+    if (odd) products([](uint4 x) { return without_odd(x); });
+    else products([](uint4 x) { return x; });
   };
 
   // All waves form the same mask words: that of the tile at hand, of the next, whose loads
@@ -435,11 +486,11 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   const float l = l_run + __shfl_xor(l_run, 32);
   int me = tid;
   asm volatile("" : "+v"(me));
-  const int in_tile = (me >> 6) * 32 + (me & 31), want = r0 + in_tile, rr = min(want, rows - 1);
-  const int64_t tok = w.q.a + rr / group;
-  const int head = hk * group + rr % group;
+  const int in_tile = (me >> 6) * 32 + (me & 31), have = min(in_tile, left - 1);
+  const int64_t tok = w.q.a + row_of.token(have);
+  const int head = hk * group + row_of.head(have);
   if (w.ch > 1) {
-    if (want >= rows) return;
+    if (in_tile >= left) return;
     const int64_t row = ((int64_t)w.slot * c.pg.kv_heads + hk) * sp.slot_rows + in_tile;
     float* po = sp.o + row * D;
 #pragma unroll
@@ -469,9 +520,9 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
         v[e] = pack_bf16x2(o[ht][4 * q4 + 2 * e] * inv, o[ht][4 * q4 + 2 * e + 1] * inv);
       const auto x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
       const auto y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-      if (want < rows) *(uint4*)(op + 32 * ht + 8 * (q4 + g)) = make_uint4(x[0], y[0], x[1], y[1]);
+      if (in_tile < left) *(uint4*)(op + 32 * ht + 8 * (q4 + g)) = make_uint4(x[0], y[0], x[1], y[1]);
     }
-  if (want >= rows) return;
+  if (in_tile >= left) return;
   if (c.lse != nullptr && g == 0) c.lse[tok * c.heads + head] = l == 0.0f ? -INFINITY : (m_run + log2f(l)) * LN2;
 }
 
@@ -483,29 +534,30 @@ cache_f32(const CacheArgs c, const Split sp, int unit0) {
   constexpr int LD = D + 4, BQ = 32, BK = 32;
   __shared__ float os[4][32][LD];
   __shared__ float ms[4][32], ls[4][32];
-  const int group = c.heads / c.pg.kv_heads;
+  const int group = c.group;
   const int hk = blockIdx.x % c.pg.kv_heads;
   Work w;
   if (!work_at<D, BQ, BK>(c, sp, unit0 + blockIdx.x / c.pg.kv_heads, w)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, r31 = lane & 31;
-  const int rows = w.q.n * group, r0 = w.qi * BQ, total = w.q.total;
-  const int rl = min(r0 + BQ, rows) - 1;         // the tile's last row
+  const int r0 = w.qi * BQ, left = min(w.q.n * group - r0, BQ), total = w.q.total;   // rows of the tile
+  const Rows row_of(r0, c);
+  const int t_last = row_of.token(left - 1);
   int lo, hi, t0, t1;
-  key_range(c, w.q, group, r0, rl, lo, hi);
+  key_range(c, w.q, row_of.tok, t_last, lo, hi);
   slice_of(lo, hi, BK, w.y, w.ch, t0, t1);
-  const int rr = min(r0 + r31, rl);
+  const int mine_row = min(r31, left - 1), my_tok = row_of.token(mine_row);
   int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
   if (c.causal) {
-    lim = min(lim, w.q.old + rr / group);
-    lim_first = min(lim_first, w.q.old + r0 / group);
+    lim = min(lim, w.q.old + my_tok);
+    lim_first = min(lim_first, w.q.old + row_of.tok);
   }
   if (c.window) {
-    low = max(w.q.old + rr / group - c.window + 1, 0);
-    low_last = max(w.q.old + rl / group - c.window + 1, 0);
+    low = max(w.q.old + my_tok - c.window + 1, 0);
+    low_last = max(w.q.old + t_last - c.window + 1, 0);
   }
   f32x4 qf[D / 8];
   {
-    const float* qp = (const float*)c.q + (int64_t)(w.q.a + rr / group) * c.q_ld + (hk * group + rr % group) * D;
+    const float* qp = (const float*)c.q + (int64_t)(w.q.a + my_tok) * c.q_ld + (hk * group + row_of.head(mine_row)) * D;
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 4 * (2 * s + g));
   }
@@ -577,28 +629,33 @@ cache_f32(const CacheArgs c, const Split sp, int unit0) {
           odd |= ((any >> (8 * (r >> 2) + (r & 3))) & 1u) && !(fabsf(vf[h][r]) <= FLT_MAX);
       odd = __any(odd);
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int b = 8 * (r >> 2) + (r & 3);
-      const bool see = (any >> b) & 1u;
-      const float p = exp2f(st[r] - m_new);
-      l += p;
-      if (!odd) {
+    if (odd) {
+      // such values are left out of the products, and the rows that see them add them
+#pragma unroll 1
+      for (int kr = 0; kr < BK; ++kr) {
+        const float* vp = (const float*)c.pg.v + __shfl(page, kr) * c.pg.v_page + ((kb + kr) & slot_mask) * c.pg.v_token +
+                          hk * c.pg.v_head;
+        const bool sees = (row_sees >> kr) & 1u;
 #pragma unroll
         for (int h = 0; h < D / 32; ++h)
-          o[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(see ? vf[h][r] : 0.0f, p, o[h], 0, 0, 0);
-        continue;
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(vp + 32 * h + 8 * q4 + 4 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              o[h][4 * q4 + e] += sees && !(fabsf(x[e]) <= FLT_MAX) ? x[e] : 0.0f;
+          }
       }
+    }
 #pragma unroll
-      for (int gg = 0; gg < 2; ++gg) {
-        const bool sees = (row_sees >> (b + 4 * gg)) & 1u;
+    for (int r = 0; r < 16; ++r) {
+      const bool see = (any >> (8 * (r >> 2) + (r & 3))) & 1u;
+      const float p = exp2f(st[r] - m_new);
+      l += p;
 #pragma unroll
-        for (int h = 0; h < D / 32; ++h) {
-          const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x2f32(g == gg ? vf[h][r] : 0.0f, g == gg ? p : 0.0f, o[h], 0, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[h][e] = sees ? x[e] : o[h][e];
-        }
-      }
+      for (int h = 0; h < D / 32; ++h)
+        o[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(see && !(odd && !(fabsf(vf[h][r]) <= FLT_MAX)) ? vf[h][r] : 0.0f, p,
+                                                    o[h], 0, 0, 0);
     }
   }
   l += __shfl_xor(l, 32);
@@ -611,9 +668,9 @@ cache_f32(const CacheArgs c, const Split sp, int unit0) {
           make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
   __syncthreads();
   const int q = tid >> 3;
-  if (r0 + q > rl) return;
-  const int64_t tok = w.q.a + (r0 + q) / group;
-  const int head = hk * group + (r0 + q) % group;
+  if (q >= left) return;
+  const int64_t tok = w.q.a + row_of.token(q);
+  const int head = hk * group + row_of.head(q);
   const float mt = fmaxf(fmaxf(ms[0][q], ms[1][q]), fmaxf(ms[2][q], ms[3][q]));
   float f[4], lt = 0.0f;
 #pragma unroll
@@ -648,61 +705,586 @@ cache_f32(const CacheArgs c, const Split sp, int unit0) {
   }
 }
 
-// One wave per token and head of a split sequence adds up its slices, in their order.
+// One wave per token and head of a split sequence adds up its slices, in a fixed order:
+// D / 4 lanes hold a slice's row, so a wave reads several at once and eight such loads are
+// in flight.
 template <typename T, int D, int BQ, int BK>
 __global__ void __launch_bounds__(256)
 cache_join(const CacheArgs c, const Split sp) {
-  const int tiles = sp.plan[0];
-  if (tiles == 0) return;                       // nothing was split
-  const int lane = threadIdx.x & 63, kvh = c.pg.kv_heads, group = c.heads / kvh;
-  const int64_t n = (int64_t)c.n_q * c.heads;
+  constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8;
+  const int lg = sp.plan[0];
+  if (lg == NO_SPLIT) return;                   // nothing was split
+  const int lane = threadIdx.x & 63, kvh = c.pg.kv_heads;
+  const int set = lane / PER, col = lane % PER * 4;
   const int per = (c.pg.n_seqs + 63) >> 6;
-  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < n; id += (int64_t)gridDim.x * 4) {
-    const int tok = (int)(id / c.heads), head = (int)(id % c.heads);
+  const int n = c.n_q * c.heads;               // (below 2^30)
+  const int64_t pitch = (int64_t)kvh * sp.slot_rows;
+  for (int id = blockIdx.x * 4 + (threadIdx.x >> 6); id < n; id += gridDim.x * 4) {
+    const int tok = id / c.heads, head = id % c.heads;
     const int s = seq_of(c.pg, tok);
-    const Seq q = seq_at<BQ, BK>(c, group, s);
-    const int ch = max((q.nk + tiles - 1) / tiles, 1);
+    const Seq q = seq_at<BQ, BK>(c, s);
+    const int ch = slices(q.nk, lg);
     if (tok < q.a || tok >= q.a + q.n || ch == 1) continue;
     // units of the split sequences in front of it
     int units = 0;
     for (int i = 0; i < per; ++i) {
       const int b = lane * per + i;
       if (b >= s) break;
-      const Seq f = seq_at<BQ, BK>(c, group, b);
-      const int fc = max((f.nk + tiles - 1) / tiles, 1);
+      const Seq f = seq_at<BQ, BK>(c, b);
+      const int fc = slices(f.nk, lg);
       units += fc > 1 ? f.qt * fc : 0;
     }
+    if (s > 0) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) units += __shfl_xor(units, o);
-    const int r = (tok - q.a) * group + head % group, qi = r / BQ;
+      for (int o = 32; o > 0; o >>= 1) units += __shfl_xor(units, o);
+    }
+    const int r = (tok - q.a) * c.group + head % c.group, qi = r / BQ;
     // (the workgroups count the row tiles from the last)
-    const int64_t slot = ((int64_t)(units + (q.qt - 1 - qi) * ch) * kvh + head / group) * sp.slot_rows + r % BQ;
-    const int64_t pitch = (int64_t)kvh * sp.slot_rows;
-    float m = -FLT_MAX;
+    const int64_t slot = ((int64_t)(units + (q.qt - 1 - qi) * ch) * kvh + head / c.group) * sp.slot_rows + r % BQ;
+    float m = -FLT_MAX, l = 0.0f;
     for (int y = lane; y < ch; y += 64) m = fmaxf(m, sp.ml[(slot + y * pitch) * 2]);
     m = warp_max(m);
-    float l = 0.0f, acc[D / 64];
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int y0 = 0; y0 < ch; y0 += SETS * AHEAD) {
+      float4 v[AHEAD];
+      float2 w[AHEAD];
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) acc[e] = 0.0f;
-    for (int y = 0; y < ch; ++y) {
-      const float f = exp2f(sp.ml[(slot + y * pitch) * 2] - m);
-      l = fmaf(sp.ml[(slot + y * pitch) * 2 + 1], f, l);
+      for (int a = 0; a < AHEAD; ++a) {
+        const int64_t at = slot + min(y0 + SETS * a + set, ch - 1) * pitch;
+        w[a] = *reinterpret_cast<const float2*>(sp.ml + at * 2);
+        v[a] = *reinterpret_cast<const float4*>(sp.o + at * D + col);
+      }
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(sp.o[(slot + y * pitch) * D + 64 * e + lane], f, acc[e]);
+      for (int a = 0; a < AHEAD; ++a) {
+        if (y0 + SETS * a + set < ch) {
+          const float f = exp2f(w[a].x - m);
+          l = fmaf(w[a].y, f, l);
+          acc[0] = fmaf(v[a].x, f, acc[0]);
+          acc[1] = fmaf(v[a].y, f, acc[1]);
+          acc[2] = fmaf(v[a].z, f, acc[2]);
+          acc[3] = fmaf(v[a].w, f, acc[3]);
+        }
+      }
+    }
+#pragma unroll
+    for (int o = PER; o < 64; o <<= 1) {
+      l += __shfl_xor(l, o);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (set == 0) {
+      T* op = (T*)c.o + tok * c.o_ld + head * D + col;
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+      else
+        *reinterpret_cast<float4*>(op) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      if (c.lse != nullptr && lane == 0) c.lse[id] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// few rows: single tokens, short chunks
+// ---------------------------------------------------------------------------
+// Here K and V are read once and their bytes are the time.  A workgroup is one wave with a ring
+// of its own in LDS: nothing waits for another wave, and a tile of 16 KB is always in
+// flight.  All key tiles of all (sequence, row tile, K/V head) segments stand in one line that is
+// cut evenly over the waves, so unequal lengths cost nothing; a segment cut by a border
+// leaves partial results, at most two to a wave.
+struct Few {
+  float* o;           // [2 waves][slot_rows][head_dim] sums
+  float* ml;          // [2 waves][slot_rows] (maximum, sum)
+  int waves;          // of the launch
+  int cut;            // waves that tiles may be cut over, 0: segments stay whole
+  int slot_rows;
+};
+constexpr int FEW_BQ = 32, FEW_STAGES = 2;
+template <int D> constexpr int FEW_BK = D == 64 ? 64 : 32;     // 16 KB of K and V either way
+
+// The line of tiles (or of whole segments) as the lanes hold it, `per` sequences to a lane.
+struct Line {
+  int per, mine, upto;                         // this lane's units, and all up to its last
+  int all;                                     // units
+  int waves;                                   // that share them
+  bool cut;                                    // units are tiles
+  __device__ __forceinline__ static int count(const Seq& q, int kvh, bool cut) {
+    return q.qt * kvh * (cut ? q.nk : 1);
+  }
+  // the units [begin(w), begin(w + 1)) are wave w's
+  __device__ __forceinline__ int begin(int w) const {
+    const int each = all / waves;
+    return w * each + min(w, all - each * waves);
+  }
+  // the wave of unit x
+  __device__ __forceinline__ int wave_of(int x) const {
+    const int each = all / waves, more = all - each * waves;
+    return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each;
+  }
+};
+template <int D>
+__device__ __forceinline__ Line line_of(const CacheArgs& c, const Few& f) {
+  constexpr int BK = FEW_BK<D>;
+  const int lane = threadIdx.x & 63, lanes = min(c.pg.n_seqs, 64), kvh = c.pg.kv_heads;
+  Line l;
+  l.per = (c.pg.n_seqs + 63) >> 6;
+  int tiles = 0, segs = 0, most = 0;
+  for (int i = 0; i < l.per; ++i) {
+    const Seq q = seq_at<FEW_BQ, BK>(c, lane * l.per + i);
+    tiles += Line::count(q, kvh, true);
+    segs += Line::count(q, kvh, false);
+    most = max(most, q.nk);
+  }
+  const int tiles_upto = wave_scan(tiles, lanes), segs_upto = wave_scan(segs, lanes);
+  for (int o = 1; o < lanes; o <<= 1) most = max(most, __shfl_xor(most, o));
+  const int n_tiles = __builtin_amdgcn_readlane(tiles_upto, lanes - 1);
+  const int n_segs = __builtin_amdgcn_readlane(segs_upto, lanes - 1);
+  most = __builtin_amdgcn_readfirstlane(most);
+  // cut where that saves the time of more tiles than the joining pass takes
+  const int cut_waves = min(f.cut, (n_tiles + 3) / 4);
+  l.cut = false;
+  if (cut_waves > 0) {
+    const int whole = (n_segs + f.waves - 1) / f.waves * most, each = (n_tiles + cut_waves - 1) / cut_waves;
+    l.cut = whole > each + 8;
+  }
+  l.mine = l.cut ? tiles : segs;
+  l.upto = l.cut ? tiles_upto : segs_upto;
+  l.all = l.cut ? n_tiles : n_segs;
+  l.waves = l.cut ? cut_waves : min(f.waves, max(n_segs, 1));
+  return l;
+}
+
+// RUN: 8-key slabs that share a page for certain
+template <int D, int RUN>
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 8)))
+cache_few(const CacheArgs c, const Few f) {
+  constexpr int H2 = D / 64, BK = FEW_BK<D>, KT = BK / 32, SLABS = BK / 8;
+  constexpr int TILE = BK * 8 * H2;              // uint4 of a K or V tile
+  constexpr int NI = 2 * SLABS * H2;             // loads of a stage
+  __shared__ uint4 kv[FEW_STAGES][2][TILE];      // [stage][K | V][half][key][8 chunks]
+  const int lane = threadIdx.x, g = lane >> 5, r31 = lane & 31, kvh = c.pg.kv_heads;
+  const Line line = line_of<D>(c, f);
+  const int wid = blockIdx.x;
+  if (wid >= line.waves) return;
+  const int first = line.begin(wid), end = line.begin(wid + 1);
+
+  const int lrow = lane >> 3;
+  int off_k[2], off_v[2];                        // of even and odd 8-key slabs
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e)
-      Elem<T>::store((T*)c.o + tok * c.o_ld + head * D + 64 * e + lane, acc[e] * inv);
-    if (c.lse != nullptr && lane == 0) c.lse[id] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
+  for (int j = 0; j < 2; ++j) {
+    const int col = 8 * ((lane & 7) ^ lds_swz(j * 8 + lrow));
+    off_k[j] = (lrow * (int)c.pg.k_token + col) * 2;
+    off_v[j] = (lrow * (int)c.pg.v_token + col) * 2;
+  }
+  // (operand layouts as in the kernel above)
+  const int a16 = lane & 15, G = lane >> 4, rlo = 4 * g + (a16 >> 2);
+  int vofs[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int hd = 32 * x + 16 * (G & 1) + 4 * (a16 & 3);
+    vofs[x] = rlo * 64 + 8 * ((hd >> 3) ^ lds_swz(rlo)) + (hd & 7);
+  }
+  int kofs[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) kofs[s] = r31 * 8 + ((2 * s + g) ^ lds_swz(r31));
+  const float sc = LOG2E * c.scale;
+
+  for (int unit = first; unit < end;) {
+    // the segment of this unit
+    const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(line.upto > unit)) - 1);
+    int at = __builtin_amdgcn_readlane(line.upto, b) - __builtin_amdgcn_readlane(line.mine, b), seq = b * line.per;
+    Seq q = seq_at<FEW_BQ, BK>(c, seq);
+    for (int n = Line::count(q, kvh, line.cut); unit >= at + n; n = Line::count(q, kvh, line.cut)) {
+      at += n;
+      q = seq_at<FEW_BQ, BK>(c, ++seq);
+    }
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    q.a = __builtin_amdgcn_readfirstlane(q.a);
+    q.n = __builtin_amdgcn_readfirstlane(q.n);
+    q.old = __builtin_amdgcn_readfirstlane(q.old);
+    q.total = __builtin_amdgcn_readfirstlane(q.total);
+    q.nk = __builtin_amdgcn_readfirstlane(q.nk);
+    const int rel = __builtin_amdgcn_readfirstlane(unit - at);
+    const int seg = line.cut ? rel / q.nk : rel, from = line.cut ? rel - seg * q.nk : 0;
+    const int upto = line.cut ? min(q.nk, from + end - unit) : q.nk;
+    const bool whole = from == 0 && upto == q.nk;
+    const int qi = seg / kvh, hk = seg - qi * kvh;
+    // the segment starts this wave's units, or ends them behind others
+    const int slot = 2 * wid + (unit != first);
+    unit += line.cut ? upto - from : 1;
+
+    const int r0 = qi * FEW_BQ, left = min(q.n * c.group - r0, FEW_BQ), total = q.total;
+    const Rows row_of(r0, c);
+    const int t_last = row_of.token(left - 1);
+    int lo, hi;
+    key_range(c, q, row_of.tok, t_last, lo, hi);
+    const int base = lo / BK, t0 = base + from, t1 = min(base + upto, (hi + BK - 1) / BK);
+    const int mine = min(r31, left - 1), my_tok = row_of.token(mine);
+    int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
+    if (c.causal) {
+      lim = min(lim, q.old + my_tok);
+      lim_first = min(lim_first, q.old + row_of.tok);
+    }
+    if (c.window) {
+      low = max(q.old + my_tok - c.window + 1, 0);
+      low_last = max(q.old + t_last - c.window + 1, 0);
+    }
+    const_i32* table = (const_i32*)(c.pg.table + seq * c.pg.table_ld);
+    const bf16_t* k_head = (const bf16_t*)c.pg.k + hk * c.pg.k_head;
+    const bf16_t* v_head = (const bf16_t*)c.pg.v + hk * c.pg.v_head;
+
+    // the pages of the runs of tile t, -1: none
+    auto pages_of = [&](int t, int (&pages)[SLABS / RUN]) {
+#pragma unroll
+      for (int j = 0; j < SLABS / RUN; ++j) {
+        const int key = t * BK + 8 * RUN * j;
+        const int p = key < total && t < t1 ? table[key >> c.pg.lg_page] : -1;
+        pages[j] = p < c.pg.n_pages ? p : -1;
+      }
+    };
+    auto keys_of = [&](int t, const int (&pages)[SLABS / RUN]) -> uint64_t {
+      uint64_t m = 0;
+#pragma unroll
+      for (int j = 0; j < SLABS / RUN; ++j)
+        m |= pages[j] >= 0 ? (~0ull >> (64 - 8 * RUN)) << (8 * RUN * j) : 0ull;
+      const int n = total - t * BK;
+      return n >= BK ? m : n <= 0 ? 0ull : m & ((1ull << n) - 1);
+    };
+    // (always as many loads: what has no page stores zeros)
+    auto issue = [&](int stage, int t, const int (&pages)[SLABS / RUN]) {
+#pragma unroll
+      for (int j = 0; j < SLABS / RUN; ++j) {
+        const int key = t * BK + 8 * RUN * j, n = pages[j] < 0 ? 0 : min(total - key, 8 * RUN);
+        const int64_t p = max(pages[j], 0), slot = key & ((1 << c.pg.lg_page) - 1);
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(k_head + p * c.pg.k_page + slot * c.pg.k_token), (short)0, n ? ((n - 1) * (int)c.pg.k_token + D) * 2 : 0,
+            SWAM_BUF_DWORD3);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(v_head + p * c.pg.v_page + slot * c.pg.v_token), (short)0, n ? ((n - 1) * (int)c.pg.v_token + D) * 2 : 0,
+            SWAM_BUF_DWORD3);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i)
+#pragma unroll
+          for (int h = 0; h < H2; ++h) {
+            const int slab = j * RUN + i;
+            dma_slab(rk, &kv[stage][0][(h * SLABS + slab) * 64], vadd_sgpr(off_k[slab & 1], 128 * h + 16 * i * (int)c.pg.k_token));
+            dma_slab(rv, &kv[stage][1][(h * SLABS + slab) * 64], vadd_sgpr(off_v[slab & 1], 128 * h + 16 * i * (int)c.pg.v_token));
+          }
+      }
+    };
+
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+    float m_run = -FLT_MAX, l_run = 0.0f;
+
+    int pages[SLABS / RUN];
+    pages_of(t0, pages);
+    uint64_t keys = keys_of(t0, pages), ahead;   // of the tile at hand and the next
+    issue(0, t0, pages);
+    pages_of(t0 + 1, pages);
+    bf16x8 qf[D / 16];
+    {
+      const bf16_t* qp = (const bf16_t*)c.q + (int64_t)(q.a + my_tok) * c.q_ld + (hk * c.group + row_of.head(mine)) * D;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s)
+        qf[s] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 8 * (2 * s + g)));
+    }
+    int buf = 0;
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t, keys = ahead, buf ^= 1) {
+        ahead = keys_of(t + 1, pages);
+        issue(buf ^ 1, t + 1, pages);
+        pages_of(t + 2, pages);
+        wait_stage<NI>();
+        if (keys == 0) continue;
+        const uint4* Kt = kv[buf][0];
+        const unsigned short* vs = reinterpret_cast<const unsigned short*>(kv[buf][1]);
+        f32x16 st[KT];
+#pragma unroll
+        for (int x = 0; x < KT; ++x) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) st[x][r] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s) {
+            const bf16x8 kf = __builtin_bit_cast(bf16x8, Kt[(s >> 2) * BK * 8 + kofs[s & 3] + x * 32 * 8]);
+            st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[x], 0, 0, 0);
+          }
+        }
+        const int k0 = t * BK, h = lim - k0, u = low - k0;
+        constexpr uint64_t ALL = ~0ull >> (64 - BK);
+        uint64_t sees = h < 0 ? 0 : h >= BK - 1 ? keys : keys & ((2ull << h) - 1);
+        sees = u >= BK ? 0 : u > 0 ? sees & (~0ull << u) : sees;
+        if (__any(sees != ALL)) {
+          const uint64_t m = sees >> (4 * g);
+          uint32_t bits[2] = {(uint32_t)m, (uint32_t)(m >> 32)};
+          asm volatile("" : "+v"(bits[0]), "+v"(bits[1]));
+#pragma unroll
+          for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits[x], 8 * (r >> 2) + (r & 3), 1);
+              st[x][r] = __uint_as_float((__float_as_uint(st[x][r]) & keep) | (0xff800000u & ~keep));
+            }
+        }
+        float mx = st[0][0];
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[x][r]);
+        // the running maximum moves only when some weight would pass 2^8
+        if (__any(mx * sc > m_run + 8.0f)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          const float m_new = fmaxf(m_run, mx * sc), corr = __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          l_run *= corr;
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[x][r] *= corr;
+        }
+        bf16x8 pf[KT][2];
+        float ps0 = 0.0f, ps1 = 0.0f;
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(st[x][r], sc, -m_run));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(st[x][r + 1], sc, -m_run));
+            ps0 += p0; ps1 += p1;
+            pf[x][r >> 3][r & 7] = (__bf16)p0; pf[x][r >> 3][(r & 7) + 1] = (__bf16)p1;
+          }
+        l_run += ps0 + ps1;
+        bool odd = false;
+        if ((k0 + BK - 1 > lim_first && lim_first < total - 1) || k0 < low_last) {
+          u16x2 top = {0, 0};
+#pragma unroll
+          for (int i = 0; i < TILE / 64; ++i) {
+            const uint4 x = kv[buf][1][i * 64 + lane];
+            const uint32_t x4[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x4[e] & 0x7fff7fffu));
+          }
+          odd = __any(top[0] >= 0x7f80 || top[1] >= 0x7f80);
+        }
+        if (odd) {
+#pragma unroll 1
+          for (int key = 0; key < BK; ++key) {
+            const bool see = (sees >> key) & 1u;
+#pragma unroll
+            for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+              for (int q4 = 0; q4 < 4; ++q4) {
+                const int chunk = (4 * (ht & 1) + q4) ^ lds_swz(key);
+                add_odd(o[ht], q4, see, *reinterpret_cast<const uint2*>(vs + (ht >> 1) * BK * 64 + key * 64 + 8 * chunk + 4 * g));
+              }
+          }
+        }
+        auto products = [&](auto clean) {
+#pragma unroll
+          for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+            for (int x = 0; x < KT; ++x)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const int at = (ht >> 1) * BK * 64 + (32 * x + 16 * u) * 64;
+                const v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[ht & 1] + at));
+                const v4i16 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + vofs[(ht & 1) ^ 1] + 8 * 64 + at));
+                const uint2 w1 = __builtin_bit_cast(uint2, x1), w2 = __builtin_bit_cast(uint2, x2);
+                const uint4 vf = clean(make_uint4(w1.x, w1.y, w2.x, w2.y));
+                o[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf[x][u], o[ht], 0, 0, 0);
+              }
+        };
+        // (head_dim 128: the reads of V stay behind the softmax, or 256 registers do not hold them)
+        if constexpr (D == 128) asm volatile("" ::: "memory");
+        if (odd) products([](uint4 x) { return without_odd(x); });
+        else products([](uint4 x) { return x; });
+    }
+    wait_stage<0>();                             // (the ring is free again)
+    const float l = l_run + __shfl_xor(l_run, 32);
+    const int64_t tok = q.a + my_tok;
+    const int head = hk * c.group + row_of.head(mine);
+    if (!whole) {
+      if (r31 < left) {
+        const int64_t row = (int64_t)slot * f.slot_rows + r31;
+        float* po = f.o + row * D;
+#pragma unroll
+        for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4)
+            *reinterpret_cast<float4*>(po + 32 * ht + 8 * q4 + 4 * g) =
+                make_float4(o[ht][4 * q4], o[ht][4 * q4 + 1], o[ht][4 * q4 + 2], o[ht][4 * q4 + 3]);
+        if (g == 0) *reinterpret_cast<float2*>(f.ml + row * 2) = make_float2(m_run, l);
+      }
+      continue;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    bf16_t* op = (bf16_t*)c.o + tok * c.o_ld + head * D;
+#pragma unroll
+    for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; q4 += 2) {
+        uint32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = pack_bf16x2(o[ht][4 * q4 + 2 * e] * inv, o[ht][4 * q4 + 2 * e + 1] * inv);
+        const auto x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+        if (r31 < left) *(uint4*)(op + 32 * ht + 8 * (q4 + g)) = make_uint4(x[0], y[0], x[1], y[1]);
+      }
+    if (c.lse != nullptr && g == 0 && r31 < left)
+      c.lse[tok * c.heads + head] = l == 0.0f ? -INFINITY : (m_run + log2f(l)) * LN2;
+  }
+}
+
+// One workgroup of NW waves per token and head adds up what the waves left of a segment that
+// was cut, in a fixed order: each of its waves every NW-th group of them.
+template <int D, int NW>
+__global__ void __launch_bounds__(64 * NW)
+cache_few_join(const CacheArgs c, const Few f) {
+  constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8, BK = FEW_BK<D>;
+  __shared__ float4 os[NW][PER];
+  __shared__ float2 mls[NW];
+  const Line line = line_of<D>(c, f);
+  if (!line.cut) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kvh = c.pg.kv_heads;
+  const int set = lane / PER, col = lane % PER * 4;
+  const int n = c.n_q * c.heads;
+  for (int id = blockIdx.x; id < n; id += gridDim.x) {
+    const int tok = id / c.heads, head = id % c.heads;
+    const int s = seq_of(c.pg, tok);
+    const Seq q = seq_at<FEW_BQ, BK>(c, s);
+    if (tok < q.a || tok >= q.a + q.n || q.nk == 0) continue;
+    // tiles in front of the sequence
+    int before = __shfl(line.upto, s / line.per) - __shfl(line.mine, s / line.per);
+    for (int i = s / line.per * line.per; i < s; ++i) before += Line::count(seq_at<FEW_BQ, BK>(c, i), kvh, true);
+    const int r = (tok - q.a) * c.group + head % c.group, qi = r / FEW_BQ;
+    const int a = before + (qi * kvh + head / c.group) * q.nk;
+    const int w0 = line.wave_of(a), ch = line.wave_of(a + q.nk - 1) - w0 + 1;
+    if (ch == 1) continue;
+    // the first wave's may be the end of its units, the others' start theirs
+    const int begins = line.begin(w0) == a;
+    auto row_at = [&](int y) -> int64_t {
+      return (int64_t)(2 * (w0 + y) + (y == 0 && !begins)) * f.slot_rows + r % FEW_BQ;
+    };
+    // each group of lanes with a maximum of its own
+    float m = -FLT_MAX, l = 0.0f;
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int y0 = wave * SETS * AHEAD; y0 < ch; y0 += NW * SETS * AHEAD) {
+      float4 v[AHEAD];
+      float2 w[AHEAD];
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) {
+        const int y = y0 + SETS * x + set;
+        const int64_t at = row_at(min(y, ch - 1));
+        w[x] = *reinterpret_cast<const float2*>(f.ml + at * 2);
+        v[x] = *reinterpret_cast<const float4*>(f.o + at * D + col);
+        if (y >= ch) w[x] = make_float2(-FLT_MAX, 0.0f);
+      }
+      float m_new = m;
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) m_new = fmaxf(m_new, w[x].x);
+      const float corr = exp2f(m - m_new);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= corr;
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) {
+        if (y0 + SETS * x + set < ch) {
+          const float e = exp2f(w[x].x - m);
+          l = fmaf(w[x].y, e, l);
+          acc[0] = fmaf(v[x].x, e, acc[0]);
+          acc[1] = fmaf(v[x].y, e, acc[1]);
+          acc[2] = fmaf(v[x].z, e, acc[2]);
+          acc[3] = fmaf(v[x].w, e, acc[3]);
+        }
+      }
+    }
+    float mt = m;
+#pragma unroll
+    for (int x = PER; x < 64; x <<= 1) mt = fmaxf(mt, __shfl_xor(mt, x));
+    const float e0 = exp2f(m - mt);
+    l *= e0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] *= e0;
+#pragma unroll
+    for (int x = PER; x < 64; x <<= 1) {
+      l += __shfl_xor(l, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x);
+    }
+    __syncthreads();                             // (the last row's are read)
+    if (set == 0) os[wave][lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    if (lane == 0) mls[wave] = make_float2(mt, l);
+    __syncthreads();
+    if (wave == 0 && set == 0) {
+      float top = -FLT_MAX, sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) top = fmaxf(top, mls[v].x);
+      float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float e = exp2f(mls[v].x - top);
+        const float4 p = os[v][lane];
+        sum = fmaf(mls[v].y, e, sum);
+        x[0] = fmaf(p.x, e, x[0]);
+        x[1] = fmaf(p.y, e, x[1]);
+        x[2] = fmaf(p.z, e, x[2]);
+        x[3] = fmaf(p.w, e, x[3]);
+      }
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      bf16_t* op = (bf16_t*)c.o + tok * c.o_ld + head * D + col;
+      *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+      if (c.lse != nullptr && lane == 0) c.lse[id] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
+    }
+  }
+}
+
+template <int D>
+static void run_few(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
+  constexpr int SLABS = FEW_BK<D> / 8;
+  // One wave to a SIMD, 64 KB in flight on a CU: 8 x 10,160 keys of 24 heads 91 us, 1 x 139,776 of
+  // 4 heads of 128 48, with three to a CU 92 and 48, with five (a SIMD then has two) 116 and 62.
+  constexpr int PER_CU = 4;
+  const int64_t rows = (int64_t)c.n_q * c.group;
+  Few f{};
+  f.slot_rows = (int)std::min<int64_t>(FEW_BQ, rows);
+  f.waves = 256 * PER_CU;
+  f.cut = (int)std::max<int64_t>(0, std::min<int64_t>(f.waves, ws_floats / (2 * (int64_t)f.slot_rows * (D + 2))));
+  f.o = ws;
+  f.ml = ws + 2 * (int64_t)f.cut * f.slot_rows * D;
+  const int run = std::min(1 << c.pg.lg_page >> 3, SLABS);
+  if (run == 1) hipLaunchKernelGGL((cache_few<D, 1>), dim3(f.waves), dim3(64), 0, st, c, f);
+  else if (run == 2) hipLaunchKernelGGL((cache_few<D, 2>), dim3(f.waves), dim3(64), 0, st, c, f);
+  else if (run == 4) hipLaunchKernelGGL((cache_few<D, 4>), dim3(f.waves), dim3(64), 0, st, c, f);
+  else hipLaunchKernelGGL((cache_few<D, SLABS>), dim3(f.waves), dim3(64), 0, st, c, f);
+  if (f.cut) {
+    // few rows have many partial results each
+    const unsigned n = (unsigned)std::min<int64_t>((int64_t)c.n_q * c.heads, 4096);
+    if (n <= 64) hipLaunchKernelGGL((cache_few_join<D, 16>), dim3(n), dim3(1024), 0, st, c, f);
+    else hipLaunchKernelGGL((cache_few_join<D, 4>), dim3(n), dim3(256), 0, st, c, f);
   }
 }
 
 template <typename T, int D>
 static void run_cache(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
   constexpr bool F32 = sizeof(T) == 4;
+  // few rows to a sequence, by the mean that the host knows (the line of tiles is counted in
+  // 32 bits)
+  if constexpr (!F32) {
+    const int64_t tiles = (((int64_t)c.pg.max_pages << c.pg.lg_page) / FEW_BK<D> + 1) * c.pg.kv_heads;
+    const int64_t most = ((int64_t)c.n_q * c.group + (int64_t)(FEW_BQ - 1) * c.pg.n_seqs) / FEW_BQ;
+    if ((int64_t)c.n_q * c.group <= (int64_t)FEW_BQ * c.pg.n_seqs && tiles < (1ll << 31) / most) {
+      run_few<D>(c, ws, ws_floats, st);
+      return;
+    }
+  }
   constexpr int BQ = F32 ? 32 : 128, BK = F32 ? 32 : CA_BK;
-  const int kvh = c.pg.kv_heads, group = c.heads / kvh;
+  const int kvh = c.pg.kv_heads, group = c.group;
   // row tiles at most and at least: the chunks' lengths are on the device
   const int64_t rows = (int64_t)c.n_q * group;
   const int64_t most = std::min((rows + (int64_t)(BQ - 1) * c.pg.n_seqs) / BQ, rows), least = (rows + BQ - 1) / BQ;

@@ -330,6 +330,8 @@ struct CacheArgs {
   int n_q, heads, dim;
   int causal, window;
   float scale;
+  int group;                           // heads to a K/V head
+  uint32_t group_magic;                // ceil(2^32 / group)
 };
 hipError_t launch_cache_attention(int dtype, const CacheArgs& a, float* ws, int64_t ws_floats, hipStream_t st);
 

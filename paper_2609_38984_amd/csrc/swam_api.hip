@@ -1830,7 +1830,9 @@ int swam_cache_attention(swam_ctx* c, const swam_kv_cache* cache, const int32_t*
   if (meet(os, ls)) return set_err(c, SWAM_E_INVALID, "o overlaps lse");
   if (!c) return set_err(nullptr, SWAM_E_INVALID, "ctx is NULL");
   if (rows == 0) return SWAM_OK;
-  CacheArgs a{paged(cache, cu), q, o, lse, q_stride, o_stride, (int)rows, n_heads, cache->head_dim, causal, window, scale};
+  CacheArgs a{paged(cache, cu), q, o, lse, q_stride, o_stride, (int)rows, n_heads, cache->head_dim, causal, window, scale,
+              n_heads / cache->n_kv_heads, 0};
+  a.group_magic = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   OnDevice dev(c);
   Timed t(c, SWAM_T_CACHE_ATTN);
   SWAM_HIP(c, launch_cache_attention(c->cfg.dtype, a, c->ptr<float>(c->lay.splitk), c->dv.splitk_floats, c->st),
