@@ -315,7 +315,7 @@ struct HeadPost {
   int64_t rows;
   int heads, kv_heads, dim;
   int norm, rot, half;                 // rot: rotated elements, half: their layout
-  float eps, mag;
+  float eps, mag, inv_dim;             // 1 / dim
 };
 hipError_t launch_head_post(int dtype, const HeadPost& a, const Paged* cache, hipStream_t st);
 

@@ -1750,6 +1750,7 @@ int swam_qk_norm_rope(swam_ctx* c, const swam_qk_post* post, const int32_t* pos,
   a.q_out = q_out; a.qo_ld = qo_stride; a.k_out = k_out; a.ko_ld = ko_stride;
   a.pos = pos; a.rows = rows;
   a.heads = n_heads; a.kv_heads = n_kv_heads; a.dim = head_dim;
+  a.inv_dim = 1.0f / (float)head_dim;
   OnDevice dev(c);
   Timed t(c, SWAM_T_HEAD_POST);
   SWAM_HIP(c, launch_head_post(c->cfg.dtype, a, nullptr, c->st), "qk_norm_rope");
@@ -1797,6 +1798,7 @@ int swam_cache_append(swam_ctx* c, const swam_kv_cache* cache, const swam_qk_pos
   a.q_out = q_out; a.qo_ld = qo_stride;
   a.pos = pos; a.rows = rows;
   a.heads = n_heads; a.kv_heads = cache->n_kv_heads; a.dim = cache->head_dim;
+  a.inv_dim = 1.0f / (float)cache->head_dim;
   const Paged pg = paged(cache, cu);
   OnDevice dev(c);
   Timed t(c, SWAM_T_APPEND);
