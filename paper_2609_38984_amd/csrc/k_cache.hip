@@ -30,11 +30,11 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 struct Split {
   float* o;
   float* ml;
-  int* plan;          // [0]: log2 of a slice's tiles, written by workgroup 0 for the joining pass
+  int* plan;          // [0]: tiles of a slice, written by workgroup 0 for the joining pass
   int budget;         // slices beyond the first of every row tile, 0: keys are not split
   int slot_rows;
 };
-constexpr int NO_SPLIT = 30;                   // log2 of more tiles than any sequence has
+constexpr int NO_SPLIT = 1 << 30;              // more tiles than any sequence has
 
 // Sequence s as the kernels see it.
 struct Seq {
@@ -69,27 +69,28 @@ __device__ __forceinline__ T wave_scan(T v, int n) {
   return v;
 }
 
-// log2 of the tiles of a slice, from the key tiles of all row tiles (`all`, over all K/V heads) and
-// the most of one: modelled time (us) of a workgroup by itself (`lone` a tile) and of several that
-// share a CU, and of the pass that joins the slices.  all / 2^lg slices beyond the first
-// are within the budget; a row tile of more than 2^lg tiles has fewer than 2 all / 2^lg.
+// Tiles of a slice, from the key tiles of all row tiles (`all`, over all K/V heads) and the most of
+// one: modelled time (us) of a workgroup by itself (`lone` a tile) and of several that share a
+// CU, and of the pass that joins the slices.  all / t slices beyond the first are within the
+// budget; a row tile of more than t tiles has fewer than 2 all / t.
 template <int D>
 __device__ __forceinline__ int slice_tiles(float all, int most, const Split& sp) {
   if (sp.budget == 0) return NO_SPLIT;
-  const float lone = D == 64 ? 1.2f : 1.6f, share = (D == 64 ? 0.64f : 1.0f) / 256.0f * all;
-  const float join = 2.0f * all * (float)sp.slot_rows * (D + 2) * (4.0f / 3.0e6f);
+  const float lone = D == 64 ? 1.0f : 1.4f, share = (D == 64 ? 0.64f : 1.0f) / 256.0f * all;
+  const float join = 2.0f * all * (float)sp.slot_rows * (D + 2) * (4.0f / 4.0e6f);
   int best = NO_SPLIT;
   float best_us = fmaxf(lone * (float)most, share);
-#pragma unroll 1
-  for (int lg = 1; (1 << lg) < most; ++lg) {
-    const float t = (float)(1 << lg);
-    if (t * (float)sp.budget < all * 1.0001f + 1.0f) continue;
+  constexpr int PARTS[] = {2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32, 64};
+#pragma unroll
+  for (int k = 0; k < (int)(sizeof(PARTS) / sizeof(int)); ++k) {
+    const int n = (most + PARTS[k] - 1) / PARTS[k];
+    const float t = (float)n;
     const float us = fmaxf(lone * t, share) + 4.5f + join * __builtin_amdgcn_rcpf(t);
-    if (us < best_us) { best_us = us; best = lg; }
+    if (n > 1 && t * (float)sp.budget >= all * 1.0001f + 1.0f && us < best_us) { best_us = us; best = n; }
   }
   return best;
 }
-__device__ __forceinline__ int slices(int nk, int lg) { return max((nk + (1 << lg) - 1) >> lg, 1); }
+__device__ __forceinline__ int slices(int nk, int tiles) { return nk <= tiles ? 1 : (nk + tiles - 1) / tiles; }
 
 // What a workgroup does: slice y of ch of the keys of row tile qi of sequence s, its
 // partial results in `slot` (units before it in split sequences).
@@ -104,7 +105,7 @@ __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int
   const int lane = threadIdx.x & 63;
   const int per = (c.pg.n_seqs + 63) >> 6, lanes = min(c.pg.n_seqs, 64);
   const Seq first = seq_at<BQ, BK>(c, lane * per);
-  int lg = NO_SPLIT;
+  int tiles = NO_SPLIT;
   if (sp.budget) {
     float all = (float)first.qt * (float)first.nk;
     int most = first.nk;
@@ -118,14 +119,14 @@ __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int
       most = max(most, __shfl_xor(most, o));
     }
     all = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, all)));
-    lg = __builtin_amdgcn_readfirstlane(
+    tiles = __builtin_amdgcn_readfirstlane(
         slice_tiles<D>(all * (float)c.pg.kv_heads, __builtin_amdgcn_readfirstlane(most), sp));
-    if (blockIdx.x == 0 && threadIdx.x == 0) sp.plan[0] = lg;
+    if (blockIdx.x == 0 && threadIdx.x == 0) sp.plan[0] = tiles;
   }
   int units = 0, split = 0;
   for (int i = 0; i < per; ++i) {
     const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, lane * per + i);
-    const int ch = slices(q.nk, lg);
+    const int ch = slices(q.nk, tiles);
     units += q.qt * ch;
     split += ch > 1 ? q.qt * ch : 0;
   }
@@ -138,7 +139,7 @@ __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int
   int r = 0;
   for (int i = 0; i < per; ++i) {
     const Seq q = i == 0 ? first : seq_at<BQ, BK>(c, lane * per + i);
-    const int ch = slices(q.nk, lg), n = q.qt * ch;
+    const int ch = slices(q.nk, tiles), n = q.qt * ch;
     if (unit >= at && unit < at + n) {
       w.q = q;
       w.s = lane * per + i;
@@ -526,312 +527,149 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   if (c.lse != nullptr && g == 0) c.lse[tok * c.heads + head] = l == 0.0f ? -INFINITY : (m_run + log2f(l)) * LN2;
 }
 
-// float32: the same products on 32x32x2 MFMAs with operands straight from global memory.
-// Four waves take every fourth tile of 32 keys of the same 32 rows and meet in LDS.
-template <int D>
-__global__ void __launch_bounds__(256)
-cache_f32(const CacheArgs c, const Split sp, int unit0) {
-  constexpr int LD = D + 4, BQ = 32, BK = 32;
-  __shared__ float os[4][32][LD];
-  __shared__ float ms[4][32], ls[4][32];
-  const int group = c.group;
-  const int hk = blockIdx.x % c.pg.kv_heads;
-  Work w;
-  if (!work_at<D, BQ, BK>(c, sp, unit0 + blockIdx.x / c.pg.kv_heads, w)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, r31 = lane & 31;
-  const int r0 = w.qi * BQ, left = min(w.q.n * group - r0, BQ), total = w.q.total;   // rows of the tile
-  const Rows row_of(r0, c);
-  const int t_last = row_of.token(left - 1);
-  int lo, hi, t0, t1;
-  key_range(c, w.q, row_of.tok, t_last, lo, hi);
-  slice_of(lo, hi, BK, w.y, w.ch, t0, t1);
-  const int mine_row = min(r31, left - 1), my_tok = row_of.token(mine_row);
-  int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
-  if (c.causal) {
-    lim = min(lim, w.q.old + my_tok);
-    lim_first = min(lim_first, w.q.old + row_of.tok);
-  }
-  if (c.window) {
-    low = max(w.q.old + my_tok - c.window + 1, 0);
-    low_last = max(w.q.old + t_last - c.window + 1, 0);
-  }
-  f32x4 qf[D / 8];
-  {
-    const float* qp = (const float*)c.q + (int64_t)(w.q.a + my_tok) * c.q_ld + (hk * group + row_of.head(mine_row)) * D;
-#pragma unroll
-    for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 4 * (2 * s + g));
-  }
-  const int32_t* table = c.pg.table + w.s * c.pg.table_ld;
-  const int slot_mask = (1 << c.pg.lg_page) - 1;
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-  const float sc = LOG2E * c.scale;
-  float m = -FLT_MAX, l = 0.0f;
-  for (int t = t0 + wave; t < t1; t += 4) {
-    const int kb = t * BK, key = kb + r31;
-    int page = key < total ? table[key >> c.pg.lg_page] : -1;
-    if (page >= c.pg.n_pages) page = -1;
-    const uint32_t vis = (uint32_t)__ballot(page >= 0);
-    if (vis == 0) continue;
-    page = max(page, 0);                         // (a tile with a visible key has a page 0)
-    // all operands of the tile are requested before the first product
-    const float* kp = (const float*)c.pg.k + page * c.pg.k_page + (key & slot_mask) * c.pg.k_token + hk * c.pg.k_head;
-    f32x4 kf[D / 8];
-#pragma unroll
-    for (int s = 0; s < D / 8; ++s) kf[s] = *reinterpret_cast<const f32x4*>(kp + 4 * (2 * s + g));
-    float vf[D / 32][16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int kr = 8 * (r >> 2) + 4 * g + (r & 3);
-      const float* vp = (const float*)c.pg.v + __shfl(page, kr) * c.pg.v_page + ((kb + kr) & slot_mask) * c.pg.v_token +
-                        hk * c.pg.v_head + r31;
-#pragma unroll
-      for (int h = 0; h < D / 32; ++h) vf[h][r] = vp[32 * h];
-    }
-    f32x16 st;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) st[r] = 0.0f;
-#pragma unroll
-    for (int s = 0; s < D / 8; ++s) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[s][e], qf[s][e], st, 0, 0, 0);
-    }
-    // the keys that this lane's row sees
-    const int h = lim - kb, u = low - kb;
-    uint32_t row_sees = h < 0 ? 0u : h >= 31 ? vis : vis & ((2u << h) - 1);
-    row_sees = u > 31 ? 0u : u > 0 ? row_sees & (~0u << u) : row_sees;
-    const uint32_t mine = row_sees >> (4 * g), any = vis >> (4 * g);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      st[r] = ((mine >> (8 * (r >> 2) + (r & 3))) & 1u) ? st[r] * sc : -INFINITY;
-      mx = fmaxf(mx, st[r]);
-    }
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m, mx), corr = exp2f(m - m_new);
-    m = m_new;
-    l *= corr;
-#pragma unroll
-    for (int h = 0; h < D / 32; ++h)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[h][r] *= corr;
-    // a weight of zero does not hide a value that is not finite: where rows see different keys
-    // such a tile is summed key by key
-    bool odd = false;
-    if (kb + BK - 1 > lim_first || kb < low_last) {
-#pragma unroll
-      for (int h = 0; h < D / 32; ++h)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          odd |= ((any >> (8 * (r >> 2) + (r & 3))) & 1u) && !(fabsf(vf[h][r]) <= FLT_MAX);
-      odd = __any(odd);
-    }
-    if (odd) {
-      // such values are left out of the products, and the rows that see them add them
-#pragma unroll 1
-      for (int kr = 0; kr < BK; ++kr) {
-        const float* vp = (const float*)c.pg.v + __shfl(page, kr) * c.pg.v_page + ((kb + kr) & slot_mask) * c.pg.v_token +
-                          hk * c.pg.v_head;
-        const bool sees = (row_sees >> kr) & 1u;
-#pragma unroll
-        for (int h = 0; h < D / 32; ++h)
-#pragma unroll
-          for (int q4 = 0; q4 < 4; ++q4) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(vp + 32 * h + 8 * q4 + 4 * g);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              o[h][4 * q4 + e] += sees && !(fabsf(x[e]) <= FLT_MAX) ? x[e] : 0.0f;
-          }
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const bool see = (any >> (8 * (r >> 2) + (r & 3))) & 1u;
-      const float p = exp2f(st[r] - m_new);
-      l += p;
-#pragma unroll
-      for (int h = 0; h < D / 32; ++h)
-        o[h] = __builtin_amdgcn_mfma_f32_32x32x2f32(see && !(odd && !(fabsf(vf[h][r]) <= FLT_MAX)) ? vf[h][r] : 0.0f, p,
-                                                    o[h], 0, 0, 0);
-    }
-  }
-  l += __shfl_xor(l, 32);
-  if (g == 0) { ms[wave][r31] = m; ls[wave][r31] = l; }
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4)
-      *reinterpret_cast<float4*>(&os[wave][r31][32 * t + 8 * q4 + 4 * g]) =
-          make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
-  __syncthreads();
-  const int q = tid >> 3;
-  if (q >= left) return;
-  const int64_t tok = w.q.a + row_of.token(q);
-  const int head = hk * group + row_of.head(q);
-  const float mt = fmaxf(fmaxf(ms[0][q], ms[1][q]), fmaxf(ms[2][q], ms[3][q]));
-  float f[4], lt = 0.0f;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    f[v] = exp2f(ms[v][q] - mt);
-    lt = fmaf(ls[v][q], f[v], lt);
-  }
-  const bool whole = w.ch <= 1;
-  const int64_t row = ((int64_t)w.slot * c.pg.kv_heads + hk) * sp.slot_rows + q;
-  const float inv = !whole ? 1.0f : lt == 0.0f ? 0.0f : 1.0f / lt;
-  float* dst = whole ? (float*)c.o + tok * c.o_ld + head * D : sp.o + row * D;
-#pragma unroll
-  for (int h = 0; h < D / 64; ++h) {
-    const int col = 64 * h + (tid & 7) * 8;
-    float acc[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      acc[e] = 0.0f;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) acc[e] = fmaf(os[v][q][col + e], f[v], acc[e]);
-      acc[e] *= inv;
-    }
-    store8(dst + col, acc);
-  }
-  if ((tid & 7) == 0) {
-    if (!whole) {
-      sp.ml[row * 2] = mt;
-      sp.ml[row * 2 + 1] = lt;
-    } else if (c.lse != nullptr) {
-      c.lse[tok * c.heads + head] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * LN2;
-    }
-  }
-}
-
-// One wave per token and head of a split sequence adds up its slices, in a fixed order:
-// D / 4 lanes hold a slice's row, so a wave reads several at once and eight such loads are
-// in flight.
-template <typename T, int D, int BQ, int BK>
-__global__ void __launch_bounds__(256)
-cache_join(const CacheArgs c, const Split sp) {
+// Adds up the `ch` partial results of rows [r0, r1) of a row tile, slot_at(y) the slot of the
+// y-th, in their order.  A wave takes 256 / D rows at a time, eight slices on their way.
+template <typename T, int D, typename SlotAt>
+__device__ __forceinline__ void join_rows(const CacheArgs& c, const float* po, const float* pml, int slot_rows, int ch,
+                                          int a, int hk, const Rows& row_of, int r0, int r1, SlotAt slot_at) {
   constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8;
-  const int lg = sp.plan[0];
-  if (lg == NO_SPLIT) return;                   // nothing was split
-  const int lane = threadIdx.x & 63, kvh = c.pg.kv_heads;
-  const int set = lane / PER, col = lane % PER * 4;
-  const int per = (c.pg.n_seqs + 63) >> 6;
-  const int n = c.n_q * c.heads;               // (below 2^30)
-  const int64_t pitch = (int64_t)kvh * sp.slot_rows;
-  for (int id = blockIdx.x * 4 + (threadIdx.x >> 6); id < n; id += gridDim.x * 4) {
-    const int tok = id / c.heads, head = id % c.heads;
-    const int s = seq_of(c.pg, tok);
-    const Seq q = seq_at<BQ, BK>(c, s);
-    const int ch = slices(q.nk, lg);
-    if (tok < q.a || tok >= q.a + q.n || ch == 1) continue;
-    // units of the split sequences in front of it
-    int units = 0;
-    for (int i = 0; i < per; ++i) {
-      const int b = lane * per + i;
-      if (b >= s) break;
-      const Seq f = seq_at<BQ, BK>(c, b);
-      const int fc = slices(f.nk, lg);
-      units += fc > 1 ? f.qt * fc : 0;
-    }
-    if (s > 0) {
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) units += __shfl_xor(units, o);
-    }
-    const int r = (tok - q.a) * c.group + head % c.group, qi = r / BQ;
-    // (the workgroups count the row tiles from the last)
-    const int64_t slot = ((int64_t)(units + (q.qt - 1 - qi) * ch) * kvh + head / c.group) * sp.slot_rows + r % BQ;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % PER * 4;
+  for (int rb = r0 + wave * SETS; rb < r1; rb += 4 * SETS) {
+    const int r = min(rb + lane / PER, r1 - 1);
     float m = -FLT_MAX, l = 0.0f;
-    for (int y = lane; y < ch; y += 64) m = fmaxf(m, sp.ml[(slot + y * pitch) * 2]);
-    m = warp_max(m);
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int y0 = 0; y0 < ch; y0 += SETS * AHEAD) {
+    for (int y0 = 0; y0 < ch; y0 += AHEAD) {
       float4 v[AHEAD];
       float2 w[AHEAD];
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) {
-        const int64_t at = slot + min(y0 + SETS * a + set, ch - 1) * pitch;
-        w[a] = *reinterpret_cast<const float2*>(sp.ml + at * 2);
-        v[a] = *reinterpret_cast<const float4*>(sp.o + at * D + col);
+      for (int x = 0; x < AHEAD; ++x) {
+        const int64_t at = (int64_t)slot_at(min(y0 + x, ch - 1)) * slot_rows + r;
+        w[x] = *reinterpret_cast<const float2*>(pml + at * 2);
+        v[x] = *reinterpret_cast<const float4*>(po + at * D + col);
+        if (y0 + x >= ch) w[x] = make_float2(-FLT_MAX, 0.0f);
       }
+      float m_new = m;
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) {
-        if (y0 + SETS * a + set < ch) {
-          const float f = exp2f(w[a].x - m);
-          l = fmaf(w[a].y, f, l);
-          acc[0] = fmaf(v[a].x, f, acc[0]);
-          acc[1] = fmaf(v[a].y, f, acc[1]);
-          acc[2] = fmaf(v[a].z, f, acc[2]);
-          acc[3] = fmaf(v[a].w, f, acc[3]);
+      for (int x = 0; x < AHEAD; ++x) m_new = fmaxf(m_new, w[x].x);
+      const float corr = exp2f(m - m_new);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= corr;
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) {
+        if (y0 + x < ch) {
+          const float e = exp2f(w[x].x - m);
+          l = fmaf(w[x].y, e, l);
+          acc[0] = fmaf(v[x].x, e, acc[0]);
+          acc[1] = fmaf(v[x].y, e, acc[1]);
+          acc[2] = fmaf(v[x].z, e, acc[2]);
+          acc[3] = fmaf(v[x].w, e, acc[3]);
         }
       }
     }
-#pragma unroll
-    for (int o = PER; o < 64; o <<= 1) {
-      l += __shfl_xor(l, o);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
-    }
+    if (rb + lane / PER >= r1) continue;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (set == 0) {
-      T* op = (T*)c.o + tok * c.o_ld + head * D + col;
-      if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-      else
-        *reinterpret_cast<float4*>(op) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-      if (c.lse != nullptr && lane == 0) c.lse[id] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
-    }
+    const int64_t tok = a + row_of.token(r);
+    const int head = hk * c.group + row_of.head(r);
+    T* op = (T*)c.o + tok * c.o_ld + head * D + col;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+    else
+      *reinterpret_cast<float4*>(op) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    if (c.lse != nullptr && col == 0) c.lse[tok * c.heads + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
   }
 }
 
+// The slices of a chunk's row tiles: workgroup (x, y) adds up rows [32 y, 32 y + 32) of the x-th
+// (row tile, K/V head).
+template <int D>
+__global__ void __launch_bounds__(256)
+cache_join(const CacheArgs c, const Split sp) {
+  constexpr int BQ = 128, BK = CA_BK;
+  const int tiles = sp.plan[0];
+  if (tiles == NO_SPLIT) return;                // nothing was split
+  const int lane = threadIdx.x & 63, kvh = c.pg.kv_heads;
+  const int per = (c.pg.n_seqs + 63) >> 6, lanes = min(c.pg.n_seqs, 64);
+  const int hk = blockIdx.x % kvh, tile = blockIdx.x / kvh;
+  int own = 0, split = 0;
+  for (int i = 0; i < per; ++i) {
+    const Seq q = seq_at<BQ, BK>(c, lane * per + i);
+    const int ch = slices(q.nk, tiles);
+    own += q.qt;
+    split += ch > 1 ? q.qt * ch : 0;
+  }
+  int at = wave_scan(own, lanes), units = wave_scan(split, lanes);
+  const uint64_t past = __ballot(at > tile);
+  if (past == 0) return;
+  const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+  at = __builtin_amdgcn_readlane(at - own, b);
+  units = __builtin_amdgcn_readlane(units - split, b);
+  Seq q = seq_at<BQ, BK>(c, b * per);
+  int ch = slices(q.nk, tiles);
+  for (int s = b * per; tile >= at + q.qt;) {
+    at += q.qt;
+    units += ch > 1 ? q.qt * ch : 0;
+    q = seq_at<BQ, BK>(c, ++s);
+    ch = slices(q.nk, tiles);
+  }
+  if (ch == 1) return;
+  const int qi = tile - at, left = min(q.n * c.group - qi * BQ, BQ);
+  const Rows row_of(qi * BQ, c);
+  // (the workgroups count the row tiles from the last)
+  const int first = units + (q.qt - 1 - qi) * ch;
+  join_rows<bf16_t, D>(c, sp.o, sp.ml, sp.slot_rows, ch, q.a, hk, row_of, (int)blockIdx.y * 32,
+                       min(left, (int)blockIdx.y * 32 + 32), [&](int y) { return (first + y) * kvh + hk; });
+}
+
 // ---------------------------------------------------------------------------
-// few rows: single tokens, short chunks
+// one line of key tiles
 // ---------------------------------------------------------------------------
-// Here K and V are read once and their bytes are the time.  A workgroup is one wave with a ring
-// of its own in LDS: nothing waits for another wave, and a tile of 16 KB is always in
-// flight.  All key tiles of all (sequence, row tile, K/V head) segments stand in one line that is
-// cut evenly over the waves, so unequal lengths cost nothing; a segment cut by a border
-// leaves partial results, at most two to a wave.
+// Single tokens and short chunks read K and V once and their bytes are the time; in float32 the
+// matrix unit is slow enough for small row tiles.  There all key tiles of all (sequence, K/V
+// head, row tile) segments stand in one line that is cut evenly over the workgroups, so
+// unequal lengths cost nothing; a segment cut by a border leaves partial results, at most two
+// to a workgroup.
 struct Few {
-  float* o;           // [2 waves][slot_rows][head_dim] sums
-  float* ml;          // [2 waves][slot_rows] (maximum, sum)
-  int waves;          // of the launch
-  int cut;            // waves that tiles may be cut over, 0: segments stay whole
+  float* o;           // [2 wgs][slot_rows][head_dim] sums
+  float* ml;          // [2 wgs][slot_rows] (maximum, sum)
+  int wgs;            // of the launch
+  int cut;            // workgroups that tiles may be cut over, 0: segments stay whole
   int slot_rows;
 };
-constexpr int FEW_BQ = 32, FEW_STAGES = 2;
-template <int D> constexpr int FEW_BK = D == 64 ? 64 : 32;     // 16 KB of K and V either way
+constexpr int FEW_BQ = 32;
 
 // The line of tiles (or of whole segments) as the lanes hold it, `per` sequences to a lane.
 struct Line {
   int per, mine, upto;                         // this lane's units, and all up to its last
   int all;                                     // units
-  int waves;                                   // that share them
+  int wgs;                                     // that share them
   bool cut;                                    // units are tiles
+  Seq first;                                   // the lane's first sequence
   __device__ __forceinline__ static int count(const Seq& q, int kvh, bool cut) {
     return q.qt * kvh * (cut ? q.nk : 1);
   }
-  // the units [begin(w), begin(w + 1)) are wave w's
+  // the units [begin(w), begin(w + 1)) are workgroup w's
   __device__ __forceinline__ int begin(int w) const {
-    const int each = all / waves;
-    return w * each + min(w, all - each * waves);
+    const int each = all / wgs;
+    return w * each + min(w, all - each * wgs);
   }
-  // the wave of unit x
-  __device__ __forceinline__ int wave_of(int x) const {
-    const int each = all / waves, more = all - each * waves;
+  // the workgroup of unit x
+  __device__ __forceinline__ int wg_of(int x) const {
+    const int each = all / wgs, more = all - each * wgs;
     return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each;
   }
 };
-template <int D>
+template <int BK>
 __device__ __forceinline__ Line line_of(const CacheArgs& c, const Few& f) {
-  constexpr int BK = FEW_BK<D>;
   const int lane = threadIdx.x & 63, lanes = min(c.pg.n_seqs, 64), kvh = c.pg.kv_heads;
   Line l;
   l.per = (c.pg.n_seqs + 63) >> 6;
   int tiles = 0, segs = 0, most = 0;
+  l.first = seq_at<FEW_BQ, BK>(c, lane * l.per);
   for (int i = 0; i < l.per; ++i) {
-    const Seq q = seq_at<FEW_BQ, BK>(c, lane * l.per + i);
-    tiles += Line::count(q, kvh, true);
+    const Seq q = i == 0 ? l.first : seq_at<FEW_BQ, BK>(c, lane * l.per + i);
+    if (f.cut) tiles += Line::count(q, kvh, true);
     segs += Line::count(q, kvh, false);
     most = max(most, q.nk);
   }
@@ -840,20 +678,89 @@ __device__ __forceinline__ Line line_of(const CacheArgs& c, const Few& f) {
   const int n_tiles = __builtin_amdgcn_readlane(tiles_upto, lanes - 1);
   const int n_segs = __builtin_amdgcn_readlane(segs_upto, lanes - 1);
   most = __builtin_amdgcn_readfirstlane(most);
-  // cut where that saves the time of more tiles than the joining pass takes
-  const int cut_waves = min(f.cut, (n_tiles + 3) / 4);
+  // cut where that saves the time of more tiles than the joining pass adds
+  const int cut_wgs = min(f.cut, (n_tiles + 1) / 2);
   l.cut = false;
-  if (cut_waves > 0) {
-    const int whole = (n_segs + f.waves - 1) / f.waves * most, each = (n_tiles + cut_waves - 1) / cut_waves;
-    l.cut = whole > each + 8;
+  if (cut_wgs > 0) {
+    const int whole = (n_segs + f.wgs - 1) / f.wgs * most, each = (n_tiles + cut_wgs - 1) / cut_wgs;
+    l.cut = whole > each + 2;
   }
   l.mine = l.cut ? tiles : segs;
   l.upto = l.cut ? tiles_upto : segs_upto;
   l.all = l.cut ? n_tiles : n_segs;
-  l.waves = l.cut ? cut_waves : min(f.waves, max(n_segs, 1));
+  l.wgs = l.cut ? cut_wgs : min(f.wgs, max(n_segs, 1));
   return l;
 }
 
+// Row tiles stand in the line as first, last, second, last but one ...: of a causal chunk the later
+// ones see more, and the line counts the most for each.
+__device__ __forceinline__ int folded(int i, int n) { return i & 1 ? n - 1 - (i >> 1) : i >> 1; }
+__device__ __forceinline__ int fold_index(int tile, int n) { return 2 * tile < n ? 2 * tile : 2 * (n - 1 - tile) + 1; }
+
+// The part of the line that starts at `unit`: tiles [from, upto) of one segment.
+struct Part {
+  Seq q;
+  int seq, hk, r0;    // sequence, K/V head, first row
+  int from, upto;
+  bool whole;
+};
+template <int BK>
+__device__ __forceinline__ Part part_at(const CacheArgs& c, const Line& line, int unit, int end) {
+  const int kvh = c.pg.kv_heads;
+  Part p;
+  const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(line.upto > unit)) - 1);
+  int at = __builtin_amdgcn_readlane(line.upto, b) - __builtin_amdgcn_readlane(line.mine, b), seq = b * line.per;
+  auto held = [&](int v) { return __builtin_amdgcn_readlane(v, b); };
+  Seq q{held(line.first.a), held(line.first.n), held(line.first.old), held(line.first.total), held(line.first.qt),
+        held(line.first.nk)};
+  for (int n = Line::count(q, kvh, line.cut); unit >= at + n; n = Line::count(q, kvh, line.cut)) {
+    at += n;
+    q = seq_at<FEW_BQ, BK>(c, ++seq);
+  }
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  p.seq = uniform(seq);
+  p.q = Seq{uniform(q.a), uniform(q.n), uniform(q.old), uniform(q.total), uniform(q.qt), uniform(q.nk)};
+  const int rel = uniform(unit - at);
+  const int seg = line.cut ? rel / p.q.nk : rel;
+  p.from = line.cut ? rel - seg * p.q.nk : 0;
+  p.upto = line.cut ? min(p.q.nk, p.from + end - unit) : p.q.nk;
+  p.whole = p.from == 0 && p.upto == p.q.nk;
+  // row tiles of a K/V head side by side: they read the same keys
+  p.hk = seg / p.q.qt;
+  p.r0 = folded(seg - p.hk * p.q.qt, p.q.qt) * FEW_BQ;
+  return p;
+}
+// Neighbouring workgroups run on different XCDs: each XCD gets a stretch of the line.
+__device__ __forceinline__ int place_of(int wg, int wgs) {
+  const int xcd = wg & 7;
+  return xcd * (wgs >> 3) + min(xcd, wgs & 7) + (wg >> 3);
+}
+// Loads into LDS that this wave has read: its reads have arrived.
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Pages of the runs of RUN 8-key slabs of a tile, -1: none; and which of its keys there are.
+template <int N, int RUN>
+__device__ __forceinline__ void pages_of(const Paged& pg, const_i32* table, int key0, int total, int (&pages)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int key = key0 + 8 * RUN * j;
+    const int p = key < total ? table[key >> pg.lg_page] : -1;
+    pages[j] = p < pg.n_pages ? p : -1;
+  }
+}
+template <int N, int RUN>
+__device__ __forceinline__ uint64_t keys_of(int key0, int total, const int (&pages)[N]) {
+  uint64_t m = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) m |= pages[j] >= 0 ? (~0ull >> (64 - 8 * RUN)) << (8 * RUN * j) : 0ull;
+  const int n = total - key0;
+  return n >= 8 * RUN * N ? m : n <= 0 ? 0ull : m & ((1ull << n) - 1);
+}
+
+// bf16, few rows: a workgroup is one wave with a ring of its own in LDS: nothing waits for
+// another wave, and a tile of 16 KB is always in flight.
+constexpr int FEW_STAGES = 2;
+template <int D> constexpr int FEW_BK = D == 64 ? 64 : 32;     // 16 KB of K and V either way
 // RUN: 8-key slabs that share a page for certain
 template <int D, int RUN>
 __global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 8)))
@@ -863,9 +770,9 @@ cache_few(const CacheArgs c, const Few f) {
   constexpr int NI = 2 * SLABS * H2;             // loads of a stage
   __shared__ uint4 kv[FEW_STAGES][2][TILE];      // [stage][K | V][half][key][8 chunks]
   const int lane = threadIdx.x, g = lane >> 5, r31 = lane & 31, kvh = c.pg.kv_heads;
-  const Line line = line_of<D>(c, f);
-  const int wid = blockIdx.x;
-  if (wid >= line.waves) return;
+  const Line line = line_of<BK>(c, f);
+  if ((int)blockIdx.x >= line.wgs) return;
+  const int wid = place_of(blockIdx.x, line.wgs);
   const int first = line.begin(wid), end = line.begin(wid + 1);
 
   const int lrow = lane >> 3;
@@ -890,35 +797,18 @@ cache_few(const CacheArgs c, const Few f) {
   const float sc = LOG2E * c.scale;
 
   for (int unit = first; unit < end;) {
-    // the segment of this unit
-    const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(line.upto > unit)) - 1);
-    int at = __builtin_amdgcn_readlane(line.upto, b) - __builtin_amdgcn_readlane(line.mine, b), seq = b * line.per;
-    Seq q = seq_at<FEW_BQ, BK>(c, seq);
-    for (int n = Line::count(q, kvh, line.cut); unit >= at + n; n = Line::count(q, kvh, line.cut)) {
-      at += n;
-      q = seq_at<FEW_BQ, BK>(c, ++seq);
-    }
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    q.a = __builtin_amdgcn_readfirstlane(q.a);
-    q.n = __builtin_amdgcn_readfirstlane(q.n);
-    q.old = __builtin_amdgcn_readfirstlane(q.old);
-    q.total = __builtin_amdgcn_readfirstlane(q.total);
-    q.nk = __builtin_amdgcn_readfirstlane(q.nk);
-    const int rel = __builtin_amdgcn_readfirstlane(unit - at);
-    const int seg = line.cut ? rel / q.nk : rel, from = line.cut ? rel - seg * q.nk : 0;
-    const int upto = line.cut ? min(q.nk, from + end - unit) : q.nk;
-    const bool whole = from == 0 && upto == q.nk;
-    const int qi = seg / kvh, hk = seg - qi * kvh;
+    const Part p = part_at<BK>(c, line, unit, end);
+    const Seq& q = p.q;
     // the segment starts this wave's units, or ends them behind others
     const int slot = 2 * wid + (unit != first);
-    unit += line.cut ? upto - from : 1;
+    unit += line.cut ? p.upto - p.from : 1;
 
-    const int r0 = qi * FEW_BQ, left = min(q.n * c.group - r0, FEW_BQ), total = q.total;
+    const int hk = p.hk, r0 = p.r0, left = min(q.n * c.group - r0, FEW_BQ), total = q.total;
     const Rows row_of(r0, c);
     const int t_last = row_of.token(left - 1);
     int lo, hi;
     key_range(c, q, row_of.tok, t_last, lo, hi);
-    const int base = lo / BK, t0 = base + from, t1 = min(base + upto, (hi + BK - 1) / BK);
+    const int base = lo / BK, t0 = base + p.from, t1 = min(base + p.upto, (hi + BK - 1) / BK);
     const int mine = min(r31, left - 1), my_tok = row_of.token(mine);
     int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
     if (c.causal) {
@@ -929,38 +819,22 @@ cache_few(const CacheArgs c, const Few f) {
       low = max(q.old + my_tok - c.window + 1, 0);
       low_last = max(q.old + t_last - c.window + 1, 0);
     }
-    const_i32* table = (const_i32*)(c.pg.table + seq * c.pg.table_ld);
+    const_i32* table = (const_i32*)(c.pg.table + p.seq * c.pg.table_ld);
     const bf16_t* k_head = (const bf16_t*)c.pg.k + hk * c.pg.k_head;
     const bf16_t* v_head = (const bf16_t*)c.pg.v + hk * c.pg.v_head;
 
-    // the pages of the runs of tile t, -1: none
-    auto pages_of = [&](int t, int (&pages)[SLABS / RUN]) {
-#pragma unroll
-      for (int j = 0; j < SLABS / RUN; ++j) {
-        const int key = t * BK + 8 * RUN * j;
-        const int p = key < total && t < t1 ? table[key >> c.pg.lg_page] : -1;
-        pages[j] = p < c.pg.n_pages ? p : -1;
-      }
-    };
-    auto keys_of = [&](int t, const int (&pages)[SLABS / RUN]) -> uint64_t {
-      uint64_t m = 0;
-#pragma unroll
-      for (int j = 0; j < SLABS / RUN; ++j)
-        m |= pages[j] >= 0 ? (~0ull >> (64 - 8 * RUN)) << (8 * RUN * j) : 0ull;
-      const int n = total - t * BK;
-      return n >= BK ? m : n <= 0 ? 0ull : m & ((1ull << n) - 1);
-    };
+    constexpr int RUNS = SLABS / RUN;
     // (always as many loads: what has no page stores zeros)
-    auto issue = [&](int stage, int t, const int (&pages)[SLABS / RUN]) {
+    auto issue = [&](int stage, int t, const int (&pages)[RUNS]) {
 #pragma unroll
-      for (int j = 0; j < SLABS / RUN; ++j) {
+      for (int j = 0; j < RUNS; ++j) {
         const int key = t * BK + 8 * RUN * j, n = pages[j] < 0 ? 0 : min(total - key, 8 * RUN);
-        const int64_t p = max(pages[j], 0), slot = key & ((1 << c.pg.lg_page) - 1);
+        const int64_t pg = max(pages[j], 0), slot = key & ((1 << c.pg.lg_page) - 1);
         const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(k_head + p * c.pg.k_page + slot * c.pg.k_token), (short)0, n ? ((n - 1) * (int)c.pg.k_token + D) * 2 : 0,
+            (void*)(k_head + pg * c.pg.k_page + slot * c.pg.k_token), (short)0, n ? ((n - 1) * (int)c.pg.k_token + D) * 2 : 0,
             SWAM_BUF_DWORD3);
         const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(v_head + p * c.pg.v_page + slot * c.pg.v_token), (short)0, n ? ((n - 1) * (int)c.pg.v_token + D) * 2 : 0,
+            (void*)(v_head + pg * c.pg.v_page + slot * c.pg.v_token), (short)0, n ? ((n - 1) * (int)c.pg.v_token + D) * 2 : 0,
             SWAM_BUF_DWORD3);
 #pragma unroll
         for (int i = 0; i < RUN; ++i)
@@ -980,11 +854,13 @@ cache_few(const CacheArgs c, const Few f) {
       for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
     float m_run = -FLT_MAX, l_run = 0.0f;
 
-    int pages[SLABS / RUN];
-    pages_of(t0, pages);
-    uint64_t keys = keys_of(t0, pages), ahead;   // of the tile at hand and the next
+    // (behind the last tile there are no pages)
+    const int stop = min(total, t1 * BK);
+    int pages[RUNS];
+    pages_of<RUNS, RUN>(c.pg, table, t0 * BK, stop, pages);
+    uint64_t keys = keys_of<RUNS, RUN>(t0 * BK, total, pages), ahead;   // of the tile at hand and the next
     issue(0, t0, pages);
-    pages_of(t0 + 1, pages);
+    pages_of<RUNS, RUN>(c.pg, table, (t0 + 1) * BK, stop, pages);
     bf16x8 qf[D / 16];
     {
       const bf16_t* qp = (const bf16_t*)c.q + (int64_t)(q.a + my_tok) * c.q_ld + (hk * c.group + row_of.head(mine)) * D;
@@ -995,9 +871,10 @@ cache_few(const CacheArgs c, const Few f) {
     int buf = 0;
 #pragma unroll 1
     for (int t = t0; t < t1; ++t, keys = ahead, buf ^= 1) {
-        ahead = keys_of(t + 1, pages);
+        ahead = keys_of<RUNS, RUN>((t + 1) * BK, total, pages);
+        reads_done();
         issue(buf ^ 1, t + 1, pages);
-        pages_of(t + 2, pages);
+        pages_of<RUNS, RUN>(c.pg, table, (t + 2) * BK, stop, pages);
         wait_stage<NI>();
         if (keys == 0) continue;
         const uint4* Kt = kv[buf][0];
@@ -1107,7 +984,7 @@ cache_few(const CacheArgs c, const Few f) {
     const float l = l_run + __shfl_xor(l_run, 32);
     const int64_t tok = q.a + my_tok;
     const int head = hk * c.group + row_of.head(mine);
-    if (!whole) {
+    if (!p.whole) {
       if (r31 < left) {
         const int64_t row = (int64_t)slot * f.slot_rows + r31;
         float* po = f.o + row * D;
@@ -1140,15 +1017,272 @@ cache_few(const CacheArgs c, const Few f) {
   }
 }
 
-// One workgroup of NW waves per token and head adds up what the waves left of a segment that
-// was cut, in a fixed order: each of its waves every NW-th group of them.
-template <int D, int NW>
+// float32: 32x32x2 MFMAs.  Four waves take every fourth tile of 32 keys of the same 32 rows and
+// meet in LDS.  Each has room for one tile of K and one of V there: V is on its way during the
+// scores, the next K during the products with V, so a wave never waits for both, and two
+// waves share a SIMD.
+template <int D, int RUN>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, 8)))
+cache_f32(const CacheArgs c, const Few f) {
+  constexpr int H2 = D / 64, BK = 32, SLABS = BK / 8, RUNS = SLABS / RUN;
+  constexpr int TILE = BK * 16 * H2;             // float4 of a K or V tile
+  constexpr int NI = 8 * H2;                     // loads of one
+  constexpr int LD = D + 4;
+  __shared__ float4 kv[4][2][TILE];              // [wave][K | V][half][key][16 chunks]
+  __shared__ float ms[4][32], ls[4][32];
+  static_assert(sizeof(kv) >= 4 * 32 * LD * 4, "the waves meet in the tiles' place");
+  float (*os)[32][LD] = reinterpret_cast<float (*)[32][LD]>(&kv[0][0][0]);
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, r31 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Line line = line_of<BK>(c, f);
+  if ((int)blockIdx.x >= line.wgs) return;
+  const int wid = place_of(blockIdx.x, line.wgs);
+  const int first = line.begin(wid), end = line.begin(wid + 1);
+
+  // A load brings 4 keys of 256 bytes.  Chunk x of K's key r stands in place x ^ (r & 15), so that
+  // 16 keys at one chunk (the scores' operand) hit every bank once; V's in x ^ 8 for every second
+  // four keys, so that two rows 4 keys apart at 32 columns do.
+  const int lrow = lane >> 4, lcol = 16 * (lane & 15), lcol_k = lcol ^ (16 * lrow);
+  const int vofs[2] = {4 * g * 64 + r31 + 32 * g, 4 * g * 64 + r31 + 32 * (g ^ 1)};
+  const float sc = LOG2E * c.scale;
+
+  for (int unit = first; unit < end;) {
+    const Part p = part_at<BK>(c, line, unit, end);
+    const Seq& q = p.q;
+    const int slot = 2 * wid + (unit != first);
+    unit += line.cut ? p.upto - p.from : 1;
+
+    const int hk = p.hk, r0 = p.r0, left = min(q.n * c.group - r0, FEW_BQ), total = q.total;
+    const Rows row_of(r0, c);
+    const int t_last = row_of.token(left - 1);
+    int lo, hi;
+    key_range(c, q, row_of.tok, t_last, lo, hi);
+    const int base = lo / BK, t0 = base + p.from, t1 = min(base + p.upto, (hi + BK - 1) / BK);
+    const int mine = min(r31, left - 1), my_tok = row_of.token(mine);
+    int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
+    if (c.causal) {
+      lim = min(lim, q.old + my_tok);
+      lim_first = min(lim_first, q.old + row_of.tok);
+    }
+    if (c.window) {
+      low = max(q.old + my_tok - c.window + 1, 0);
+      low_last = max(q.old + t_last - c.window + 1, 0);
+    }
+    const_i32* table = (const_i32*)(c.pg.table + p.seq * c.pg.table_ld);
+    const float* k_head = (const float*)c.pg.k + hk * c.pg.k_head;
+    const float* v_head = (const float*)c.pg.v + hk * c.pg.v_head;
+    // (always as many loads: what has no page stores zeros)
+    auto issue = [&](bool is_v, int t, const int (&pages)[RUNS]) {
+      float4* to = kv[wave][is_v];
+      const float* head = is_v ? v_head : k_head;
+      const int64_t page_ld = is_v ? c.pg.v_page : c.pg.k_page, token_ld = is_v ? c.pg.v_token : c.pg.k_token;
+      const int row = lrow * (int)token_ld * 4;
+#pragma unroll
+      for (int j = 0; j < RUNS; ++j) {
+        const int key = t * BK + 8 * RUN * j, n = pages[j] < 0 ? 0 : min(total - key, 8 * RUN);
+        const int64_t pg = max(pages[j], 0), at = key & ((1 << c.pg.lg_page) - 1);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(head + pg * page_ld + at * token_ld), (short)0, n ? ((n - 1) * (int)token_ld + D) * 4 : 0, SWAM_BUF_DWORD3);
+#pragma unroll
+        for (int i = 0; i < 2 * RUN; ++i)
+#pragma unroll
+          for (int h = 0; h < H2; ++h) {
+            const int four = 2 * RUN * j + i;    // 4 keys
+            dma_slab(r, (uint4*)&to[(h * 2 * SLABS + four) * 64],
+                     vadd_sgpr(row + (is_v ? lcol ^ ((four & 1) << 7) : lcol_k ^ ((four & 3) << 6)), 256 * h + 16 * i * (int)token_ld));
+          }
+      }
+    };
+    f32x4 qf[D / 8];
+    {
+      const float* qp = (const float*)c.q + (int64_t)(q.a + my_tok) * c.q_ld + (hk * c.group + row_of.head(mine)) * D;
+#pragma unroll
+      for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 4 * (2 * s + g));
+    }
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+    float m = -FLT_MAX, l = 0.0f;
+
+    const float4* Kt = kv[wave][0];
+    const float4* Vt = kv[wave][1];
+    const int stop = min(total, t1 * BK);
+    int pages[RUNS], ahead[RUNS];
+    pages_of<RUNS, RUN>(c.pg, table, (t0 + wave) * BK, stop, pages);
+    issue(false, t0 + wave, pages);
+#pragma unroll 1
+    for (int t = t0 + wave; t < t1; t += 4) {
+      const int k0 = t * BK;
+      reads_done();
+      issue(true, t, pages);
+      pages_of<RUNS, RUN>(c.pg, table, k0 + 4 * BK, stop, ahead);
+      const uint32_t vis = (uint32_t)keys_of<RUNS, RUN>(k0, total, pages);
+      wait_stage<NI>();
+      f32x16 st;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < D / 8; ++s) {
+        const float4 kf = Kt[(s >> 3) * BK * 16 + r31 * 16 + ((2 * (s & 7) + g) ^ (r31 & 15))];
+        st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.x, qf[s][0], st, 0, 0, 0);
+        st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.y, qf[s][1], st, 0, 0, 0);
+        st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.z, qf[s][2], st, 0, 0, 0);
+        st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.w, qf[s][3], st, 0, 0, 0);
+      }
+      reads_done();
+      issue(false, t + 4, ahead);
+#pragma unroll
+      for (int j = 0; j < RUNS; ++j) pages[j] = ahead[j];
+      // the keys that this lane's row sees
+      const int h = lim - k0, u = low - k0;
+      uint32_t sees = h < 0 ? 0u : h >= BK - 1 ? vis : vis & ((2u << h) - 1);
+      sees = u > 31 ? 0u : u > 0 ? sees & (~0u << u) : sees;
+      if (__any(sees != ~0u)) {
+        uint32_t bits = sees >> (4 * g);
+        asm volatile("" : "+v"(bits));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (r >> 2) + (r & 3), 1);
+          st[r] = __uint_as_float((__float_as_uint(st[r]) & keep) | (0xff800000u & ~keep));
+        }
+      }
+      float mx = st[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, st[r]);
+      // the running maximum moves only when some weight would pass 2^8
+      if (__any(mx * sc > m + 8.0f)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m, mx * sc), corr = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= corr;
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[x][r] *= corr;
+      }
+      wait_stage<NI>();
+      // a weight of zero does not hide a value that is not finite: where rows see different keys
+      // such values are left out of the products and added by hand
+      bool odd = false;
+      if ((k0 + BK - 1 > lim_first && lim_first < total - 1) || k0 < low_last) {
+#pragma unroll
+        for (int i = 0; i < TILE / 64; ++i) {
+          const float4 x = Vt[i * 64 + lane];
+          odd |= !(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w))) <= FLT_MAX) || x.x != x.x ||
+                 x.y != x.y || x.z != x.z || x.w != x.w;
+        }
+        odd = __any(odd);
+      }
+      if (odd) {
+#pragma unroll 1
+        for (int key = 0; key < BK; ++key) {
+          const bool see = (sees >> key) & 1u;
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              const float4 v = Vt[(x >> 1) * BK * 16 + key * 16 + ((8 * (x & 1) + 2 * q4 + g) ^ (2 * (key & 4)))];
+              const float e4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                o[x][4 * q4 + e] += see && !(fabsf(e4[e]) <= FLT_MAX) ? e4[e] : 0.0f;
+            }
+        }
+      }
+      float w[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        w[r] = __builtin_amdgcn_exp2f(fmaf(st[r], sc, -m));
+        l += w[r];
+      }
+      auto products = [&](auto clean) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x) {
+            const float v = reinterpret_cast<const float*>(Vt)[vofs[x & 1] + (x >> 1) * BK * 64 + (8 * (r >> 2) + (r & 3)) * 64];
+            o[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(clean(v), w[r], o[x], 0, 0, 0);
+          }
+      };
+      if (odd) products([](float v) { return fabsf(v) <= FLT_MAX ? v : 0.0f; });
+      else products([](float v) { return v; });
+    }
+    wait_stage<0>();
+    l += __shfl_xor(l, 32);
+    __syncthreads();                             // the tiles are read
+    if (g == 0) { ms[wave][r31] = m; ls[wave][r31] = l; }
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<float4*>(&os[wave][r31][32 * t + 8 * q4 + 4 * g]) =
+            make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
+    __syncthreads();
+    const int row = tid >> 3;
+    if (row < left) {
+      const int64_t tok = q.a + row_of.token(row);
+      const int head = hk * c.group + row_of.head(row);
+      const float mt = fmaxf(fmaxf(ms[0][row], ms[1][row]), fmaxf(ms[2][row], ms[3][row]));
+      float e4[4], lt = 0.0f;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        e4[v] = exp2f(ms[v][row] - mt);
+        lt = fmaf(ls[v][row], e4[v], lt);
+      }
+      const int64_t at = (int64_t)slot * f.slot_rows + row;
+      const float inv = !p.whole ? 1.0f : lt == 0.0f ? 0.0f : 1.0f / lt;
+      float* dst = p.whole ? (float*)c.o + tok * c.o_ld + head * D : f.o + at * D;
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h) {
+        const int col = 64 * h + (tid & 7) * 8;
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          acc[e] = 0.0f;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) acc[e] = fmaf(os[v][row][col + e], e4[v], acc[e]);
+          acc[e] *= inv;
+        }
+        store8(dst + col, acc);
+      }
+      if ((tid & 7) == 0) {
+        if (!p.whole) *reinterpret_cast<float2*>(f.ml + at * 2) = make_float2(mt, lt);
+        else if (c.lse != nullptr) c.lse[tok * c.heads + head] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * LN2;
+      }
+    }
+    __syncthreads();                             // the tiles' place is free again
+  }
+}
+
+// The segment that the border behind workgroup j's units cuts, where j has its start: a
+// workgroup for each border.
+template <typename T, int D, int BK>
+__global__ void __launch_bounds__(256)
+line_join(const CacheArgs c, const Few f) {
+  const Line line = line_of<BK>(c, f);
+  const int j = blockIdx.x;
+  if (!line.cut || j + 1 >= line.wgs) return;
+  const int begin = line.begin(j), end = line.begin(j + 1);
+  const Part p = part_at<BK>(c, line, end - 1, end);
+  const int start = end - 1 - p.from;
+  if (start < begin || start + p.q.nk <= end) return;
+  const int ch = line.wg_of(start + p.q.nk - 1) - j + 1, left = min(p.q.n * c.group - p.r0, FEW_BQ);
+  const Rows row_of(p.r0, c);
+  // j's may be the end of its units, the others' start theirs
+  join_rows<T, D>(c, f.o, f.ml, f.slot_rows, ch, p.q.a, p.hk, row_of, 0, left,
+                  [&](int y) { return 2 * (j + y) + (y == 0 && start != begin); });
+}
+// The same for few rows, which have many partial results each: a workgroup of NW waves per
+// token and head, each wave every NW-th group of them.
+template <typename T, int D, int BK, int NW>
 __global__ void __launch_bounds__(64 * NW)
-cache_few_join(const CacheArgs c, const Few f) {
-  constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8, BK = FEW_BK<D>;
+line_join_row(const CacheArgs c, const Few f) {
+  constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8;
   __shared__ float4 os[NW][PER];
   __shared__ float2 mls[NW];
-  const Line line = line_of<D>(c, f);
+  const Line line = line_of<BK>(c, f);
   if (!line.cut) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kvh = c.pg.kv_heads;
   const int set = lane / PER, col = lane % PER * 4;
@@ -1162,10 +1296,10 @@ cache_few_join(const CacheArgs c, const Few f) {
     int before = __shfl(line.upto, s / line.per) - __shfl(line.mine, s / line.per);
     for (int i = s / line.per * line.per; i < s; ++i) before += Line::count(seq_at<FEW_BQ, BK>(c, i), kvh, true);
     const int r = (tok - q.a) * c.group + head % c.group, qi = r / FEW_BQ;
-    const int a = before + (qi * kvh + head / c.group) * q.nk;
-    const int w0 = line.wave_of(a), ch = line.wave_of(a + q.nk - 1) - w0 + 1;
+    const int a = before + (head / c.group * q.qt + fold_index(qi, q.qt)) * q.nk;
+    const int w0 = line.wg_of(a), ch = line.wg_of(a + q.nk - 1) - w0 + 1;
     if (ch == 1) continue;
-    // the first wave's may be the end of its units, the others' start theirs
+    // the first one's may be the end of its units, the others' start theirs
     const int begins = line.begin(w0) == a;
     auto row_at = [&](int y) -> int64_t {
       return (int64_t)(2 * (w0 + y) + (y == 0 && !begins)) * f.slot_rows + r % FEW_BQ;
@@ -1237,56 +1371,61 @@ cache_few_join(const CacheArgs c, const Few f) {
         x[3] = fmaf(p.w, e, x[3]);
       }
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      bf16_t* op = (bf16_t*)c.o + tok * c.o_ld + head * D + col;
-      *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+      T* op = (T*)c.o + tok * c.o_ld + head * D + col;
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+      else
+        *reinterpret_cast<float4*>(op) = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
       if (c.lse != nullptr && lane == 0) c.lse[id] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
     }
   }
 }
 
-template <int D>
-static void run_few(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
-  constexpr int SLABS = FEW_BK<D> / 8;
-  // One wave to a SIMD, 64 KB in flight on a CU: 8 x 10,160 keys of 24 heads 91 us, 1 x 139,776 of
-  // 4 heads of 128 48, with three to a CU 92 and 48, with five (a SIMD then has two) 116 and 62.
-  constexpr int PER_CU = 4;
+template <typename T, int D>
+static void run_line(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int BK = F32 ? 32 : FEW_BK<D>, SLABS = BK / 8;
   const int64_t rows = (int64_t)c.n_q * c.group;
   Few f{};
   f.slot_rows = (int)std::min<int64_t>(FEW_BQ, rows);
-  f.waves = 256 * PER_CU;
-  f.cut = (int)std::max<int64_t>(0, std::min<int64_t>(f.waves, ws_floats / (2 * (int64_t)f.slot_rows * (D + 2))));
+  // bf16: one wave to a SIMD, 64 KB in flight on a CU: 8 x 10,160 keys of 24 heads 91 us, 1 x 139,776
+  // of 4 heads of 128 48, with three to a CU 92 and 48, with five (a SIMD then has two) 116 and 62.
+  // float32: as many workgroups as the LDS holds.
+  f.wgs = 256 * (!F32 ? 4 : D == 64 ? 2 : 1);
+  f.cut = (int)std::max<int64_t>(0, std::min<int64_t>(f.wgs, ws_floats / (2 * (int64_t)f.slot_rows * (D + 2))));
+  // (the line of tiles is counted in 32 bits)
+  const int64_t tiles = (((int64_t)c.pg.max_pages << c.pg.lg_page) / BK + 1) * c.pg.kv_heads;
+  const int64_t most = (rows + (int64_t)(FEW_BQ - 1) * c.pg.n_seqs) / FEW_BQ;
+  if (tiles >= (1ll << 31) / most) f.cut = 0;
+  // nothing to cut, and no pass to join it, where a table holds two tiles
+  if ((int64_t)c.pg.max_pages << c.pg.lg_page <= 2 * BK) f.cut = 0;
   f.o = ws;
   f.ml = ws + 2 * (int64_t)f.cut * f.slot_rows * D;
+  auto launch = [&](auto run) {
+    constexpr int RUN = decltype(run)::value;
+    if constexpr (F32) hipLaunchKernelGGL((cache_f32<D, RUN>), dim3(f.wgs), dim3(256), 0, st, c, f);
+    else hipLaunchKernelGGL((cache_few<D, RUN>), dim3(f.wgs), dim3(64), 0, st, c, f);
+  };
   const int run = std::min(1 << c.pg.lg_page >> 3, SLABS);
-  if (run == 1) hipLaunchKernelGGL((cache_few<D, 1>), dim3(f.waves), dim3(64), 0, st, c, f);
-  else if (run == 2) hipLaunchKernelGGL((cache_few<D, 2>), dim3(f.waves), dim3(64), 0, st, c, f);
-  else if (run == 4) hipLaunchKernelGGL((cache_few<D, 4>), dim3(f.waves), dim3(64), 0, st, c, f);
-  else hipLaunchKernelGGL((cache_few<D, SLABS>), dim3(f.waves), dim3(64), 0, st, c, f);
+  if (run == 1) launch(std::integral_constant<int, 1>{});
+  else if (run == 2) launch(std::integral_constant<int, 2>{});
+  else if (run == 4) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, SLABS>{});
   if (f.cut) {
-    // few rows have many partial results each
-    const unsigned n = (unsigned)std::min<int64_t>((int64_t)c.n_q * c.heads, 4096);
-    if (n <= 64) hipLaunchKernelGGL((cache_few_join<D, 16>), dim3(n), dim3(1024), 0, st, c, f);
-    else hipLaunchKernelGGL((cache_few_join<D, 4>), dim3(n), dim3(256), 0, st, c, f);
+    const int64_t n = (int64_t)c.n_q * c.heads;
+    if (n <= 64) hipLaunchKernelGGL((line_join_row<T, D, BK, 16>), dim3((unsigned)n), dim3(1024), 0, st, c, f);
+    else if (n <= 512) hipLaunchKernelGGL((line_join_row<T, D, BK, 4>), dim3((unsigned)n), dim3(256), 0, st, c, f);
+    else hipLaunchKernelGGL((line_join<T, D, BK>), dim3(f.cut), dim3(256), 0, st, c, f);
   }
 }
 
-template <typename T, int D>
-static void run_cache(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
-  constexpr bool F32 = sizeof(T) == 4;
-  // few rows to a sequence, by the mean that the host knows (the line of tiles is counted in
-  // 32 bits)
-  if constexpr (!F32) {
-    const int64_t tiles = (((int64_t)c.pg.max_pages << c.pg.lg_page) / FEW_BK<D> + 1) * c.pg.kv_heads;
-    const int64_t most = ((int64_t)c.n_q * c.group + (int64_t)(FEW_BQ - 1) * c.pg.n_seqs) / FEW_BQ;
-    if ((int64_t)c.n_q * c.group <= (int64_t)FEW_BQ * c.pg.n_seqs && tiles < (1ll << 31) / most) {
-      run_few<D>(c, ws, ws_floats, st);
-      return;
-    }
-  }
-  constexpr int BQ = F32 ? 32 : 128, BK = F32 ? 32 : CA_BK;
-  const int kvh = c.pg.kv_heads, group = c.group;
+// bf16 chunks
+template <int D>
+static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
+  constexpr int BQ = 128;
+  const int kvh = c.pg.kv_heads;
   // row tiles at most and at least: the chunks' lengths are on the device
-  const int64_t rows = (int64_t)c.n_q * group;
+  const int64_t rows = (int64_t)c.n_q * c.group;
   const int64_t most = std::min((rows + (int64_t)(BQ - 1) * c.pg.n_seqs) / BQ, rows), least = (rows + BQ - 1) / BQ;
   Split sp{};
   sp.slot_rows = (int)std::min<int64_t>(BQ, rows);
@@ -1302,26 +1441,24 @@ static void run_cache(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
   const int64_t units = most + sp.budget / kvh;
   // a grid holds less than 2^32 threads: more take another launch
   const int64_t step = ((1 << 24) - 1) / kvh;
-  for (int64_t u = 0; u < units; u += step) {
-    const dim3 grid((unsigned)(std::min(units - u, step) * kvh));
-    if constexpr (F32) hipLaunchKernelGGL((cache_f32<D>), grid, dim3(256), 0, st, c, sp, (int)u);
-    else hipLaunchKernelGGL((cache_bf16<D>), grid, dim3(256), 0, st, c, sp, (int)u);
-  }
-  if (sp.budget) {
-    const unsigned n = (unsigned)std::min<int64_t>(((int64_t)c.n_q * c.heads + 3) / 4, 2048);
-    hipLaunchKernelGGL((cache_join<T, D, BQ, BK>), dim3(n), dim3(256), 0, st, c, sp);
-  }
+  for (int64_t u = 0; u < units; u += step)
+    hipLaunchKernelGGL((cache_bf16<D>), dim3((unsigned)(std::min(units - u, step) * kvh)), dim3(256), 0, st, c, sp, (int)u);
+  if (sp.budget)                                // (row tiles below 2,048 + n_seqs here)
+    hipLaunchKernelGGL((cache_join<D>), dim3((unsigned)(most * kvh), (unsigned)((sp.slot_rows + 31) / 32)), dim3(256), 0, st, c, sp);
+}
+
+template <int D>
+static void run_cache(int dtype, const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
+  // few rows to a sequence, by the mean that the host knows
+  if (dtype != 1) run_line<float, D>(c, ws, ws_floats, st);
+  else if ((int64_t)c.n_q * c.group <= (int64_t)FEW_BQ * c.pg.n_seqs) run_line<bf16_t, D>(c, ws, ws_floats, st);
+  else run_chunk<D>(c, ws, ws_floats, st);
 }
 
 hipError_t launch_cache_attention(int dtype, const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
   if (c.n_q <= 0) return hipSuccess;
-  if (dtype == 1) {
-    if (c.dim == 64) run_cache<bf16_t, 64>(c, ws, ws_floats, st);
-    else run_cache<bf16_t, 128>(c, ws, ws_floats, st);
-  } else {
-    if (c.dim == 64) run_cache<float, 64>(c, ws, ws_floats, st);
-    else run_cache<float, 128>(c, ws, ws_floats, st);
-  }
+  if (c.dim == 64) run_cache<64>(dtype, c, ws, ws_floats, st);
+  else run_cache<128>(dtype, c, ws, ws_floats, st);
   return hipGetLastError();
 }
 
