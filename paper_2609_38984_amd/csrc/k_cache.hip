@@ -70,22 +70,28 @@ __device__ __forceinline__ T wave_scan(T v, int n) {
 }
 
 // Tiles of a slice, from the key tiles of all row tiles (`all`, over all K/V heads) and the most of
-// one: modelled time (us) of a workgroup by itself (`lone` a tile) and of several that share a
-// CU, and of the pass that joins the slices.  all / t slices beyond the first are within the
-// budget; a row tile of more than t tiles has fewer than 2 all / t.
-template <int D>
+// one: modelled time (us) of the workgroups, by how many share a CU (`tile`: the time that each
+// takes for a tile then), of what they write, and of the pass that joins the slices.  all / t
+// slices beyond the first are within the budget; a row tile of more than t tiles has
+// fewer than 2 all / t.
+template <int D, int KG>
 __device__ __forceinline__ int slice_tiles(float all, int most, const Split& sp) {
   if (sp.budget == 0) return NO_SPLIT;
-  const float lone = D == 64 ? 1.0f : 1.4f, share = (D == 64 ? 0.64f : 1.0f) / 256.0f * all;
-  const float join = 2.0f * all * (float)sp.slot_rows * (D + 2) * (4.0f / 4.0e6f);
+  const float bytes = all * (float)sp.slot_rows * (D + 2) * 4.0f;     // of one tile to a slice
+  auto time_of = [&](float t) {
+    const float n = all * __builtin_amdgcn_rcpf(t) * (1.0f / 256.0f);   // workgroups to a CU
+    if (KG > 1) return t * (D == 64 ? 0.68f : 1.0f) * fmaxf(n, 1.0f);
+    if (D == 64) return t * (n <= 1.0f ? 1.77f : n <= 2.0f ? 1.89f : n <= 3.0f ? 2.07f : 0.675f * fmaxf(n, 4.0f));
+    return t * (n <= 1.0f ? 1.8f : 1.1f * fmaxf(n, 2.0f));
+  };
   int best = NO_SPLIT;
-  float best_us = fmaxf(lone * (float)most, share);
+  float best_us = time_of((float)most);
   constexpr int PARTS[] = {2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32, 64};
 #pragma unroll
   for (int k = 0; k < (int)(sizeof(PARTS) / sizeof(int)); ++k) {
     const int n = (most + PARTS[k] - 1) / PARTS[k];
     const float t = (float)n;
-    const float us = fmaxf(lone * t, share) + 4.5f + join * __builtin_amdgcn_rcpf(t);
+    const float us = time_of(t) + 6.0f + bytes * (1.0f / 1.6e6f) * __builtin_amdgcn_rcpf(t);
     if (n > 1 && t * (float)sp.budget >= all * 1.0001f + 1.0f && us < best_us) { best_us = us; best = n; }
   }
   return best;
@@ -100,7 +106,7 @@ struct Work {
 };
 // The lanes hold the sequences in order, `per` to a lane; passes over them find the
 // slices' length, the units in front of each, and the one that holds `unit`.
-template <int D, int BQ, int BK>
+template <int D, int KG, int BQ, int BK>
 __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int unit, Work& w) {
   const int lane = threadIdx.x & 63;
   const int per = (c.pg.n_seqs + 63) >> 6, lanes = min(c.pg.n_seqs, 64);
@@ -120,7 +126,7 @@ __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int
     }
     all = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, all)));
     tiles = __builtin_amdgcn_readfirstlane(
-        slice_tiles<D>(all * (float)c.pg.kv_heads, __builtin_amdgcn_readfirstlane(most), sp));
+        slice_tiles<D, KG>(all * (float)c.pg.kv_heads, __builtin_amdgcn_readfirstlane(most), sp));
     if (blockIdx.x == 0 && threadIdx.x == 0) sp.plan[0] = tiles;
   }
   int units = 0, split = 0;
@@ -191,6 +197,28 @@ __device__ __forceinline__ void slice_of(int lo, int hi, int bk, int y, int ch, 
   t1 = t0 + each + (y < more);
 }
 
+// Pages of the runs of RUN 8-key slabs of a tile, -1: none; and which of its keys there are.
+template <int N, int RUN>
+__device__ __forceinline__ void pages_of(const Paged& pg, const_i32* table, int key0, int total, int (&pages)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int key = key0 + 8 * RUN * j;
+    const int p = key < total ? table[key >> pg.lg_page] : -1;
+    pages[j] = p < pg.n_pages ? p : -1;
+  }
+}
+template <int N, int RUN>
+__device__ __forceinline__ uint64_t keys_of(int key0, int total, const int (&pages)[N]) {
+  uint64_t m = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) m |= pages[j] >= 0 ? (~0ull >> (64 - 8 * RUN)) << (8 * RUN * j) : 0ull;
+  const int n = total - key0;
+  return n >= 8 * RUN * N ? m : n <= 0 ? 0ull : m & ((1ull << n) - 1);
+}
+
+// Loads into LDS that this wave has read: its reads have arrived.
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Values that are not finite (bf16, exponent all ones): a weight of zero does not hide them, so
 // where rows see different keys they are left out of the products and added by hand.
 __device__ __forceinline__ uint4 without_odd(uint4 x) {
@@ -207,21 +235,25 @@ __device__ __forceinline__ void add_odd(f32x16& o, int q4, bool sees, uint2 x) {
   for (int e = 0; e < 4; ++e) o[4 * q4 + e] += sees && !(fabsf(f[e]) <= FLT_MAX) ? f[e] : 0.0f;
 }
 
-template <int D>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, 8)))
+// RUN: 8-key slabs that share a page for certain
+// KG: groups of four waves.  Each takes every KG-th tile of the same rows; they meet in LDS.
+template <int D, int RUN, int KG>
+__global__ void __launch_bounds__(256 * KG) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, 8)))
 cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   constexpr int H2 = D / 64;                     // 128-byte halves of a head's row
   constexpr int NW = 4, BQ = 32 * NW;
   constexpr int TILE = CA_BK * 8 * H2;           // uint4 of a K or V tile
-  __shared__ uint4 kv[2][2][TILE];               // [stage][K | V][half][key][8 chunks]
+  constexpr int RUNS = CA_BK / 8 / RUN;
+  __shared__ uint4 kv[KG][2][2][TILE];           // [group][stage][K | V][half][key][8 chunks]
   const int group = c.group;
   // neighbouring workgroups take the K/V heads in turn: with a multiple of 8 of them a
   // head stays on one XCD
   const int hk = blockIdx.x % c.pg.kv_heads;
   Work w;
-  if (!work_at<D, BQ, CA_BK>(c, sp, unit0 + blockIdx.x / c.pg.kv_heads, w)) return;
+  if (!work_at<D, KG, BQ, CA_BK>(c, sp, unit0 + blockIdx.x / c.pg.kv_heads, w)) return;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 8);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;     // of its group
   const int g = lane >> 5, r31 = lane & 31;
   const int r0 = w.qi * BQ, left = w.q.n * group - r0, total = w.q.total;   // rows of the sequence from r0 on
   const Rows row_of(r0, c);
@@ -252,15 +284,8 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     for (int s = 0; s < D / 16; ++s)
       qf[s] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 8 * (2 * s + g)));
   }
-  const int32_t* table = c.pg.table + w.s * c.pg.table_ld;
+  const_i32* table = (const_i32*)(c.pg.table + w.s * c.pg.table_ld);
 
-  // the page of this lane's key of tile t, -1: none
-  auto page_at = [&](int t) -> int {
-    const int key = t * CA_BK + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-    if (t >= t1 || key >= total) return -1;
-    const int p = table[key >> c.pg.lg_page];
-    return p >= 0 && p < c.pg.n_pages ? p : -1;
-  };
   const int lrow = lane >> 3;
   constexpr int SL = 8 * H2 / NW;                // 8-key slabs of a tile that a wave stages
   const int slab0 = wave * SL, key0 = (slab0 & 7) * 8, half = slab0 >> 3;
@@ -273,13 +298,14 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   }
   const bf16_t* k_head = (const bf16_t*)c.pg.k + hk * c.pg.k_head + 64 * half;
   const bf16_t* v_head = (const bf16_t*)c.pg.v + hk * c.pg.v_head + 64 * half;
-  // K and V of tile t into LDS, `pages` of its keys in the lanes; RUN slabs share a page
-  auto issue_runs = [&](uint4 (&to)[2][TILE], int t, int pages, auto run) {
-    constexpr int RUN = decltype(run)::value;
+  // K and V of tile t into LDS, `pages` those of this wave's slabs (always as many loads: what has
+  // no page stores zeros)
+  constexpr int MINE = RUN < SL ? RUN : SL;      // slabs of this wave that share a page
+  auto issue = [&](uint4 (&to)[2][TILE], int t, const int (&pages)[SL / MINE]) {
 #pragma unroll
-    for (int j = 0; j < SL; j += RUN) {
-      const int page = __builtin_amdgcn_readlane(pages, key0 + 8 * j);
-      const int key = t * CA_BK + key0 + 8 * j, n = page < 0 ? 0 : min(total - key, 8 * RUN);
+    for (int j = 0; j < SL; j += MINE) {
+      const int page = pages[j / MINE];
+      const int key = t * CA_BK + key0 + 8 * j, n = page < 0 ? 0 : max(min(total - key, 8 * MINE), 0);
       const int64_t p = max(page, 0);
       const int64_t at = key & ((1 << c.pg.lg_page) - 1);
       const bf16_t* kb = k_head + p * c.pg.k_page + at * c.pg.k_token;
@@ -289,18 +315,13 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
       const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
           (void*)vb, (short)0, n ? ((n - 1) * (int)c.pg.v_token + 64) * 2 : 0, SWAM_BUF_DWORD3);
 #pragma unroll
-      for (int i = 0; i < RUN; ++i) {
-        const int slab = slab0 + j + i, e = RUN == 1 ? 8 * ((j + i) & 1) : -16 * (i >> 1);   // (rows that off_* has beyond the slab's)
-        dma_slab(rk, &to[0][slab * 64], off_k[(j + i) & 1] - e * (int)c.pg.k_token * 2);
-        dma_slab(rv, &to[1][slab * 64], off_v[(j + i) & 1] - e * (int)c.pg.v_token * 2);
+      for (int i = 0; i < MINE; ++i) {
+        // (off_* has 8 rows in front of odd slabs')
+        const int slab = slab0 + j + i, rows = MINE == 1 ? -8 * ((j + i) & 1) : 16 * (i >> 1);
+        dma_slab(rk, &to[0][slab * 64], rows ? vadd_sgpr(off_k[(j + i) & 1], rows * (int)c.pg.k_token * 2) : off_k[(j + i) & 1]);
+        dma_slab(rv, &to[1][slab * 64], rows ? vadd_sgpr(off_v[(j + i) & 1], rows * (int)c.pg.v_token * 2) : off_v[(j + i) & 1]);
       }
     }
-  };
-  auto issue = [&](uint4 (&to)[2][TILE], int t, int pages) {
-    const int run = 1 << c.pg.lg_page >> 3;
-    if (run >= SL) issue_runs(to, t, pages, std::integral_constant<int, SL>{});
-    else if (SL > 2 && run == 2) issue_runs(to, t, pages, std::integral_constant<int, 2>{});
-    else issue_runs(to, t, pages, std::integral_constant<int, 1>{});
   };
   // V^T operand by transposed LDS reads: in each 16-lane group lane a addresses
   // V[key0 + (a >> 2)][col0 + 4 (a & 3)] and lane i receives keys key0..key0+3 of
@@ -394,8 +415,9 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     // the running maximum moves only when a row sum shows that some weight passed
     // 2^8 (or is NaN): the scores are then formed again against the new one
     if (fresh || __any(!(ps0 + ps1 <= 256.0f))) {
-      uint64_t again = vis;
-      asm volatile("" : "+s"(again) : : "memory");
+      uint32_t w0 = __builtin_amdgcn_readfirstlane((uint32_t)vis), w1 = __builtin_amdgcn_readfirstlane((uint32_t)(vis >> 32));
+      asm volatile("" : "+s"(w0), "+s"(w1) : : "memory");
+      const uint64_t again = (uint64_t)w1 << 32 | w0;
       f32x16 st[2];
       scores(st, again);
       float mx = st[0][0];
@@ -460,29 +482,78 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     else products([](uint4 x) { return x; });
   };
 
-  // All waves form the same mask words: that of the tile at hand, of the next, whose loads
-  // run meanwhile, and the pages of the one after it.
-  int pages = page_at(t0), next = page_at(t0 + 1);
-  uint64_t vis = __ballot(pages >= 0);
-  if (vis) issue(kv[0], t0, pages);
+  // The next tile is on its way, with its keys in `ahead`; the pages of the one after it are read
+  // meanwhile.
+  const int stop = min(total, t1 * CA_BK);       // (behind the last tile there are no pages)
+  uint4 (&ring)[2][2][TILE] = kv[kg];
+  int all[RUNS], own[SL / MINE];
+  auto pages_for = [&](int t) {
+    pages_of<RUNS, RUN>(c.pg, table, t * CA_BK, stop, all);
+    pages_of<SL / MINE, MINE>(c.pg, table, t * CA_BK + key0, stop, own);
+  };
+  pages_for(t0 + kg);
+  uint64_t vis = keys_of<RUNS, RUN>((t0 + kg) * CA_BK, total, all);
+  issue(ring[0], t0 + kg, own);
+  pages_for(t0 + kg + KG);
   bool fresh = true;
   int buf = 0;
-  for (int t = t0; t < t1; ++t) {
-    const uint64_t ahead = __ballot(next >= 0);
-    if (vis | ahead) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-    }
-    if (ahead) issue(kv[buf ^ 1], t + 1, next);
-    next = page_at(t + 2);
+#pragma unroll 1
+  for (int tg = t0; tg < t1; tg += KG) {
+    const int t = tg + kg;
+    // the tile at hand has arrived, and every wave is done with the one before it
+    wait_stage<0>();
+    reads_done();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const uint64_t ahead = keys_of<RUNS, RUN>((t + KG) * CA_BK, total, all);
+    issue(ring[buf ^ 1], t + KG, own);
+    pages_for(t + 2 * KG);
     const int k0 = t * CA_BK, k1 = k0 + CA_BK - 1;
     if (vis && k0 <= lim_last && k1 >= low_first) {
       const bool cut = k1 > lim_first, early = k0 < low_last;
-      tile(kv[buf], t, vis, cut || early || vis != ~0ull, (cut && lim_first < total - 1) || early, fresh);
+      tile(ring[buf], t, vis, cut || early || vis != ~0ull, (cut && lim_first < total - 1) || early, fresh);
       fresh = false;
     }
     vis = ahead;
     buf ^= 1;
+  }
+  if constexpr (KG > 1) {
+    // what the other groups have, register by register: the same lanes hold the same rows
+    float* meet = reinterpret_cast<float*>(&kv[0][0][0][0]);
+    constexpr int EACH = (D / 2 + 2) * 64;       // floats of a wave
+    static_assert((KG - 1) * 4 * EACH * 4 <= (int)sizeof(kv), "they fit in the tiles' place");
+    wait_stage<0>();
+    __syncthreads();
+    if (kg > 0) {
+      float* to = meet + ((kg - 1) * 4 + wave) * EACH;
+#pragma unroll
+      for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<float4*>(to + ((4 * ht + q4) * 64 + lane) * 4) =
+              make_float4(o[ht][4 * q4], o[ht][4 * q4 + 1], o[ht][4 * q4 + 2], o[ht][4 * q4 + 3]);
+      *reinterpret_cast<float2*>(to + D / 2 * 64 + 2 * lane) = make_float2(m_run, l_run);
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll 1
+    for (int k = 0; k < KG - 1; ++k) {
+      const float* from = meet + (k * 4 + wave) * EACH;
+      const float2 ml = *reinterpret_cast<const float2*>(from + D / 2 * 64 + 2 * lane);
+      const float m_new = fmaxf(m_run, ml.x), mine = __builtin_amdgcn_exp2f(m_run - m_new), theirs = __builtin_amdgcn_exp2f(ml.x - m_new);
+      m_run = m_new;
+      l_run = l_run * mine + ml.y * theirs;
+#pragma unroll
+      for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const float4 x = *reinterpret_cast<const float4*>(from + ((4 * ht + q4) * 64 + lane) * 4);
+          o[ht][4 * q4] = fmaf(x.x, theirs, o[ht][4 * q4] * mine);
+          o[ht][4 * q4 + 1] = fmaf(x.y, theirs, o[ht][4 * q4 + 1] * mine);
+          o[ht][4 * q4 + 2] = fmaf(x.z, theirs, o[ht][4 * q4 + 2] * mine);
+          o[ht][4 * q4 + 3] = fmaf(x.w, theirs, o[ht][4 * q4 + 3] * mine);
+        }
+    }
   }
   const float l = l_run + __shfl_xor(l_run, 32);
   int me = tid;
@@ -734,27 +805,6 @@ __device__ __forceinline__ Part part_at(const CacheArgs& c, const Line& line, in
 __device__ __forceinline__ int place_of(int wg, int wgs) {
   const int xcd = wg & 7;
   return xcd * (wgs >> 3) + min(xcd, wgs & 7) + (wg >> 3);
-}
-// Loads into LDS that this wave has read: its reads have arrived.
-__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-// Pages of the runs of RUN 8-key slabs of a tile, -1: none; and which of its keys there are.
-template <int N, int RUN>
-__device__ __forceinline__ void pages_of(const Paged& pg, const_i32* table, int key0, int total, int (&pages)[N]) {
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int key = key0 + 8 * RUN * j;
-    const int p = key < total ? table[key >> pg.lg_page] : -1;
-    pages[j] = p < pg.n_pages ? p : -1;
-  }
-}
-template <int N, int RUN>
-__device__ __forceinline__ uint64_t keys_of(int key0, int total, const int (&pages)[N]) {
-  uint64_t m = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) m |= pages[j] >= 0 ? (~0ull >> (64 - 8 * RUN)) << (8 * RUN * j) : 0ull;
-  const int n = total - key0;
-  return n >= 8 * RUN * N ? m : n <= 0 ? 0ull : m & ((1ull << n) - 1);
 }
 
 // bf16, few rows: a workgroup is one wave with a ring of its own in LDS: nothing waits for
@@ -1429,9 +1479,10 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
   const int64_t most = std::min((rows + (int64_t)(BQ - 1) * c.pg.n_seqs) / BQ, rows), least = (rows + BQ - 1) / BQ;
   Split sp{};
   sp.slot_rows = (int)std::min<int64_t>(BQ, rows);
-  // keys are split where the row tiles do not fill the card twice, as far as the
-  // workspace holds the partial results: at most two per slice of the budget
-  if (least * kvh < 2048) {
+  // Keys are split, as far as the workspace holds the partial results (at most two per slice of
+  // the budget), unless the row tiles fill the card: those of one sequence are as long
+  // as each other, those of several may not be.
+  if (least * kvh < (c.pg.n_seqs == 1 ? 192 : 2048)) {
     const int64_t fit = (ws_floats - 64) / (2 * (int64_t)sp.slot_rows * (D + 2));
     sp.budget = (int)std::min<int64_t>(1024, std::max<int64_t>(fit, 0));
     sp.plan = (int*)ws;
@@ -1441,8 +1492,24 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
   const int64_t units = most + sp.budget / kvh;
   // a grid holds less than 2^32 threads: more take another launch
   const int64_t step = ((1 << 24) - 1) / kvh;
-  for (int64_t u = 0; u < units; u += step)
-    hipLaunchKernelGGL((cache_bf16<D>), dim3((unsigned)(std::min(units - u, step) * kvh)), dim3(256), 0, st, c, sp, (int)u);
+  auto launch_with = [&](auto run, auto groups) {
+    constexpr int KG = decltype(groups)::value;
+    for (int64_t u = 0; u < units; u += step)
+      hipLaunchKernelGGL((cache_bf16<D, decltype(run)::value, KG>), dim3((unsigned)(std::min(units - u, step) * kvh)),
+                         dim3(256 * KG), 0, st, c, sp, (int)u);
+  };
+  // Few row tiles: one workgroup to a CU that takes several key tiles at once, as many as the LDS
+  // holds.
+  auto launch = [&](auto run) {
+    if (most * kvh <= 640) launch_with(run, std::integral_constant<int, D == 64 ? 4 : 2>{});
+    else launch_with(run, std::integral_constant<int, 1>{});
+  };
+  switch (std::min(c.pg.lg_page, 6)) {
+    case 3: launch(std::integral_constant<int, 1>{}); break;
+    case 4: launch(std::integral_constant<int, 2>{}); break;
+    case 5: launch(std::integral_constant<int, 4>{}); break;
+    default: launch(std::integral_constant<int, 8>{});
+  }
   if (sp.budget)                                // (row tiles below 2,048 + n_seqs here)
     hipLaunchKernelGGL((cache_join<D>), dim3((unsigned)(most * kvh), (unsigned)((sp.slot_rows + 31) / 32)), dim3(256), 0, st, c, sp);
 }
