@@ -517,12 +517,12 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     vis = ahead;
     buf ^= 1;
   }
+  wait_stage<0>();
   if constexpr (KG > 1) {
     // what the other groups have, register by register: the same lanes hold the same rows
     float* meet = reinterpret_cast<float*>(&kv[0][0][0][0]);
     constexpr int EACH = (D / 2 + 2) * 64;       // floats of a wave
     static_assert((KG - 1) * 4 * EACH * 4 <= (int)sizeof(kv), "they fit in the tiles' place");
-    wait_stage<0>();
     __syncthreads();
     if (kg > 0) {
       float* to = meet + ((kg - 1) * 4 + wave) * EACH;

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libswam (include/swam.h).
+"""Thin ctypes binding of libswam (include/swam.h, swam_ops.h and swam_cache.h).
 
 Argument marshalling only: tensors are checked for device, dtype, size and
 contiguity, then their device pointers are passed to the C ABI.  Every step of
@@ -316,26 +316,28 @@ class QkPost:
 
     def __init__(self, norm: bool = True, eps: float = 1e-6, q_gain=None, k_gain=None, rope: Rope | None = None):
         self.q_gain, self.k_gain, self.rope = q_gain, k_gain, rope
-        held = [t for t in (q_gain, k_gain, None if rope is None else rope.freq) if t is not None]
-        self.devices = {t.get_device() for t in held if isinstance(t, torch.Tensor)}
-        self.act_dtypes = {t.dtype for t in (q_gain, k_gain) if isinstance(t, torch.Tensor)}
-        self.gain_dims = {t.numel() for t in (q_gain, k_gain) if isinstance(t, torch.Tensor)}
         self.struct = QkPostStruct(int(bool(norm)), float(eps), _ptr(q_gain, name="q_gain"), _ptr(k_gain, name="k_gain"))
         if rope is not None:
             self.struct.rope_dims = 2 * rope.freq.numel()
             self.struct.rope_layout = ROPE_LAYOUTS[rope.layout]
             self.struct.rope_freq = rope.freq.data_ptr()
             self.struct.rope_magnitude = rope.magnitude
+        self._ref, self._fits = C.byref(self.struct), None
 
     def _for(self, act, dim, device):
-        """The descriptor, once its tensors fit the call."""
-        if any(d != device for d in self.devices):
-            raise ValueError(f"post is on GPU {self.devices}, the context on {device}")
-        if any(t is not act for t in self.act_dtypes):
-            raise TypeError(f"gains must be {act}, got {self.act_dtypes}")
-        if any(n != dim for n in self.gain_dims):
-            raise ValueError(f"gains have {self.gain_dims} elements, need {dim}")
-        return C.byref(self.struct)
+        """The descriptor, once its tensors fit the call (what fitted the last one does)."""
+        if self._fits != (act, dim, device):
+            for name in ("q_gain", "k_gain"):
+                t = getattr(self, name)
+                if t is not None:
+                    if t.dtype is not act or t.get_device() != device:
+                        _refuse(t, act, name, device)
+                    if t.numel() != dim:
+                        raise ValueError(f"{name} has {t.numel()} elements, needs {dim}")
+            if self.rope is not None and self.rope.freq.get_device() != device:
+                _refuse(self.rope.freq, torch.float64, "freq", device)
+            self._fits = (act, dim, device)
+        return self._ref
 
 
 class Cache:
@@ -368,6 +370,7 @@ class Cache:
         ks, vs = ([st if n > 1 else 0 for n, st in zip(t.shape, t.stride())] for t in (k, v))
         self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), *ks[:3], *vs[:3], n_pages, page, self.kv_heads,
                                   self.head_dim, n_seqs, max_pages, ts, tp, lp)
+        self._ref = C.byref(self.struct)
 
     def _for(self, act, device, cu):
         """The descriptor, once the cache and the offsets fit the call."""
@@ -377,7 +380,7 @@ class Cache:
             raise ValueError(f"the cache is on GPU {self.device}, the context on {device}")
         if cu is not None and cu.numel() != self.n_seqs + 1:
             raise ValueError(f"cu has {cu.numel()} elements, needs {self.n_seqs + 1}")
-        return C.byref(self.struct)
+        return self._ref
 
 
 NOALLOC_SCRATCH_BYTES = 1 << 20   # SWAM_NOALLOC_SCRATCH_BYTES

@@ -814,3 +814,72 @@ def test_steps_and_cache_calls_share_a_context(contexts):
     for a, b in zip(*outs):
         assert torch.equal(a, b)
     assert ctx.timer_read("HEAD_POST")[0] == 1 and ctx.timer_read("APPEND")[0] == 4 and ctx.timer_read("CACHE_ATTN")[0] == 4
+
+
+# ---------------------------------------------------------------------------
+# every form of the kernels
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page", [8, 16, 32, 64, 128])
+@pytest.mark.parametrize("new,old", [([1, 1, 1], [700, 5, 2100]), ([20, 3], [333, 1500]), ([90, 200], [700, 61]), ([33], [0])])
+def test_every_page_size(contexts, dtype, dim, page, new, old):
+    """Loads of 8, 16, 32 and 64 keys to a page, for few rows and for chunks."""
+    run_cache_attention(contexts[dtype], TYPES[dtype], new, old, 4, 2, dim, page, True, 0, page + dim)
+    run_cache_attention(contexts[dtype], TYPES[dtype], new, old, 3, 3, dim, page, False, 150, page)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("new,old,heads,kvh,dim", [
+    ([1500], [0], 56, 56, 64),                              # more row tiles than groups of waves take
+    ([700, 300], [0, 900], 80, 80, 64),
+    ([900], [300], 70, 70, 128),
+    ([1300], [200], 24, 24, 64),                            # one sequence that fills the card unsplit
+    ([1] * 40, [3000] + [40] * 38 + [1200], 16, 16, 64),     # cut lines of many rows
+    ([2] * 30, [2500, 9] * 15, 32, 4, 128),
+    ([1] * 100, [4000] + [(31 * i) % 300 for i in range(99)], 4, 2, 64),    # two sequences to a lane
+    ([(13 * i) % 60 + 40 for i in range(80)], [3000] + [(17 * i) % 200 for i in range(79)], 2, 1, 64),
+    ([1] * 300, [(41 * i) % 700 for i in range(300)], 2, 1, 128),
+    ([1], [20000], 4, 1, 64), ([3, 1], [15000, 9], 8, 1, 128)])
+def test_many_rows_long_lines_and_many_sequences(contexts, dtype, new, old, heads, kvh, dim):
+    for causal, window in ((True, 0), (False, 0), (True, 700)):
+        run_cache_attention(contexts[dtype], TYPES[dtype], new, old, heads, kvh, dim, 16, causal, window, heads + dim)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("new,old", [([1, 1], [5000, 300]), ([200], [3000]), ([30, 2], [900, 2000])])
+def test_workspaces_of_any_size(dtype, new, old):
+    """A context of one narrow block holds partial results of few slices, and one of a single
+    short sequence of next to none; both give what the large one gives, within the bounds."""
+    from paper_2609_38984_amd import swam
+    for cfg in (W.preset(1).replace(dtype=dtype), W.preset(1).replace(dtype=dtype, d_model=64, n_heads=1),
+                W.preset(1).replace(dtype=dtype, d_model=64, n_heads=1, n_ctx=0, n_frames=1, frame_h=2, frame_w=2, n_act=1, k_core=2,
+                                    k_anchor=1)):
+        ctx = swam.Context(cfg)
+        for heads, kvh, dim in ((8, 2, 128), (6, 6, 64)):
+            run_cache_attention(ctx, TYPES[dtype], new, old, heads, kvh, dim, 16, seed=3)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_strided_tables_shared_pages_and_repeated_sequences(contexts, dtype):
+    """A table that is a column range of a wider one, a prompt whose pages several sequences
+    share, and a page that stands in a table twice."""
+    from paper_2609_38984_amd import swam
+    dt, g = TYPES[dtype], gen(77)
+    n, page, kvh = 12, 16, 2
+    k, v = (torch.randn((n, page, kvh, 64), device="cuda", generator=g).to(dt) for _ in range(2))
+    wide = torch.full((3, 9), 1 << 30, dtype=torch.int32, device="cuda")
+    wide[:, 2:7] = torch.tensor([[0, 1, 2, 3, 4], [0, 1, 5, 5, 6], [0, 1, 7, 8, 9]], device="cuda")
+    table = wide[:, 2:7]
+    length = torch.tensor([70, 60, 33], dtype=torch.int32, device="cuda")
+    cache = swam.Cache(k, v, table, length)
+    new = [3, 1, 40]
+    q, _ = rows_of((44, 4, 64), dt, g)
+    o, lse = torch.empty_like(q), torch.empty((44, 4), device="cuda")
+    contexts[dtype].cache_attention(cache, q, o, cu=offsets(new), lse=lse)
+
+    class C:
+        lengths = [70, 60, 33]
+        where = staticmethod(lambda s, j: (table[s].long()[j // page], j % page))
+    C.kvh, C.k, C.v = kvh, k, v
+    check_cache_attention(C, q, o, lse, new, True, 0, 0.125, o, lse)
