@@ -366,15 +366,16 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     const uint4* Kt = from[0];
     auto scores = [&](f32x16 (&st)[2], uint64_t vis) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[t][r] = 0.0f;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
+      for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
           const bf16x8 kf = __builtin_bit_cast(bf16x8, Kt[(s >> 2) * CA_BK * 8 + kofs[s & 3] + t * 32 * 8]);
           st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[t], 0, 0, 0);
         }
-      }
       if (part) {
         // register r holds key 8 (r >> 2) + 4 g + (r & 3) of its half.  (A branch: no tile
         // but the first and last of a row needs these)
@@ -469,11 +470,11 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     }
     auto products = [&](auto clean) {
 #pragma unroll
-      for (int ht = 0; ht < D / 32; ++ht)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
+          for (int ht = 0; ht < D / 32; ++ht) {
             const uint4 x = clean(v_operand(vs, ht, t, u));
             o[ht] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf[t][u], o[ht], 0, 0, 0);
           }
@@ -599,11 +600,11 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
 }
 
 // Adds up the `ch` partial results of rows [r0, r1) of a row tile, slot_at(y) the slot of the
-// y-th, in their order.  A wave takes 256 / D rows at a time, eight slices on their way.
-template <typename T, int D, typename SlotAt>
+// y-th, in their order.  A wave takes 256 / D rows at a time, AHEAD slices on their way.
+template <typename T, int D, int AHEAD, typename SlotAt>
 __device__ __forceinline__ void join_rows(const CacheArgs& c, const float* po, const float* pml, int slot_rows, int ch,
                                           int a, int hk, const Rows& row_of, int r0, int r1, SlotAt slot_at) {
-  constexpr int PER = D / 4, SETS = 64 / PER, AHEAD = 8;
+  constexpr int PER = D / 4, SETS = 64 / PER;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % PER * 4;
   for (int rb = r0 + wave * SETS; rb < r1; rb += 4 * SETS) {
     const int r = min(rb + lane / PER, r1 - 1);
@@ -689,7 +690,7 @@ cache_join(const CacheArgs c, const Split sp) {
   const Rows row_of(qi * BQ, c);
   // (the workgroups count the row tiles from the last)
   const int first = units + (q.qt - 1 - qi) * ch;
-  join_rows<bf16_t, D>(c, sp.o, sp.ml, sp.slot_rows, ch, q.a, hk, row_of, (int)blockIdx.y * 32,
+  join_rows<bf16_t, D, 8>(c, sp.o, sp.ml, sp.slot_rows, ch, q.a, hk, row_of, (int)blockIdx.y * 32,
                        min(left, (int)blockIdx.y * 32 + 32), [&](int y) { return (first + y) * kvh + hk; });
 }
 
@@ -1077,10 +1078,10 @@ cache_f32(const CacheArgs c, const Few f) {
   constexpr int H2 = D / 64, BK = 32, SLABS = BK / 8, RUNS = SLABS / RUN;
   constexpr int TILE = BK * 16 * H2;             // float4 of a K or V tile
   constexpr int NI = 8 * H2;                     // loads of one
-  constexpr int LD = D + 4;
-  __shared__ float4 kv[4][2][TILE];              // [wave][K | V][half][key][16 chunks]
-  __shared__ float ms[4][32], ls[4][32];
-  static_assert(sizeof(kv) >= 4 * 32 * LD * 4, "the waves meet in the tiles' place");
+  constexpr int LD = D + 4, NW = 4;
+  __shared__ float4 kv[NW][2][TILE];             // [wave][K | V][half][key][16 chunks]
+  __shared__ float ms[NW][32], ls[NW][32];
+  static_assert(sizeof(kv) >= NW * 32 * LD * 4, "the waves meet in the tiles' place");
   float (*os)[32][LD] = reinterpret_cast<float (*)[32][LD]>(&kv[0][0][0]);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, r31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1163,11 +1164,11 @@ cache_f32(const CacheArgs c, const Few f) {
     pages_of<RUNS, RUN>(c.pg, table, (t0 + wave) * BK, stop, pages);
     issue(false, t0 + wave, pages);
 #pragma unroll 1
-    for (int t = t0 + wave; t < t1; t += 4) {
+    for (int t = t0 + wave; t < t1; t += NW) {
       const int k0 = t * BK;
       reads_done();
       issue(true, t, pages);
-      pages_of<RUNS, RUN>(c.pg, table, k0 + 4 * BK, stop, ahead);
+      pages_of<RUNS, RUN>(c.pg, table, k0 + NW * BK, stop, ahead);
       const uint32_t vis = (uint32_t)keys_of<RUNS, RUN>(k0, total, pages);
       wait_stage<NI>();
       f32x16 st;
@@ -1182,7 +1183,7 @@ cache_f32(const CacheArgs c, const Few f) {
         st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.w, qf[s][3], st, 0, 0, 0);
       }
       reads_done();
-      issue(false, t + 4, ahead);
+      issue(false, t + NW, ahead);
 #pragma unroll
       for (int j = 0; j < RUNS; ++j) pages[j] = ahead[j];
       // the keys that this lane's row sees
@@ -1270,14 +1271,15 @@ cache_f32(const CacheArgs c, const Few f) {
         *reinterpret_cast<float4*>(&os[wave][r31][32 * t + 8 * q4 + 4 * g]) =
             make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
     __syncthreads();
-    const int row = tid >> 3;
-    if (row < left) {
+    for (int row = tid >> 3; row < left; row += 8 * NW) {
       const int64_t tok = q.a + row_of.token(row);
       const int head = hk * c.group + row_of.head(row);
-      const float mt = fmaxf(fmaxf(ms[0][row], ms[1][row]), fmaxf(ms[2][row], ms[3][row]));
-      float e4[4], lt = 0.0f;
+      float mt = ms[0][row];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
+      for (int v = 1; v < NW; ++v) mt = fmaxf(mt, ms[v][row]);
+      float e4[NW], lt = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
         e4[v] = exp2f(ms[v][row] - mt);
         lt = fmaf(ls[v][row], e4[v], lt);
       }
@@ -1292,7 +1294,7 @@ cache_f32(const CacheArgs c, const Few f) {
         for (int e = 0; e < 8; ++e) {
           acc[e] = 0.0f;
 #pragma unroll
-          for (int v = 0; v < 4; ++v) acc[e] = fmaf(os[v][row][col + e], e4[v], acc[e]);
+          for (int v = 0; v < NW; ++v) acc[e] = fmaf(os[v][row][col + e], e4[v], acc[e]);
           acc[e] *= inv;
         }
         store8(dst + col, acc);
@@ -1321,8 +1323,9 @@ line_join(const CacheArgs c, const Few f) {
   const int ch = line.wg_of(start + p.q.nk - 1) - j + 1, left = min(p.q.n * c.group - p.r0, FEW_BQ);
   const Rows row_of(p.r0, c);
   // j's may be the end of its units, the others' start theirs
-  join_rows<T, D>(c, f.o, f.ml, f.slot_rows, ch, p.q.a, p.hk, row_of, 0, left,
-                  [&](int y) { return 2 * (j + y) + (y == 0 && start != begin); });
+  auto slot_at = [&](int y) { return 2 * (j + y) + (y == 0 && start != begin); };
+  if (ch > 8) join_rows<T, D, 16>(c, f.o, f.ml, f.slot_rows, ch, p.q.a, p.hk, row_of, 0, left, slot_at);
+  else join_rows<T, D, 8>(c, f.o, f.ml, f.slot_rows, ch, p.q.a, p.hk, row_of, 0, left, slot_at);
 }
 // The same for few rows, which have many partial results each: a workgroup of NW waves per
 // token and head, each wave every NW-th group of them.
@@ -1516,9 +1519,15 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
 
 template <int D>
 static void run_cache(int dtype, const CacheArgs& c, float* ws, int64_t ws_floats, hipStream_t st) {
-  // few rows to a sequence, by the mean that the host knows
+  // Few rows to a sequence, by the mean that the host knows; also twice as many where there are few
+  // row tiles in all, which the line cuts finer: one chunk of 64 rows behind 10,000 keys, 3 heads of 128,
+  // 27 us on the line and 53 in slices, 24 heads of 64 43 and 47; eight such of 24 heads behind
+  // 2,000 55 and 42.
+  const int64_t rows = (int64_t)c.n_q * c.group;
+  const bool few = rows <= (int64_t)FEW_BQ * c.pg.n_seqs ||
+                   (rows <= 2 * (int64_t)FEW_BQ * c.pg.n_seqs && rows * c.pg.kv_heads <= FEW_BQ * 128);
   if (dtype != 1) run_line<float, D>(c, ws, ws_floats, st);
-  else if ((int64_t)c.n_q * c.group <= (int64_t)FEW_BQ * c.pg.n_seqs) run_line<bf16_t, D>(c, ws, ws_floats, st);
+  else if (few) run_line<bf16_t, D>(c, ws, ws_floats, st);
   else run_chunk<D>(c, ws, ws_floats, st);
 }
 
