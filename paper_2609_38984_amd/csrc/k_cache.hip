@@ -160,6 +160,8 @@ __device__ __forceinline__ bool work_at(const CacheArgs& c, const Split& sp, int
   auto bcast = [&](int& v) { v = __builtin_amdgcn_readlane(v, b); };
   bcast(w.q.a); bcast(w.q.n); bcast(w.q.old); bcast(w.q.total); bcast(w.q.qt); bcast(w.q.nk);
   bcast(w.s); bcast(w.ch); bcast(w.slot); bcast(r);
+  // (sequences that overlap against the contract can pass what 32 bits count: nothing is done then)
+  if (w.ch == 0 || (w.ch > 1 && (uint32_t)w.slot >= (uint32_t)(2 * sp.budget / c.pg.kv_heads))) return false;
   // the last rows of a causal chunk see most: they come first
   const int qi = w.ch == 1 ? r : r / w.ch;
   w.qi = w.q.qt - 1 - qi;
@@ -690,6 +692,7 @@ cache_join(const CacheArgs c, const Split sp) {
   const Rows row_of(qi * BQ, c);
   // (the workgroups count the row tiles from the last)
   const int first = units + (q.qt - 1 - qi) * ch;
+  if (first < 0 || first + ch > 2 * sp.budget / kvh) return;
   join_rows<bf16_t, D, 8>(c, sp.o, sp.ml, sp.slot_rows, ch, q.a, hk, row_of, (int)blockIdx.y * 32,
                        min(left, (int)blockIdx.y * 32 + 32), [&](int y) { return (first + y) * kvh + hk; });
 }
@@ -737,28 +740,36 @@ __device__ __forceinline__ Line line_of(const CacheArgs& c, const Few& f) {
   const int lane = threadIdx.x & 63, lanes = min(c.pg.n_seqs, 64), kvh = c.pg.kv_heads;
   Line l;
   l.per = (c.pg.n_seqs + 63) >> 6;
-  int tiles = 0, segs = 0, most = 0;
+  // (in 64 bits: sequences that overlap against the contract can pass what 32 bits count, and
+  // nothing is done then)
+  int64_t tiles = 0, segs = 0;
+  int most = 0;
   l.first = seq_at<FEW_BQ, BK>(c, lane * l.per);
   for (int i = 0; i < l.per; ++i) {
     const Seq q = i == 0 ? l.first : seq_at<FEW_BQ, BK>(c, lane * l.per + i);
-    if (f.cut) tiles += Line::count(q, kvh, true);
-    segs += Line::count(q, kvh, false);
+    if (f.cut) tiles += (int64_t)q.qt * kvh * q.nk;
+    segs += (int64_t)q.qt * kvh;
     most = max(most, q.nk);
   }
-  const int tiles_upto = wave_scan(tiles, lanes), segs_upto = wave_scan(segs, lanes);
+  const int64_t tiles_upto = wave_scan(tiles, lanes), segs_upto = wave_scan(segs, lanes);
   for (int o = 1; o < lanes; o <<= 1) most = max(most, __shfl_xor(most, o));
-  const int n_tiles = __builtin_amdgcn_readlane(tiles_upto, lanes - 1);
-  const int n_segs = __builtin_amdgcn_readlane(segs_upto, lanes - 1);
+  auto last = [&](int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, lanes - 1), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), lanes - 1);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+  };
+  constexpr int64_t MOST = 1 << 30;
+  const int n_segs = last(segs_upto) < MOST ? (int)last(segs_upto) : 0;
+  const int n_tiles = last(tiles_upto) < MOST ? (int)last(tiles_upto) : 0;
   most = __builtin_amdgcn_readfirstlane(most);
   // cut where that saves the time of more tiles than the joining pass adds
-  const int cut_wgs = min(f.cut, (n_tiles + 1) / 2);
+  const int cut_wgs = n_segs > 0 ? min(f.cut, (n_tiles + 1) / 2) : 0;
   l.cut = false;
   if (cut_wgs > 0) {
     const int whole = (n_segs + f.wgs - 1) / f.wgs * most, each = (n_tiles + cut_wgs - 1) / cut_wgs;
     l.cut = whole > each + 2;
   }
-  l.mine = l.cut ? tiles : segs;
-  l.upto = l.cut ? tiles_upto : segs_upto;
+  l.mine = (int)(l.cut ? tiles : segs);
+  l.upto = (int)(l.cut ? tiles_upto : segs_upto);
   l.all = l.cut ? n_tiles : n_segs;
   l.wgs = l.cut ? cut_wgs : min(f.wgs, max(n_segs, 1));
   return l;
@@ -1446,10 +1457,6 @@ static void run_line(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream
   // float32: as many workgroups as the LDS holds.
   f.wgs = 256 * (!F32 ? 4 : D == 64 ? 2 : 1);
   f.cut = (int)std::max<int64_t>(0, std::min<int64_t>(f.wgs, ws_floats / (2 * (int64_t)f.slot_rows * (D + 2))));
-  // (the line of tiles is counted in 32 bits)
-  const int64_t tiles = (((int64_t)c.pg.max_pages << c.pg.lg_page) / BK + 1) * c.pg.kv_heads;
-  const int64_t most = (rows + (int64_t)(FEW_BQ - 1) * c.pg.n_seqs) / FEW_BQ;
-  if (tiles >= (1ll << 31) / most) f.cut = 0;
   // nothing to cut, and no pass to join it, where a table holds two tiles
   if ((int64_t)c.pg.max_pages << c.pg.lg_page <= 2 * BK) f.cut = 0;
   f.o = ws;
