@@ -1100,11 +1100,13 @@ cache_f32(const CacheArgs c, const Few f) {
   constexpr int H2 = D / 64, BK = 32, SLABS = BK / 8, RUNS = SLABS / RUN;
   constexpr int TILE = BK * 16 * H2;             // float4 of a K or V tile
   constexpr int NI = 8 * H2;                     // loads of one
-  constexpr int LD = D + 4, NW = 4;
+  constexpr int NW = 4;
   __shared__ float4 kv[NW][2][TILE];             // [wave][K | V][half][key][16 chunks]
   __shared__ float ms[NW][32], ls[NW][32];
-  static_assert(sizeof(kv) >= NW * 32 * LD * 4, "the waves meet in the tiles' place");
-  float (*os)[32][LD] = reinterpret_cast<float (*)[32][LD]>(&kv[0][0][0]);
+  // a part's sums meet in the places of V while the next part's first K is on its way: row r's chunk x
+  // in place x ^ (r & 15)
+  static_assert(TILE == 32 * D / 4, "a wave's sums fill its V tile");
+  auto sum_at = [&](int w, int row, int x) -> float4& { return kv[w][1][(x >> 4) * 512 + row * 16 + ((x ^ row) & 15)]; };
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, r31 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Line line = line_of<BK>(c, f);
@@ -1119,7 +1121,47 @@ cache_f32(const CacheArgs c, const Few f) {
   const int vofs[2] = {4 * g * 64 + r31 + 32 * g, 4 * g * 64 + r31 + 32 * (g ^ 1)};
   const float sc = LOG2E * c.scale;
 
-  for (int unit = first; unit < end;) {
+  // the part whose sums wait in LDS
+  struct { int a, hk, left, slot; bool whole; Rows rows; } last{0, 0, 0, 0, false, Rows(0, c)};
+  int unit = first;
+  auto join = [&]() {
+    __syncthreads();                             // the waves' sums are there
+    for (int row = tid >> 3; row < last.left; row += 8 * NW) {
+      const int64_t tok = last.a + last.rows.token(row);
+      const int head = last.hk * c.group + last.rows.head(row);
+      float mt = ms[0][row];
+#pragma unroll
+      for (int v = 1; v < NW; ++v) mt = fmaxf(mt, ms[v][row]);
+      float e4[NW], lt = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        e4[v] = exp2f(ms[v][row] - mt);
+        lt = fmaf(ls[v][row], e4[v], lt);
+      }
+      const int64_t at = (int64_t)last.slot * f.slot_rows + row;
+      const float inv = !last.whole ? 1.0f : lt == 0.0f ? 0.0f : 1.0f / lt;
+      float* dst = last.whole ? (float*)c.o + tok * c.o_ld + head * D : f.o + at * D;
+#pragma unroll
+      for (int x = tid & 7; x < D / 4; x += 8) {
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+          const float4 y = sum_at(v, row, x);
+          acc[0] = fmaf(y.x, e4[v], acc[0]);
+          acc[1] = fmaf(y.y, e4[v], acc[1]);
+          acc[2] = fmaf(y.z, e4[v], acc[2]);
+          acc[3] = fmaf(y.w, e4[v], acc[3]);
+        }
+        *reinterpret_cast<float4*>(dst + 4 * x) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      }
+      if ((tid & 7) == 0) {
+        if (!last.whole) *reinterpret_cast<float2*>(f.ml + at * 2) = make_float2(mt, lt);
+        else if (c.lse != nullptr) c.lse[tok * c.heads + head] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * LN2;
+      }
+    }
+    __syncthreads();                             // V's places are free again
+  };
+  while (unit < end) {
     const Part p = part_at<BK>(c, line, unit, end);
     const Seq& q = p.q;
     const int slot = 2 * wid + (unit != first);
@@ -1172,19 +1214,19 @@ cache_f32(const CacheArgs c, const Few f) {
 #pragma unroll
       for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4*>(qp + 4 * (2 * s + g));
     }
-    f32x16 o[D / 32];
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-    float m = -FLT_MAX, l = 0.0f;
-
     const float4* Kt = kv[wave][0];
     const float4* Vt = kv[wave][1];
     const int stop = min(total, t1 * BK);
     int pages[RUNS], ahead[RUNS];
     pages_of<RUNS, RUN>(c.pg, table, (t0 + wave) * BK, stop, pages);
     issue(false, t0 + wave, pages);
+    if (slot != 2 * wid) join();
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+    float m = -FLT_MAX, l = 0.0f;
 #pragma unroll 1
     for (int t = t0 + wave; t < t1; t += NW) {
       const int k0 = t * BK;
@@ -1284,50 +1326,15 @@ cache_f32(const CacheArgs c, const Few f) {
     }
     wait_stage<0>();
     l += __shfl_xor(l, 32);
-    __syncthreads();                             // the tiles are read
     if (g == 0) { ms[wave][r31] = m; ls[wave][r31] = l; }
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<float4*>(&os[wave][r31][32 * t + 8 * q4 + 4 * g]) =
-            make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
-    __syncthreads();
-    for (int row = tid >> 3; row < left; row += 8 * NW) {
-      const int64_t tok = q.a + row_of.token(row);
-      const int head = hk * c.group + row_of.head(row);
-      float mt = ms[0][row];
-#pragma unroll
-      for (int v = 1; v < NW; ++v) mt = fmaxf(mt, ms[v][row]);
-      float e4[NW], lt = 0.0f;
-#pragma unroll
-      for (int v = 0; v < NW; ++v) {
-        e4[v] = exp2f(ms[v][row] - mt);
-        lt = fmaf(ls[v][row], e4[v], lt);
-      }
-      const int64_t at = (int64_t)slot * f.slot_rows + row;
-      const float inv = !p.whole ? 1.0f : lt == 0.0f ? 0.0f : 1.0f / lt;
-      float* dst = p.whole ? (float*)c.o + tok * c.o_ld + head * D : f.o + at * D;
-#pragma unroll
-      for (int h = 0; h < D / 64; ++h) {
-        const int col = 64 * h + (tid & 7) * 8;
-        float acc[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          acc[e] = 0.0f;
-#pragma unroll
-          for (int v = 0; v < NW; ++v) acc[e] = fmaf(os[v][row][col + e], e4[v], acc[e]);
-          acc[e] *= inv;
-        }
-        store8(dst + col, acc);
-      }
-      if ((tid & 7) == 0) {
-        if (!p.whole) *reinterpret_cast<float2*>(f.ml + at * 2) = make_float2(mt, lt);
-        else if (c.lse != nullptr) c.lse[tok * c.heads + head] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * LN2;
-      }
-    }
-    __syncthreads();                             // the tiles' place is free again
+        sum_at(wave, r31, 8 * t + 2 * q4 + g) = make_float4(o[t][4 * q4], o[t][4 * q4 + 1], o[t][4 * q4 + 2], o[t][4 * q4 + 3]);
+    last = {q.a, hk, left, slot, p.whole, row_of};
   }
+  join();
 }
 
 // The segment that the border behind workgroup j's units cuts, where j has its start: a
