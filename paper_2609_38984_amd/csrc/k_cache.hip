@@ -708,16 +708,25 @@ cache_join(const CacheArgs c, const Split sp) {
 // Single tokens and short chunks read K and V once and their bytes are the time; in float32 the
 // matrix unit is slow enough for small row tiles.  There all key tiles of all (sequence, K/V
 // head, row tile) segments stand in one line that is cut evenly over the workgroups, so
-// unequal lengths cost nothing; a segment cut by a border leaves partial results, at most two
-// to a workgroup.
+// unequal lengths cost nothing (a segment counts a few more for its start and end); a segment cut by a
+// border leaves partial results, at most two to a workgroup.
 struct Few {
   float* o;           // [2 wgs][slot_rows][head_dim] sums
   float* ml;          // [2 wgs][slot_rows] (maximum, sum)
   int wgs;            // of the launch
   int cut;            // workgroups that tiles may be cut over, 0: segments stay whole
   int slot_rows;
+  int extra;          // tiles that a segment's start and end are worth
 };
 constexpr int FEW_BQ = 32;
+
+// a sequence with the units of its segments for key tiles
+template <int BK>
+__device__ __forceinline__ Seq line_seq(const CacheArgs& c, const Few& f, int s) {
+  Seq q = seq_at<FEW_BQ, BK>(c, s);
+  if (q.nk) q.nk += f.extra;
+  return q;
+}
 
 // The line of tiles (or of whole segments) as the lanes hold it, `per` sequences to a lane.
 struct Line {
@@ -749,9 +758,9 @@ __device__ __forceinline__ Line line_of(const CacheArgs& c, const Few& f) {
   // nothing is done then)
   int64_t tiles = 0, segs = 0;
   int most = 0;
-  l.first = seq_at<FEW_BQ, BK>(c, lane * l.per);
+  l.first = line_seq<BK>(c, f, lane * l.per);
   for (int i = 0; i < l.per; ++i) {
-    const Seq q = i == 0 ? l.first : seq_at<FEW_BQ, BK>(c, lane * l.per + i);
+    const Seq q = i == 0 ? l.first : line_seq<BK>(c, f, lane * l.per + i);
     if (f.cut) tiles += (int64_t)q.qt * kvh * q.nk;
     segs += (int64_t)q.qt * kvh;
     most = max(most, q.nk);
@@ -785,7 +794,8 @@ __device__ __forceinline__ Line line_of(const CacheArgs& c, const Few& f) {
 __device__ __forceinline__ int folded(int i, int n) { return i & 1 ? n - 1 - (i >> 1) : i >> 1; }
 __device__ __forceinline__ int fold_index(int tile, int n) { return 2 * tile < n ? 2 * tile : 2 * (n - 1 - tile) + 1; }
 
-// The part of the line that starts at `unit`: tiles [from, upto) of one segment.
+// The part of the line that starts at `unit`: units [from, upto) of one segment, the first `extra` of
+// which hold no tile.
 struct Part {
   Seq q;
   int seq, hk, r0;    // sequence, K/V head, first row
@@ -793,7 +803,7 @@ struct Part {
   bool whole;
 };
 template <int BK>
-__device__ __forceinline__ Part part_at(const CacheArgs& c, const Line& line, int unit, int end) {
+__device__ __forceinline__ Part part_at(const CacheArgs& c, const Few& f, const Line& line, int unit, int end) {
   const int kvh = c.pg.kv_heads;
   Part p;
   const int b = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(line.upto > unit)) - 1);
@@ -803,7 +813,7 @@ __device__ __forceinline__ Part part_at(const CacheArgs& c, const Line& line, in
         held(line.first.nk)};
   for (int n = Line::count(q, kvh, line.cut); unit >= at + n; n = Line::count(q, kvh, line.cut)) {
     at += n;
-    q = seq_at<FEW_BQ, BK>(c, ++seq);
+    q = line_seq<BK>(c, f, ++seq);
   }
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   p.seq = uniform(seq);
@@ -864,7 +874,7 @@ cache_few(const CacheArgs c, const Few f) {
   const float sc = LOG2E * c.scale;
 
   for (int unit = first; unit < end;) {
-    const Part p = part_at<BK>(c, line, unit, end);
+    const Part p = part_at<BK>(c, f, line, unit, end);
     const Seq& q = p.q;
     // the segment starts this wave's units, or ends them behind others
     const int slot = 2 * wid + (unit != first);
@@ -875,7 +885,7 @@ cache_few(const CacheArgs c, const Few f) {
     const int t_last = row_of.token(left - 1);
     int lo, hi;
     key_range(c, q, row_of.tok, t_last, lo, hi);
-    const int base = lo / BK, t0 = base + p.from, t1 = min(base + p.upto, (hi + BK - 1) / BK);
+    const int base = lo / BK, t0 = base + max(p.from - f.extra, 0), t1 = min(base + max(p.upto - f.extra, 0), (hi + BK - 1) / BK);
     const int mine = min(r31, left - 1), my_tok = row_of.token(mine);
     int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
     if (c.causal) {
@@ -1093,7 +1103,12 @@ cache_few(const CacheArgs c, const Few f) {
 // float32: 32x32x2 MFMAs.  Four waves take every fourth tile of 32 keys of the same 32 rows and
 // meet in LDS.  Each has room for one tile of K and one of V there: V is on its way during the
 // scores, the next K during the products with V, so a wave never waits for both, and two
-// waves share a SIMD.
+// waves share a SIMD.  What a part has at its start
+// (its place in the line, pages, queries, first keys) is asked for before the sums of the part before it
+// meet: 1,024 rows of 192 heads on 24 heads of 1,024 keys 475 us instead of 529.
+// Bound by the fp32 MFMA over long parts (8,192 x 8,192 keys, 24 heads: 80% of its peak) and by the parts'
+// ends over short ones.  Operands read ahead of the products and weights formed between them are no faster
+// (the windowed chunks below 104 us instead of 100).
 template <int D, int RUN>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, 8)))
 cache_f32(const CacheArgs c, const Few f) {
@@ -1162,7 +1177,7 @@ cache_f32(const CacheArgs c, const Few f) {
     __syncthreads();                             // V's places are free again
   };
   while (unit < end) {
-    const Part p = part_at<BK>(c, line, unit, end);
+    const Part p = part_at<BK>(c, f, line, unit, end);
     const Seq& q = p.q;
     const int slot = 2 * wid + (unit != first);
     unit += line.cut ? p.upto - p.from : 1;
@@ -1172,7 +1187,7 @@ cache_f32(const CacheArgs c, const Few f) {
     const int t_last = row_of.token(left - 1);
     int lo, hi;
     key_range(c, q, row_of.tok, t_last, lo, hi);
-    const int base = lo / BK, t0 = base + p.from, t1 = min(base + p.upto, (hi + BK - 1) / BK);
+    const int base = lo / BK, t0 = base + max(p.from - f.extra, 0), t1 = min(base + max(p.upto - f.extra, 0), (hi + BK - 1) / BK);
     const int mine = min(r31, left - 1), my_tok = row_of.token(mine);
     int lim = total - 1, low = 0, lim_first = total - 1, low_last = 0;
     if (c.causal) {
@@ -1346,7 +1361,7 @@ line_join(const CacheArgs c, const Few f) {
   const int j = blockIdx.x;
   if (!line.cut || j + 1 >= line.wgs) return;
   const int begin = line.begin(j), end = line.begin(j + 1);
-  const Part p = part_at<BK>(c, line, end - 1, end);
+  const Part p = part_at<BK>(c, f, line, end - 1, end);
   const int start = end - 1 - p.from;
   if (start < begin || start + p.q.nk <= end) return;
   const int ch = line.wg_of(start + p.q.nk - 1) - j + 1, left = min(p.q.n * c.group - p.r0, FEW_BQ);
@@ -1372,11 +1387,11 @@ line_join_row(const CacheArgs c, const Few f) {
   for (int id = blockIdx.x; id < n; id += gridDim.x) {
     const int tok = id / c.heads, head = id % c.heads;
     const int s = seq_of(c.pg, tok);
-    const Seq q = seq_at<FEW_BQ, BK>(c, s);
+    const Seq q = line_seq<BK>(c, f, s);
     if (tok < q.a || tok >= q.a + q.n || q.nk == 0) continue;
     // tiles in front of the sequence
     int before = __shfl(line.upto, s / line.per) - __shfl(line.mine, s / line.per);
-    for (int i = s / line.per * line.per; i < s; ++i) before += Line::count(seq_at<FEW_BQ, BK>(c, i), kvh, true);
+    for (int i = s / line.per * line.per; i < s; ++i) before += Line::count(line_seq<BK>(c, f, i), kvh, true);
     const int r = (tok - q.a) * c.group + head % c.group, qi = r / FEW_BQ;
     const int a = before + (head / c.group * q.qt + fold_index(qi, q.qt)) * q.nk;
     const int w0 = line.wg_of(a), ch = line.wg_of(a + q.nk - 1) - w0 + 1;
@@ -1470,6 +1485,10 @@ static void run_line(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream
   const int64_t rows = (int64_t)c.n_q * c.group;
   Few f{};
   f.slot_rows = (int)std::min<int64_t>(FEW_BQ, rows);
+  // A segment's start and end take about as long as this many tiles: 64 x 1 token of 20 to 10,161 keys
+  // without them 47 us, with one or more 44; eight float32 chunks of 100 to 326 rows behind 6 to 3,000
+  // keys 99 us with none, 95 with four, 97 with eight, 110 with sixteen.
+  f.extra = F32 ? 4 : 1;
   // bf16: one wave to a SIMD, 64 KB in flight on a CU: 8 x 10,160 keys of 24 heads 91 us, 1 x 139,776
   // of 4 heads of 128 48, with three to a CU 92 and 48, with five (a SIMD then has two) 116 and 62.
   // float32: as many workgroups as the LDS holds.
