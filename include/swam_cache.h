@@ -91,7 +91,9 @@ int swam_qk_norm_rope(swam_ctx* ctx, const swam_qk_post* post, const int32_t* po
  * lies in page table[s][j / page_size] at slot j % page_size; a table entry outside
  * [0, n_pages) holds nothing, and tokens past max_pages * page_size have no place.
  *   k, v  : act, page p, slot t, head h at k + p k_page + t k_token + h k_head (any
- *           order of the three whose elements do not meet; k and v may share a buffer)
+ *           order of the three whose elements do not meet).  k and v may share a buffer -- pages,
+ *           tokens or heads of both in turn -- but no element; where elements of one lie between
+ *           the other's, both have the same strides there
  *   table : int32 [n_seqs][max_pages], row stride table_stride
  *   length: int32 [n_seqs], tokens of each sequence before the chunk (clamped to
  *           [0, max_pages * page_size]).  Both calls take the length before the

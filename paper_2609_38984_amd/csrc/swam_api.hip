@@ -380,21 +380,47 @@ int check_heads(swam_ctx* c, const void* p, int64_t ld, int64_t rows, int64_t wi
   return SWAM_OK;
 }
 
+// The head vectors of K or V: `n` dimensions of more than one, the closest first, and the elements
+// that lie inside each (extent[n]: all).
+struct Lattice {
+  struct Dim { int64_t step, n; } d[3];
+  int n = 0;
+  int64_t extent[4];
+};
+
+// whether head vectors of the dimensions below `i` of both share an element, b's first `at` elements behind
+// a's.  What overlaps and is laid out in another way counts as shared.
+bool heads_meet(const Lattice& a, const Lattice& b, int i, int64_t at) {
+  if (at >= a.extent[i] || -at >= b.extent[i]) return false;
+  if (i == 0) return true;
+  const Lattice::Dim x = a.d[i - 1], y = b.d[i - 1];
+  if (x.step != y.step || x.n != y.n) return true;
+  // no element reaches past its step: only the two neighbours in front of `at` and behind it can meet
+  const int64_t before = at / x.step - (at % x.step < 0);
+  for (int64_t off : {before, before + 1})
+    if (std::abs(off) < x.n && heads_meet(a, b, i - 1, at - off * x.step)) return true;
+  return false;
+}
+
 // K or V of a cache: strides whose elements do not meet, and the bytes they span
-int check_pages(swam_ctx* c, const void* p, int64_t page, int64_t token, int64_t head, const swam_kv_cache* k, Span* out) {
+int check_pages(swam_ctx* c, const void* p, int64_t page, int64_t token, int64_t head, const swam_kv_cache* k, Span* out,
+                Lattice* lat) {
   const int64_t es = ops_esz(c);
   *out = Span{0, 0, 0, 0};
   if (k->n_pages == 0) return SWAM_OK;
   if (!p) return set_err(c, SWAM_E_INVALID, "the cache's k and v required");
-  struct Dim { int64_t step, n; } d[3] = {{page, k->n_pages}, {token, k->page_size}, {head, k->n_kv_heads}};
-  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.step < b.step; });
+  Lattice::Dim d[3] = {{page, k->n_pages}, {token, k->page_size}, {head, k->n_kv_heads}};
+  std::sort(d, d + 3, [](const Lattice::Dim& a, const Lattice::Dim& b) { return a.step < b.step; });
   int64_t extent = k->head_dim;                 // elements of what lies inside
-  for (const Dim& x : d) {
+  for (const Lattice::Dim& x : d) {
     if (x.n == 1) continue;
     if (x.step < extent) return set_err(c, SWAM_E_INVALID, "the cache's strides let elements meet");
     if (x.step > (1ll << 48) / x.n) return set_err(c, SWAM_E_SHAPE, "a cache's dimension times its stride below 2^48");
+    lat->d[lat->n] = x;
+    lat->extent[lat->n++] = extent;
     extent += x.step * (x.n - 1);
   }
+  lat->extent[lat->n] = extent;
   if (token > OPS_MAX_STRIDE) return set_err(c, SWAM_E_SHAPE, "the cache's token strides below 2^22");
   if (!aligned16(p) || page * es % 16 || token * es % 16 || head * es % 16)
     return set_err(c, SWAM_E_INVALID, "the cache's k, v and strides must be 16-byte aligned");
@@ -419,9 +445,12 @@ int check_cache(swam_ctx* c, const swam_kv_cache* k, const int32_t* cu, Span* ks
   if (far_apart(k->n_seqs, k->table_stride)) return set_err(c, SWAM_E_SHAPE, "n_seqs times table_stride below 2^48");
   if (!typed(k->table, 4) || !typed(k->length, 4) || !typed(cu, 4))
     return set_err(c, SWAM_E_INVALID, "a tensor is not aligned to its element type");
-  if (int rc = check_pages(c, k->k, k->k_page, k->k_token, k->k_head, k, ks)) return rc;
-  if (int rc = check_pages(c, k->v, k->v_page, k->v_token, k->v_head, k, vs)) return rc;
+  Lattice kl, vl;
+  if (int rc = check_pages(c, k->k, k->k_page, k->k_token, k->k_head, k, ks, &kl)) return rc;
+  if (int rc = check_pages(c, k->v, k->v_page, k->v_token, k->v_head, k, vs, &vl)) return rc;
   if (k->n_pages > 0 && k->k == k->v) return set_err(c, SWAM_E_INVALID, "the cache's k and v are one tensor");
+  if (k->n_pages > 0 && heads_meet(kl, vl, kl.n, ((int64_t)k->v - (int64_t)k->k) / ops_esz(c)))
+    return set_err(c, SWAM_E_INVALID, "the cache's k and v overlap");
   return SWAM_OK;
 }
 

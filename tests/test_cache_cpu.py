@@ -4,6 +4,7 @@ context shows what is wrong with the call itself; fake pointers are never derefe
 import ctypes as C
 import math
 import os
+import random
 import re
 
 import pytest
@@ -248,3 +249,77 @@ def test_append_refuses(lib, change, code, word):
 def test_attention_refuses(lib, change, code, word):
     rc, msg = _call(lib, "swam_cache_attention", change)
     assert rc == code and word in msg, msg
+
+
+def _joint(shift, **change):
+    """K and V in one buffer, V `shift` bytes behind K."""
+    a = {"cache.v": _p(10) + shift}
+    a.update({"cache." + n: v for n, v in change.items()})
+    return a
+
+
+# elements of a head, a token's heads, a head's tokens and a page of CACHE (head by head)
+HEAD, PAGE = 64, 64 * 2 * 16
+
+
+@pytest.mark.parametrize("change", [
+    # one token, one head or one page apart, to either side, and by less than a head
+    _joint(2 * HEAD), _joint(-2 * HEAD), _joint(2 * HEAD * 16), _joint(-2 * HEAD * 16), _joint(2 * PAGE), _joint(-2 * PAGE),
+    _joint(16), _joint(-16), _joint(2 * (19 * PAGE + HEAD * 16 + 15 * HEAD)), _joint(2 * 20 * PAGE - 16),
+    # tokens of both heads in turn
+    _joint(2 * HEAD, k_token=128, v_token=128, k_head=64, v_head=64), _joint(256, k_token=128, v_token=128, k_head=64, v_head=64),
+    # a page of both, V one token or one page too early or too late
+    _joint(2 * PAGE - 2 * HEAD, k_page=2 * PAGE, v_page=2 * PAGE), _joint(2 * PAGE + 2 * HEAD, k_page=2 * PAGE, v_page=2 * PAGE),
+    _joint(4 * PAGE, k_page=2 * PAGE, v_page=2 * PAGE),
+    # other strides inside or between the pages
+    _joint(2 * HEAD, k_page=2 * PAGE, v_page=4 * PAGE), _joint(2 * HEAD * 16, v_token=128, v_head=64),
+    _joint(2 * PAGE - 256, k_page=2 * PAGE, v_page=2 * PAGE, v_token=128, v_head=64),
+])
+def test_keys_and_values_that_overlap_are_refused(lib, change):
+    for fn in ("swam_cache_append", "swam_cache_attention"):
+        rc, msg = _call(lib, fn, change)
+        assert rc == INVALID and "k and v overlap" in msg, (fn, msg)
+
+
+@pytest.mark.parametrize("change", [
+    # behind each other
+    _joint(2 * 20 * PAGE), _joint(-2 * 20 * PAGE), _joint(2 * 20 * PAGE, v_token=128, v_head=64),
+    # K and V of a page side by side, in either order, laid out alike or not
+    _joint(2 * PAGE, k_page=2 * PAGE, v_page=2 * PAGE), _joint(-2 * PAGE, k_page=2 * PAGE, v_page=2 * PAGE),
+    _joint(2 * PAGE, k_page=2 * PAGE, v_page=2 * PAGE, v_token=128, v_head=64),
+    # of a token (all heads of K, then of V), of a head's tokens, of a token and head
+    _joint(2 * 128, k_token=256, v_token=256, k_head=64, v_head=64, k_page=2 * PAGE, v_page=2 * PAGE),
+    _joint(2 * HEAD * 16, k_head=2 * HEAD * 16, v_head=2 * HEAD * 16, k_page=2 * PAGE, v_page=2 * PAGE),
+    _joint(2 * HEAD, k_token=128, v_token=128, k_head=128 * 16, v_head=128 * 16, k_page=2 * PAGE, v_page=2 * PAGE),
+    # a column range of wider rows, V's a page later too
+    _joint(2 * 128 + 2 * 16 * 512, k_token=512, v_token=512, k_head=64, v_head=64, k_page=16 * 512, v_page=16 * 512),
+])
+def test_keys_and_values_may_share_a_buffer(lib, change):
+    for fn in ("swam_cache_append", "swam_cache_attention"):
+        assert _call(lib, fn, change) == (INVALID, "ctx is NULL"), fn
+
+
+def test_the_overlap_of_keys_and_values_is_found_exactly(lib):
+    """Random shifts of layouts with the same strides, against the elements themselves."""
+    rng = random.Random(3)
+    seen = [0, 0]
+    for _ in range(400):
+        n = [rng.randint(1, 3), 8, rng.randint(1, 3)]             # pages, tokens, heads
+        order, step, steps = rng.sample(range(3), 3), 64, [0] * 3
+        for i in order:                                           # the closest first, some with room between
+            step += 8 * rng.choice([0, 0, 8, 24])
+            steps[i] = step
+            step *= n[i]
+        heads = {p * steps[0] + t * steps[1] + h * steps[2] for p in range(n[0]) for t in range(8) for h in range(n[2])}
+        shift = 8 * rng.randint(-step // 8 - 8, step // 8 + 8)
+        if shift == 0:
+            continue
+        # two head vectors meet where their starts are less than one apart
+        meet = any(s + shift + x in heads for s in heads for x in range(-56, 64, 8))
+        rc, msg = _call(lib, "swam_cache_append", {
+            "cache.k": _p(10), "cache.v": _p(10) + 2 * shift, "cache.n_pages": n[0], "cache.page_size": 8, "cache.n_kv_heads": n[2],
+            "cache.k_page": steps[0], "cache.k_token": steps[1], "cache.k_head": steps[2], "cache.v_page": steps[0],
+            "cache.v_token": steps[1], "cache.v_head": steps[2], "ks": 256, "vs": 256})
+        assert (rc, msg) == (INVALID, "the cache's k and v overlap" if meet else "ctx is NULL"), (n, steps, shift)
+        seen[meet] += 1
+    assert min(seen) > 50
