@@ -142,9 +142,9 @@ int swam_cache_append(swam_ctx* ctx, const swam_kv_cache* cache, const swam_qk_p
  * h' = h / (n_heads / n_kv_heads).  A row without a visible key, or whose visible scores are
  * all minus infinity, gets zeros and the normaliser minus infinity.  Keys and values that a
  * row does not see do not matter to it, NaN and infinities included.  Scores, weights and
- * sums are float32.  In a bf16 context chunks round the weights to bf16 in front of the product
- * with v (outputs are off by 0.0024 of their size, where bf16 itself makes 0.0017); single tokens and
- * short chunks keep 16 bits of them (0.0017).
+ * sums are float32.  In a bf16 context a sequence of up to 32 rows (tokens times n_heads / n_kv_heads) keeps
+ * 16 bits of each weight in front of the product with v, whatever stands beside it in the call (outputs
+ * are off by 0.0017 of their size, which is bf16's own); longer ones may round them to bf16 (0.0024).
  *   q, o : act, token i, head h at q + i q_stride + h head_dim
  *   cu   : as above; rows of o and lse outside every sequence are left as they are
  *   causal : 1 or 0 (0: a chunk whose tokens all see each other)

@@ -28,6 +28,7 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
 constexpr int CA_BK = 64;                      // keys per tile
+constexpr int FEW_BQ = 32;                     // rows of a tile of the line below
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // How the keys are split and where partial results go: slot i holds slot_rows rows of
@@ -244,7 +245,11 @@ __device__ __forceinline__ void add_odd(f32x16& o, int q4, bool sees, uint2 x) {
 
 // RUN: 8-key slabs that share a page for certain
 // KG: groups of four waves.  Each takes every KG-th tile of the same rows; they meet in LDS.
-template <int D, int RUN, int KG>
+// FINE: sequences of up to FEW_BQ rows, which stand beside longer ones here, keep 16 bits of each weight as
+// they do on the line: their rows are one wave's, and the second wave, which has none, takes the same rows with
+// what bf16 leaves of the weights (three single tokens of 24 heads beside 1,248 behind 3,000 keys: 88 us,
+// with bf16's 8 bits alone 71; batches without such a sequence as before)
+template <int D, int RUN, int KG, bool FINE>
 __global__ void __launch_bounds__(256 * KG) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, 8)))
 cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   constexpr int H2 = D / 64;                     // 128-byte halves of a head's row
@@ -267,9 +272,10 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
   int lo, hi, t0, t1;
   key_range(c, w.q, row_of.tok, row_of.token(min(BQ, left) - 1), lo, hi);
   slice_of(lo, hi, CA_BK, w.y, w.ch, t0, t1);
+  [[maybe_unused]] const bool fine = FINE && w.q.n * group <= FEW_BQ, rest = fine && wave == 1;
   // the keys that all rows of this wave see lie in [low_last, lim_first], those that any
   // sees in [low_first, lim_last]; a wave behind the last row sees none
-  const int wr = wave * 32;
+  const int wr = FINE && rest ? 0 : wave * 32;
   int lim_first = total - 1, lim_last = wr < left ? total - 1 : -1, low_first = 0, low_last = 0;
   const int p_first = w.q.old + row_of.token(min(wr, left - 1)), p_last = w.q.old + row_of.token(min(wr + 31, left - 1));
   if (c.causal) {
@@ -415,14 +421,15 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
             pf[t][u][mm] = (__bf16)p0; pf[t][u][mm + 1] = (__bf16)p1;
           }
     };
-    if (!fresh) {
+    if (!fresh && !(FINE && fine)) {
       f32x16 st[2];
       scores(st, vis);
       probs(st);
     }
     // the running maximum moves only when a row sum shows that some weight passed
-    // 2^8 (or is NaN): the scores are then formed again against the new one
-    if (fresh || __any(!(ps0 + ps1 <= 256.0f))) {
+    // 2^8 (or is NaN): the scores are then formed again against the new one (for both parts of the weights in
+    // every tile: they have to go by the same maximum)
+    if (fresh || (FINE && fine) || __any(!(ps0 + ps1 <= 256.0f))) {
       uint32_t w0 = __builtin_amdgcn_readfirstlane((uint32_t)vis), w1 = __builtin_amdgcn_readfirstlane((uint32_t)(vis >> 32));
       asm volatile("" : "+s"(w0), "+s"(w1) : : "memory");
       const uint64_t again = (uint64_t)w1 << 32 | w0;
@@ -433,7 +440,12 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[t][r]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      if constexpr (FINE) {                        // (without the register of an index)
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      } else {
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+      }
       const float m_new = fmaxf(m_run, mx * sc);
       const float corr = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
@@ -442,12 +454,23 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
       for (int t = 0; t < D / 32; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] *= corr;
-      probs(st);
+      if (!FINE || !rest) {
+        probs(st);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(st[t][r], sc, -m_run));
+            pf[t][r >> 3][r & 7] = (__bf16)(p - (float)(__bf16)p);
+          }
+      }
     }
     l_run += ps0 + ps1;
     const unsigned short* vs = reinterpret_cast<const unsigned short*>(from[1]);
     bool odd = false;
-    if (mixed) {
+    // (what is left of a weight may be zero or negative: nor is an infinite value multiplied by it)
+    if (FINE ? mixed || rest : mixed) {
       // a weight of zero does not hide a value that is not finite
       u16x2 top = {0, 0};
 #pragma unroll
@@ -526,6 +549,33 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     buf ^= 1;
   }
   wait_stage<0>();
+  if (FINE && fine) {
+    // both parts of the weights meet in the first wave
+    float* meet = reinterpret_cast<float*>(&ring[0][0][0]);
+    static_assert(D / 2 * 64 * 4 <= (int)sizeof(kv[0]), "they fit in the tiles' place");
+    __syncthreads();
+    if (rest) {
+#pragma unroll
+      for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<float4*>(meet + ((4 * ht + q4) * 64 + lane) * 4) =
+              make_float4(o[ht][4 * q4], o[ht][4 * q4 + 1], o[ht][4 * q4 + 2], o[ht][4 * q4 + 3]);
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int ht = 0; ht < D / 32; ++ht)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const float4 x = *reinterpret_cast<const float4*>(meet + ((4 * ht + q4) * 64 + lane) * 4);
+          o[ht][4 * q4] += x.x;
+          o[ht][4 * q4 + 1] += x.y;
+          o[ht][4 * q4 + 2] += x.z;
+          o[ht][4 * q4 + 3] += x.w;
+        }
+    }
+  }
   if constexpr (KG > 1) {
     // what the other groups have, register by register: the same lanes hold the same rows
     float* meet = reinterpret_cast<float*>(&kv[0][0][0][0]);
@@ -718,7 +768,6 @@ struct Few {
   int slot_rows;
   int extra;          // tiles that a segment's start and end are worth
 };
-constexpr int FEW_BQ = 32;
 
 // a sequence with the units of its segments for key tiles
 template <int BK>
@@ -1540,10 +1589,11 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
   // a grid holds less than 2^32 threads: more take another launch
   const int64_t step = ((1 << 24) - 1) / kvh;
   auto launch_with = [&](auto run, auto groups) {
-    constexpr int KG = decltype(groups)::value;
+    constexpr int RUN = decltype(run)::value, KG = decltype(groups)::value;
+    // (a sequence of few rows is here only beside others)
+    const auto kernel = c.pg.n_seqs > 1 ? cache_bf16<D, RUN, KG, true> : cache_bf16<D, RUN, KG, false>;
     for (int64_t u = 0; u < units; u += step)
-      hipLaunchKernelGGL((cache_bf16<D, decltype(run)::value, KG>), dim3((unsigned)(std::min(units - u, step) * kvh)),
-                         dim3(256 * KG), 0, st, c, sp, (int)u);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min(units - u, step) * kvh)), dim3(256 * KG), 0, st, c, sp, (int)u);
   };
   // Few row tiles: one workgroup to a CU that takes several key tiles at once, as many as the LDS
   // holds.

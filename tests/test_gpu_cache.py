@@ -883,3 +883,78 @@ def test_strided_tables_shared_pages_and_repeated_sequences(contexts, dtype):
         where = staticmethod(lambda s, j: (table[s].long()[j // page], j % page))
     C.kvh, C.k, C.v = kvh, k, v
     check_cache_attention(C, q, o, lse, new, True, 0, 0.125, o, lse)
+
+
+# ---------------------------------------------------------------------------
+# what a sequence's neighbours do to it
+# ---------------------------------------------------------------------------
+FEW_ROWS = 32                                            # tokens times heads of a group
+
+
+def check_fine(c, q, o, new, causal, window, scale):
+    """Chunks of up to FEW_ROWS rows keep 16 bits of each weight, which stand as two bf16 numbers: the first is off
+    by 2^-8 of it at most and the second by 2^-8 of that.  Else the bound of check_cache_attention."""
+    heads, dim = q.shape[1:]
+    group, h, at, checked = heads // c.kvh, HALF[q.dtype], 0, 0
+    bits = 2.0 ** -16 if q.dtype == torch.bfloat16 else 0.0
+    for s, n in enumerate(new):
+        rows = slice(at, at + n)
+        at += n
+        if n == 0 or n * group > FEW_ROWS:
+            continue
+        total = c.lengths[s] + n
+        j = torch.arange(total, device="cuda")
+        i = torch.arange(c.lengths[s], total, device="cuda")[:, None]
+        see = torch.ones((n, total), dtype=torch.bool, device="cuda")
+        if causal:
+            see &= j <= i
+        if window:
+            see &= i - j < window
+        p, t = c.where(s, j)
+        k, v = c.k[p, t].double(), c.v[p, t].double()
+        for hd in range(heads):
+            kj, vj, qj = k[:, hd // group], v[:, hd // group], q[rows, hd].double()
+            x = (qj @ kj.t().contiguous() * scale).masked_fill(~see, -math.inf)
+            lse = torch.logsumexp(x, 1, keepdim=True)
+            w = torch.exp(x - lse)
+            want, size = w @ vj, w @ vj.abs()
+            qk = ((qj.abs() @ kj.abs().t().contiguous()) * scale).masked_fill(~see, 0.0).amax(1, keepdim=True)
+            lerr, sums = 2 * (dim + 8) * U * qk + 8 * U * lse.abs(), (total + 16) * U
+            err = (bits + 2 * lerr + 2 * sums) * 1.01 * size
+            err = err + (h + 4 * U) * (want.abs() + err)
+            off = (o[rows, hd].double() - want).abs()
+            assert bool((off <= err).all()), (s, hd, float((off / err).max()))
+            checked += off.numel()
+    assert checked
+
+
+def run_fine(ctx, dt, new, old, heads, kvh, dim, page, causal=True, window=0, seed=0):
+    """Even weights: the logits' own errors, which the bound grows with, are small beside the weights'."""
+    g = gen(seed)
+    c = Paged(dt, old, [a + b for a, b in zip(new, old)], page, kvh, dim, seed)
+    for s in range(len(new)):
+        c.put(s, 0, old[s] + new[s], g)
+    q, _ = rows_of((sum(new), heads, dim), dt, g)
+    o = torch.empty_like(q)
+    ctx.cache_attention(c.c, q, o, cu=offsets(new), causal=causal, window=window, scale=0.01)
+    check_fine(c, q, o, new, causal, window, 0.01)
+    check_cache_attention(c, q, o, None, new, causal, window, 0.01, o, None)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("new,old,heads,kvh,dim,page", [
+    ([1248, 1, 1, 7], [500, 3000, 40, 90], 4, 2, 64, 64), ([3, 400, 1], [70, 0, 200], 3, 3, 64, 8), ([300, 5, 1], [60, 77, 1000], 12, 3, 128, 16),
+    ([1, 200, 2, 0, 8], [128, 100, 31, 9, 63], 4, 1, 128, 32), ([1, 700, 16], [90, 64, 64], 160, 80, 64, 16),
+    ([500, 1, 4], [0, 55, 800], 70, 70, 128, 64)])
+def test_short_chunks_beside_long_ones_keep_16_bits_of_the_weights(contexts, dtype, new, old, heads, kvh, dim, page):
+    for causal, window in ((True, 0), (False, 0), (True, 50), (False, 33)):
+        run_fine(contexts[dtype], TYPES[dtype], new, old, heads, kvh, dim, page, causal, window, 11)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("new,old,heads,kvh,dim,page", [
+    ([1] * 8, [60 * i for i in range(8)], 4, 4, 64, 32), ([1], [3000], 14, 2, 128, 64), ([3, 8, 1], [200, 64, 5], 8, 2, 64, 8),
+    ([1] * 70, [(37 * i) % 400 for i in range(70)], 6, 3, 128, 16), ([32], [100], 2, 2, 64, 16), ([8], [900], 12, 3, 128, 256)])
+def test_single_tokens_and_short_chunks_keep_16_bits_of_the_weights(contexts, dtype, new, old, heads, kvh, dim, page):
+    for causal, window in ((True, 0), (False, 0), (True, 50)):
+        run_fine(contexts[dtype], TYPES[dtype], new, old, heads, kvh, dim, page, causal, window, 12)
