@@ -922,11 +922,14 @@ cache_few(const CacheArgs c, const Few f) {
   for (int s = 0; s < 4; ++s) kofs[s] = r31 * 8 + ((2 * s + g) ^ lds_swz(r31));
   const float sc = LOG2E * c.scale;
 
+  // What bf16 leaves of a weight may be zero or negative, and infinity times that is NaN: a part whose sums are
+  // not finite is done again, with a look at every tile's values.
+  bool look = false;
   for (int unit = first; unit < end;) {
     const Part p = part_at<BK>(c, f, line, unit, end);
     const Seq& q = p.q;
     // the segment starts this wave's units, or ends them behind others
-    const int slot = 2 * wid + (unit != first);
+    const int slot = 2 * wid + (unit != first), here = unit;
     unit += line.cut ? p.upto - p.from : 1;
 
     const int hk = p.hk, r0 = p.r0, left = min(q.n * c.group - r0, FEW_BQ), total = q.total;
@@ -1066,7 +1069,7 @@ cache_few(const CacheArgs c, const Few f) {
           }
         l_run += ps0 + ps1;
         bool odd = false;
-        if ((k0 + BK - 1 > lim_first && lim_first < total - 1) || k0 < low_last) {
+        if (look || (k0 + BK - 1 > lim_first && lim_first < total - 1) || k0 < low_last) {
           u16x2 top = {0, 0};
 #pragma unroll
           for (int i = 0; i < TILE / 64; ++i) {
@@ -1113,6 +1116,16 @@ cache_few(const CacheArgs c, const Few f) {
         else products([](uint4 x) { return x; });
     }
     wait_stage<0>();                             // (the ring is free again)
+    float odd4[4] = {0.0f, 0.0f, 0.0f, 0.0f};    // NaN where a sum is not finite
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) odd4[r & 3] = fmaf(o[x][r], 0.0f, odd4[r & 3]);
+    look = !look && __any((odd4[0] + odd4[1]) + (odd4[2] + odd4[3]) != 0.0f);
+    if (look) {
+      unit = here;
+      continue;
+    }
     const float l = l_run + __shfl_xor(l_run, 32);
     const int64_t tok = q.a + my_tok;
     const int head = hk * c.group + row_of.head(mine);

@@ -958,3 +958,36 @@ def test_short_chunks_beside_long_ones_keep_16_bits_of_the_weights(contexts, dty
 def test_single_tokens_and_short_chunks_keep_16_bits_of_the_weights(contexts, dtype, new, old, heads, kvh, dim, page):
     for causal, window in ((True, 0), (False, 0), (True, 50)):
         run_fine(contexts[dtype], TYPES[dtype], new, old, heads, kvh, dim, page, causal, window, 12)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new,old,heads,kvh", [
+    ([1], [900], 4, 2), ([1, 1, 1], [40, 500, 2000], 3, 3), ([3], [2000], 8, 1), ([200], [300], 4, 4), ([300, 1, 4], [64, 700, 90], 4, 2),
+    ([1] * 70, [100 + 3 * i for i in range(70)], 4, 4)])
+def test_infinite_values_stay_infinite(contexts, dtype, dim, new, old, heads, kvh):
+    """A value that is infinite, with a weight above zero, makes its sign's infinity of its column in the rows that
+    see it, not NaN, in whichever way the weights are held; the others stay finite."""
+    dt, g = TYPES[dtype], gen(17)
+    c = Paged(dt, old, [a + b for a, b in zip(new, old)], 16, kvh, dim)
+    q, _ = rows_of((sum(new), heads, dim), dt, g)
+    hit = []
+    for s in range(len(new)):
+        c.put(s, 0, old[s] + new[s], g)
+        # of a key that all rows see, and one that a chunk's first rows do not
+        for j, head, col, value in ((old[s] // 2, 0, 3, math.inf), (old[s] + new[s] // 2, kvh - 1, dim - 6, -math.inf)):
+            p, t = c.where(s, torch.tensor([j], device="cuda"))
+            c.v[p[0], t[0], head, col] = value
+            hit.append((s, j, head, col, value))
+    for causal in (True, False):
+        o = torch.empty_like(q)
+        contexts[dtype].cache_attention(c.c, q, o, cu=offsets(new), causal=causal, scale=0.01)
+        want = torch.zeros((sum(new), heads, dim), device="cuda")
+        group, start = heads // kvh, offsets(new).tolist()
+        for s, j, head, col, value in hit:
+            i = torch.arange(new[s], device="cuda")
+            sees = (old[s] + i >= j) | (not causal)
+            want[start[s]:start[s + 1], head * group:(head + 1) * group, col] = torch.where(sees, value, 0.0)[:, None]
+        odd = torch.isinf(want)
+        assert torch.equal(o.float()[odd], want[odd])
+        assert bool(torch.isfinite(o[~odd]).all())
