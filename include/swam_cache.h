@@ -124,7 +124,8 @@ typedef struct swam_kv_cache {
  *   pos   : int32 [rows], positions of the rotation, or NULL for the token's position in
  *           its sequence
  *   cu    : int32 [n_seqs + 1], row offsets of the sequences' chunks, or NULL for one
- *           sequence of all rows.  Bounds are clamped to [0, rows] (sequences must not overlap)
+ *           sequence of all rows.  Sequence s is the rows from cu[s] to cu[s + 1], both clamped
+ *           to [0, rows], and empty where they fall (sequences must not overlap)
  *   q, q_out : act, n_heads heads (0: none, both NULL); q_out may be q itself
  *   k, v  : act, n_kv_heads heads
  * Rows outside every sequence are neither appended nor written to q_out.  Tokens without a

@@ -1448,9 +1448,14 @@ line_join_row(const CacheArgs c, const Few f) {
   const int n = c.n_q * c.heads;
   for (int id = blockIdx.x; id < n; id += gridDim.x) {
     const int tok = id / c.heads, head = id % c.heads;
-    const int s = seq_of(c.pg, tok);
-    const Seq q = line_seq<BK>(c, f, s);
-    if (tok < q.a || tok >= q.a + q.n || q.nk == 0) continue;
+    int s = seq_of(c.pg, tok);
+    Seq q = line_seq<BK>(c, f, s);
+    if (tok < q.a || tok >= q.a + q.n) {         // offsets that fall, or nobody's
+      s = seq_that_holds(c.pg, tok);
+      if (s < 0) continue;
+      q = line_seq<BK>(c, f, s);
+    }
+    if (q.nk == 0) continue;
     // tiles in front of the sequence
     int before = __shfl(line.upto, s / line.per) - __shfl(line.mine, s / line.per);
     for (int i = s / line.per * line.per; i < s; ++i) before += Line::count(line_seq<BK>(c, f, i), kvh, true);

@@ -133,10 +133,14 @@ head_post(const HeadPost a, const Paged pg, int lg_parts) {
     int pos = (int)row;
     int64_t k_at = -1, v_at = -1;               // where the token's first head goes
     if constexpr (CACHE) {
-      const int s = seq_of(pg, row);
+      int s = seq_of(pg, row);
       int b, e;
       chunk_of(pg, s, (int)a.rows, b, e);
-      if (row < b || row >= e) continue;        // behind the last sequence
+      if (__builtin_expect(row < b || row >= e, 0)) {   // offsets that fall, or nobody's
+        s = seq_that_holds(pg, row);
+        if (s < 0) continue;
+        chunk_of(pg, s, (int)a.rows, b, e);
+      }
       const int64_t slot = held(pg, s) + (row - b);
       pos = (int)slot;
       const int64_t pi = slot >> pg.lg_page;

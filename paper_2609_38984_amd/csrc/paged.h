@@ -18,8 +18,8 @@ __device__ __forceinline__ int held(const Paged& p, int s) {
   return min(max(p.length[s], 0), p.max_pages << p.lg_page);
 }
 
-// The first sequence that ends behind row r (n_seqs - 1 at most): two rounds of 64
-// probes find it among 1,024 sequences in two latencies.
+// The first sequence that ends behind row r (n_seqs - 1 at most), which is the one that holds r, if one does, unless
+// offsets fall: two rounds of 64 probes find it among 1,024 sequences in two latencies.
 __device__ __forceinline__ int seq_of(const Paged& p, int64_t r) {
   if (p.cu == nullptr || p.n_seqs == 1) return 0;
   const int lane = threadIdx.x & 63, step = (p.n_seqs + 63) >> 6;
@@ -31,6 +31,19 @@ __device__ __forceinline__ int seq_of(const Paged& p, int64_t r) {
   const uint64_t past = __ballot(lane < step || step == 1 ? p.cu[min(at + lane + 1, p.n_seqs)] > r : false);
   at += past ? __ffsll((unsigned long long)past) - 1 : 0;
   return __builtin_amdgcn_readfirstlane(min(at, p.n_seqs - 1));
+}
+
+// The sequence that holds row r, or -1: a look at all, for where the one above does not.
+__device__ __forceinline__ int seq_that_holds(const Paged& p, int64_t r) {
+  const int lane = threadIdx.x & 63;
+  if (p.cu == nullptr) return -1;
+#pragma unroll 1
+  for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+    const int s = min(s0 + lane, p.n_seqs - 1);
+    const uint64_t holds = __ballot(p.cu[s] <= r && r < p.cu[s + 1]);
+    if (holds) return __builtin_amdgcn_readfirstlane(s0 + __ffsll((unsigned long long)holds) - 1);
+  }
+  return -1;
 }
 
 }  // namespace swam

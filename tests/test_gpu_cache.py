@@ -991,3 +991,48 @@ def test_infinite_values_stay_infinite(contexts, dtype, dim, new, old, heads, kv
         odd = torch.isinf(want)
         assert torch.equal(o.float()[odd], want[odd])
         assert bool(torch.isfinite(o[~odd]).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("cu,rows", [
+    ([-9, 20, 20, 60, 1 << 30], 80),                      # below the rows, an empty one, past the rows
+    ([30, 10, 40, 55], 60),                               # falling: the first is empty, rows 0 to 9 and 55 on are nobody's
+    ([5, 5, -3, -7, 12, 31], 40), ([1 << 30, 9, 22], 22), ([7, -(1 << 31), (1 << 31) - 1], 19),
+    ([50] + [3] * 70 + [3 + i // 3 for i in range(100)], 36), ([10] * 60 + [0, 10, 12, 36] + [36] * 40, 38),
+    ([30, 40, 20, 30, 0, 20], 43)])                       # not in the order of their rows
+def test_append_and_attention_within_clamped_and_falling_offsets(contexts, dtype, cu, rows):
+    """Sequence s is the rows from cu[s] to cu[s + 1], both clamped to the rows, and empty where they fall.  What is
+    appended, what it is attended with, and what is nobody's and left as it was."""
+    dt, g = TYPES[dtype], gen(23)
+    seqs = len(cu) - 1
+    ends = [min(max(e, 0), rows) for e in cu[1:]]
+    starts = [min(max(b, 0), e) for b, e in zip(cu, ends)]
+    new = [e - b for b, e in zip(starts, ends)]
+    old = [(11 * s) % 40 + 900 * (s % 5 == 3) for s in range(seqs)]     # (keys of the longer ones are split)
+    c = Paged(dt, old, [a + b for a, b in zip(new, old)], 8, 2, 64, fill=5.0)
+    for s in range(seqs):
+        c.put(s, 0, old[s], g)
+    q, k, v = (torch.randn((rows, n, 64), device="cuda", generator=g).to(dt) for n in (4, 2, 2))
+    want_k, want_v, mine = c.k.clone(), c.v.clone(), torch.zeros(rows, dtype=torch.bool, device="cuda")
+    for s in range(seqs):
+        if new[s]:
+            p, t = c.where(s, torch.arange(old[s], old[s] + new[s], device="cuda"))
+            want_k[p, t], want_v[p, t] = k[starts[s]:ends[s]], v[starts[s]:ends[s]]
+            assert not bool(mine[starts[s]:ends[s]].any())        # no row is two sequences'
+            mine[starts[s]:ends[s]] = True
+    at = torch.tensor(cu, device="cuda").to(torch.int32)
+    qo = torch.full_like(q, 9.0)
+    contexts[dtype].cache_append(c.c, k, v, cu=at, q=q, q_out=qo)
+    assert torch.equal(c.k, want_k) and torch.equal(c.v, want_v)
+    assert torch.equal(qo[mine], q[mine]) and bool((qo[~mine] == 9.0).all())
+    o, lse = torch.full_like(q, 7.0), torch.full((rows, 4), 7.0, device="cuda")
+    contexts[dtype].cache_attention(c.c, q, o, cu=at, lse=lse)
+    assert bool((o[~mine] == 7.0).all()) and bool((lse[~mine] == 7.0).all())
+    for s in range(seqs):
+        if new[s]:
+            r = slice(starts[s], ends[s])
+
+            class One:
+                kvh, k, v, lengths = c.kvh, c.k, c.v, [old[s]]
+                where = staticmethod(lambda _, j, s=s: c.where(s, j))
+            check_cache_attention(One, q[r], o[r], lse[r], [new[s]], True, 0, 0.125, o[r], lse[r])
