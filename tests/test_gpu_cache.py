@@ -994,6 +994,16 @@ def test_infinite_values_stay_infinite(contexts, dtype, dim, new, old, heads, kv
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("new,old,heads,kvh,dim", [
+    ([1248] + [1] * 63, [100] + [(61 * i) % 900 for i in range(63)], 3, 3, 64),      # by their mean, single tokens
+    ([1] * 40 + [700] + [1] * 23, [30] * 64, 4, 2, 128), ([0] * 100 + [900] + [0] * 155, [0] * 100 + [500] + [9] * 155, 4, 4, 64),
+    ([600] + [0] * 1023, [0] * 1024, 6, 3, 64), ([0, 0, 33, 0, 0, 0, 1, 0], [70, 0, 900, 3, 0, 0, 64, 1], 2, 1, 64)])
+def test_a_long_chunk_among_single_tokens_and_idle_sequences(contexts, dtype, new, old, heads, kvh, dim):
+    for causal, window in ((True, 0), (False, 0), (True, 130)):
+        run_cache_attention(contexts[dtype], TYPES[dtype], new, old, heads, kvh, dim, 16, causal, window, 19)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("cu,rows", [
     ([-9, 20, 20, 60, 1 << 30], 80),                      # below the rows, an empty one, past the rows
     ([30, 10, 40, 55], 60),                               # falling: the first is empty, rows 0 to 9 and 55 on are nobody's
@@ -1036,3 +1046,29 @@ def test_append_and_attention_within_clamped_and_falling_offsets(contexts, dtype
                 kvh, k, v, lengths = c.kvh, c.k, c.v, [old[s]]
                 where = staticmethod(lambda _, j, s=s: c.where(s, j))
             check_cache_attention(One, q[r], o[r], lse[r], [new[s]], True, 0, 0.125, o[r], lse[r])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_context_that_moves_to_another_stream_gives_the_same(dtype):
+    """The same calls behind set_stream give the bits of those in front of it."""
+    from paper_2609_38984_amd import swam
+    dt = TYPES[dtype]
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    ctx = swam.Context(W.preset(2).replace(dtype=dtype, n_blocks=1), first)
+    s = Stream(dt, CHUNKS, 16, 4, 2, 64, 7, False)
+    torch.cuda.synchronize()
+    kept = []
+    for stream in (first, second, first):
+        ctx.set_stream(stream)
+        with torch.cuda.stream(stream):
+            for t in s.o + s.q + [s.c.k, s.c.v]:
+                t.zero_()
+            s.run(ctx)
+            turned = torch.empty_like(s.q[0])
+            ctx.qk_norm_rope(s.q[0], None, s.post, q_out=turned)
+            kept.append([t.clone() for t in s.o + s.q + [s.c.k, s.c.v, turned]])
+        torch.cuda.synchronize()
+    assert all(bool((t != 0).any()) for t in kept[0])
+    for other in kept[1:]:
+        for a, b in zip(kept[0], other):
+            assert torch.equal(a, b)
