@@ -143,7 +143,8 @@ int swam_cache_append(swam_ctx* ctx, const swam_kv_cache* cache, const swam_qk_p
  * h' = h / (n_heads / n_kv_heads).  A row without a visible key, or whose visible scores are
  * all minus infinity, gets zeros and the normaliser minus infinity.  Keys and values that a
  * row does not see do not matter to it, NaN and infinities included.  Scores, weights and
- * sums are float32.  In a bf16 context a sequence of up to 32 rows (tokens times n_heads / n_kv_heads) keeps
+ * sums are float32 (weights up to 2^8 before the division: the size of v times the keys of a row
+ * stays below 2^118).  In a bf16 context a sequence of up to 32 rows (tokens times n_heads / n_kv_heads) keeps
  * 16 bits of each weight in front of the product with v, whatever stands beside it in the call (outputs
  * are off by 0.0017 of their size, which is bf16's own); longer ones may round them to bf16 (0.0024).
  *   q, o : act, token i, head h at q + i q_stride + h head_dim

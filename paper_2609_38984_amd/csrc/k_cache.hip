@@ -10,10 +10,10 @@
 // zeros.  Which keys a row sees is a 64-bit mask per lane, formed only for tiles that
 // some row sees in part.
 //
-// What bounds it: for chunks the instructions of a score (causal 10,160 x 24 heads of 64 375 us, 845
-// TFLOP/s: vector operations 65% of the time, MFMAs 41%, hardly side by side); for single
+// What bounds it (kernels alone, on keys from memory): for chunks the instructions of a score (causal 10,160 x 24
+// heads of 64 373 us, 850 TFLOP/s: vector operations 64% of the time, MFMAs 40%, hardly side by side); for single
 // tokens the bytes of K and V (8 x 10,160 keys of 24 heads 92 us, 5.4 TB/s); in float32 the matrix unit
-// (causal 4,096 x 24 heads 475 us, 1.4 times what its products alone take).
+// (causal 4,096 x 24 heads 443 us with the joining pass, 1.2 times its products at a large product's rate).
 #include "gemm_common.h"
 #include "paged.h"
 
@@ -80,6 +80,10 @@ __device__ __forceinline__ T wave_scan(T v, int n) {
 // takes for a tile then), of what they write, and of the pass that joins the slices.  all / t
 // slices beyond the first are within the budget; a row tile of more than t tiles has
 // fewer than 2 all / t.
+// Measured on 313 tiles out of the caches, us a tile.  head_dim 64, groups of waves: 0.6 for one workgroup to a CU,
+// then in whole rounds (1.2, 1.8); one group: 1.14, 1.37, 1.90 and 2.42 for one to four, 3.0 as soon as there are more.
+// head_dim 128: groups 1.0 and 2.1; one group 1.55, 2.13, 3.50, 4.36.  Keys from memory take longer where little
+// else runs (one group, one workgroup to a CU 1.77, two 1.89): the constants are theirs.
 template <int D, int KG>
 __device__ __forceinline__ int slice_tiles(float all, int most, const Split& sp) {
   if (sp.budget == 0) return NO_SPLIT;
@@ -758,8 +762,11 @@ cache_join(const CacheArgs c, const Split sp) {
 // Single tokens and short chunks read K and V once and their bytes are the time; in float32 the
 // matrix unit is slow enough for small row tiles.  There all key tiles of all (sequence, K/V
 // head, row tile) segments stand in one line that is cut evenly over the workgroups, so
-// unequal lengths cost nothing (a segment counts a few more for its start and end); a segment cut by a
-// border leaves partial results, at most two to a workgroup.
+// single tokens of unequal contexts have equal shares (a segment counts a few more for its start and end); a
+// segment cut by a border leaves partial results, at most two to a workgroup.  Every row tile of a sequence
+// counts the most keys that one of them reads, so shares of chunks whose masks let row tiles see unequal numbers
+// of keys are less equal: eight float32 chunks with windows of 1,000 count 29,112 tiles (and the segments' ends)
+// where 24,720 are read, and the fullest workgroup reads 65 of them, the mean 48.
 struct Few {
   float* o;           // [2 wgs][slot_rows][head_dim] sums
   float* ml;          // [2 wgs][slot_rows] (maximum, sum)
@@ -1052,8 +1059,8 @@ cache_few(const CacheArgs c, const Few f) {
             for (int r = 0; r < 16; ++r) o[x][r] *= corr;
         }
         // P in bf16, the other operand's type, and what that leaves out as a second operand: the
-        // bytes of K and V hide both products (91 us with one or two), and outputs are off by
-        // bf16's own 0.0017 of their size instead of 0.0024
+        // bytes of K and V hide most of it (8 x 10,160 keys of 24 heads 97.8 us, with one product 96.1; 64 x 300
+        // 40.7 and 39.1), and outputs are off by bf16's own 0.0017 of their size instead of 0.0024
         bf16x8 pf[KT][2], pl[KT][2];
         float ps0 = 0.0f, ps1 = 0.0f;
 #pragma unroll
@@ -1167,10 +1174,10 @@ cache_few(const CacheArgs c, const Few f) {
 // scores, the next K during the products with V, so a wave never waits for both, and two
 // waves share a SIMD.  What a part has at its start
 // (its place in the line, pages, queries, first keys) is asked for before the sums of the part before it
-// meet: 1,024 rows of 192 heads on 24 heads of 1,024 keys 475 us instead of 529.
-// Bound by the fp32 MFMA over long parts (8,192 x 8,192 keys, 24 heads: 80% of its peak) and by the parts'
-// ends over short ones.  Operands read ahead of the products and weights formed between them are no faster
-// (the windowed chunks below 104 us instead of 100).
+// meet: 1,024 rows of 192 heads on 24 heads of 1,024 keys take a tenth less (now 462 us).
+// Bound by the fp32 MFMA over long parts (8,192 x 8,192 keys, 24 heads: 3,320 us, 124 TFLOP/s) and by the parts'
+// ends over short ones.  Operands read ahead of the products and weights formed between them made windowed
+// chunks 4% slower.
 template <int D, int RUN>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, 8)))
 cache_f32(const CacheArgs c, const Few f) {
@@ -1552,12 +1559,13 @@ static void run_line(const CacheArgs& c, float* ws, int64_t ws_floats, hipStream
   const int64_t rows = (int64_t)c.n_q * c.group;
   Few f{};
   f.slot_rows = (int)std::min<int64_t>(FEW_BQ, rows);
-  // A segment's start and end take about as long as this many tiles: 64 x 1 token of 20 to 10,161 keys
-  // without them 47 us, with one or more 44; eight float32 chunks of 100 to 326 rows behind 6 to 3,000
-  // keys 99 us with none, 95 with four, 97 with eight, 110 with sixteen.
+  // A segment's start and end take about as long as this many tiles (passes with the joining one): 64 x 1 token of
+  // 20 to 10,161 keys without them 55.5 us, with one, two, four 50.2, 50.5, 51.7; eight float32 chunks of 100 to
+  // 326 rows behind 6 to 3,000 keys 97.2 us with none, 92.2 with four, 96.2 with eight, 107.5 with sixteen.
   f.extra = F32 ? 4 : 1;
-  // bf16: one wave to a SIMD, 64 KB in flight on a CU: 8 x 10,160 keys of 24 heads 91 us, 1 x 139,776
-  // of 4 heads of 128 48, with three to a CU 92 and 48, with five (a SIMD then has two) 116 and 62.
+  // bf16: one wave to a SIMD, 64 KB in flight on a CU: 8 x 10,160 keys of 24 heads 97.8 us, 1 x 139,776
+  // of 4 heads of 128 64.1, 64 x 300 of 24 heads 40.7; with three to a CU 98.8, 65.8 and 42.8, with five (a SIMD
+  // then has two) 128, 80 and 56.
   // float32: as many workgroups as the LDS holds.
   f.wgs = 256 * (!F32 ? 4 : D == 64 ? 2 : 1);
   f.cut = (int)std::max<int64_t>(0, std::min<int64_t>(f.wgs, ws_floats / (2 * (int64_t)f.slot_rows * (D + 2))));
@@ -1595,7 +1603,10 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
   sp.slot_rows = (int)std::min<int64_t>(BQ, rows);
   // Keys are split, as far as the workspace holds the partial results (at most two per slice of
   // the budget), unless the row tiles fill the card: those of one sequence are as long
-  // as each other, those of several may not be.
+  // as each other, those of several may not be.  Split and whole, us: one sequence of 24 heads behind 20,000 keys,
+  // 48 row tiles 85 and 177, 96 146 and 179, 144 207 and 183, 192 211 and 189, 240 212 and 204; several, 576 tiles
+  // of unequal contexts 43 and 84, 1,536 of equal ones 97 and 92, 3,072 163 and 153.  1,024 slices: with 256
+  // the unequal contexts take 86 us, though the first two of one sequence 59 and 108.
   if (least * kvh < (c.pg.n_seqs == 1 ? 192 : 2048)) {
     const int64_t fit = (ws_floats - 64) / (2 * (int64_t)sp.slot_rows * (D + 2));
     sp.budget = (int)std::min<int64_t>(1024, std::max<int64_t>(fit, 0));
@@ -1614,7 +1625,9 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
       hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min(units - u, step) * kvh)), dim3(256 * KG), 0, st, c, sp, (int)u);
   };
   // Few row tiles: one workgroup to a CU that takes several key tiles at once, as many as the LDS
-  // holds.
+  // holds.  With groups and without, us: chunks of 24 heads of 64 behind 2,000 keys, 192 row tiles 34 and 55, 240 38
+  // and 61, 384 66 and 75, 528 105 and 92, 648 124 and 114; of 4 K/V heads of 128, 252 73 and 103, 512 154 and 178,
+  // 752 both 285.
   auto launch = [&](auto run) {
     if (most * kvh <= 640) launch_with(run, std::integral_constant<int, D == 64 ? 4 : 2>{});
     else launch_with(run, std::integral_constant<int, 1>{});
@@ -1634,7 +1647,8 @@ static void run_cache(int dtype, const CacheArgs& c, float* ws, int64_t ws_float
   // Few rows to a sequence, by the mean that the host knows; also twice as many where there are few
   // row tiles in all, which the line cuts finer: one chunk of 64 rows behind 10,000 keys, 3 heads of 128,
   // 27 us on the line and 53 in slices, 24 heads of 64 43 and 47; eight such of 24 heads behind
-  // 2,000 55 and 42.
+  // 2,000 55 and 42.  (The mean goes wrong where one long chunk stands among many sequences that are idle: 20,000
+  // tokens of 12 heads among 1,024 take 2,040 us, alone 690.)
   const int64_t rows = (int64_t)c.n_q * c.group;
   const bool few = rows <= (int64_t)FEW_BQ * c.pg.n_seqs ||
                    (rows <= 2 * (int64_t)FEW_BQ * c.pg.n_seqs && rows * c.pg.kv_heads <= FEW_BQ * 128);

@@ -7,10 +7,10 @@
 // heads are on their way, and stay in the registers of the lanes for every head.
 //   y = x / sqrt(mean(x^2) + eps) * gain,  a' = m (a cos t - b sin t), b' = m (a sin t + b cos t)
 // What bounds it: HBM, each element read and written once: 10,160 rows of 48 heads of 64 in bf16 26 us
-// (125 MB, 4.8 TB/s), 17,472 of 20 heads of 128 40 (179 MB), an append of 10,160 x 72 heads 42 (187 MB),
-// of 18 float32 heads of 128 to 15,390 rows 70 (365 MB, 5.2 TB/s).  What counted: the loads in front of
+// (125 MB, 4.8 TB/s), 17,472 of 20 heads of 128 40 (179 MB), an append of 10,160 x 72 heads 43 (187 MB),
+// of 18 float32 heads of 128 to 15,390 rows 71 (365 MB, 5.1 TB/s).  What counted: the loads in front of
 // the angles and always some on their way (44 us without, for the first), steps of heads of one kind, so that
-// pointers and gains are scalar choices, and few registers (72: seven waves to a SIMD).
+// pointers and gains are scalar choices, and few registers (72 for the first: seven waves to a SIMD).
 #include "paged.h"
 
 #include <algorithm>
