@@ -249,10 +249,10 @@ __device__ __forceinline__ void add_odd(f32x16& o, int q4, bool sees, uint2 x) {
 
 // RUN: 8-key slabs that share a page for certain
 // KG: groups of four waves.  Each takes every KG-th tile of the same rows; they meet in LDS.
-// FINE: sequences of up to FEW_BQ rows, which stand beside longer ones here, keep 16 bits of each weight as
-// they do on the line: their rows are one wave's, and the second wave, which has none, takes the same rows with
-// what bf16 leaves of the weights (three single tokens of 24 heads beside 1,248 behind 3,000 keys: 88 us,
-// with bf16's 8 bits alone 71; batches without such a sequence as before)
+// FINE: sequences of up to FEW_BQ rows, which stand beside longer ones here or in a padded call, keep 16 bits of
+// each weight as they do on the line: their rows are one wave's, and the second wave, which has none, takes the
+// same rows with what bf16 leaves of the weights (three single tokens of 24 heads beside 1,248 behind 3,000 keys:
+// 88 us, with bf16's 8 bits alone 71; calls without such a sequence within 0.5%)
 template <int D, int RUN, int KG, bool FINE>
 __global__ void __launch_bounds__(256 * KG) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, 8)))
 cache_bf16(const CacheArgs c, const Split sp, int unit0) {
@@ -425,15 +425,14 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
             pf[t][u][mm] = (__bf16)p0; pf[t][u][mm + 1] = (__bf16)p1;
           }
     };
-    if (!fresh && !(FINE && fine)) {
+    if (!fresh) {
       f32x16 st[2];
       scores(st, vis);
       probs(st);
     }
     // the running maximum moves only when a row sum shows that some weight passed
-    // 2^8 (or is NaN): the scores are then formed again against the new one (for both parts of the weights in
-    // every tile: they have to go by the same maximum)
-    if (fresh || (FINE && fine) || __any(!(ps0 + ps1 <= 256.0f))) {
+    // 2^8 (or is NaN): the scores are then formed again against the new one
+    if (fresh || __any(!(ps0 + ps1 <= 256.0f))) {
       uint32_t w0 = __builtin_amdgcn_readfirstlane((uint32_t)vis), w1 = __builtin_amdgcn_readfirstlane((uint32_t)(vis >> 32));
       asm volatile("" : "+s"(w0), "+s"(w1) : : "memory");
       const uint64_t again = (uint64_t)w1 << 32 | w0;
@@ -547,7 +546,8 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
     if (vis && k0 <= lim_last && k1 >= low_first) {
       const bool cut = k1 > lim_first, early = k0 < low_last;
       tile(ring[buf], t, vis, cut || early || vis != ~0ull, (cut && lim_first < total - 1) || early, fresh);
-      fresh = false;
+      // (both parts of the weights have to go by the same maximum: it moves in every tile)
+      fresh = FINE && fine;
     }
     vis = ahead;
     buf ^= 1;
@@ -1619,8 +1619,8 @@ static void run_chunk(const CacheArgs& c, float* ws, int64_t ws_floats, hipStrea
   const int64_t step = ((1 << 24) - 1) / kvh;
   auto launch_with = [&](auto run, auto groups) {
     constexpr int RUN = decltype(run)::value, KG = decltype(groups)::value;
-    // (a sequence of few rows is here only beside others)
-    const auto kernel = c.pg.n_seqs > 1 ? cache_bf16<D, RUN, KG, true> : cache_bf16<D, RUN, KG, false>;
+    // (a sequence of few rows is here only beside others, or where offsets leave rows out)
+    const auto kernel = c.pg.cu != nullptr ? cache_bf16<D, RUN, KG, true> : cache_bf16<D, RUN, KG, false>;
     for (int64_t u = 0; u < units; u += step)
       hipLaunchKernelGGL(kernel, dim3((unsigned)(std::min(units - u, step) * kvh)), dim3(256 * KG), 0, st, c, sp, (int)u);
   };

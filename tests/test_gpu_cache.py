@@ -1072,3 +1072,22 @@ def test_a_context_that_moves_to_another_stream_gives_the_same(dtype):
     for other in kept[1:]:
         for a, b in zip(kept[0], other):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,old,rows,heads,kvh,dim,page", [
+    (1, 70, 200, 4, 4, 64, 16), (8, 200, 1000, 8, 2, 64, 64), (20, 33, 700, 3, 3, 128, 8), (3, 900, 2000, 100, 50, 64, 32)])
+def test_a_short_chunk_in_a_padded_call_keeps_16_bits_of_the_weights(contexts, dtype, n, old, rows, heads, kvh, dim, page):
+    """One sequence whose offsets leave most rows out, as a captured call of the longest chunk has them."""
+    dt, g = TYPES[dtype], gen(29)
+    c = Paged(dt, [old], [old + n], page, kvh, dim)
+    c.put(0, 0, old + n, g)
+    for first in (0, rows - n, 40):
+        q, _ = rows_of((rows, heads, dim), dt, g)
+        o = torch.full_like(q, 7.0)
+        cu = torch.tensor([first, first + n], dtype=torch.int32, device="cuda")
+        contexts[dtype].cache_attention(c.c, q, o, cu=cu, scale=0.01)
+        r = slice(first, first + n)
+        check_fine(c, q[r], o[r], [n], True, 0, 0.01)
+        check_cache_attention(c, q[r], o[r], None, [n], True, 0, 0.01, o[r], None)
+        assert bool((o[:first] == 7.0).all()) and bool((o[first + n:] == 7.0).all())
