@@ -228,6 +228,10 @@ __device__ __forceinline__ uint64_t keys_of(int key0, int total, const int (&pag
   return n >= 8 * RUN * N ? m : n <= 0 ? 0ull : m & ((1ull << n) - 1);
 }
 
+// A sum over its weights' (inv: 1 / them, or 0 where no key with a weight was seen: its values then do not
+// matter, whatever they are).
+__device__ __forceinline__ float norm(float o, float inv) { return inv == 0.0f ? 0.0f : o * inv; }
+
 // Loads into LDS that this wave has read: its reads have arrived.
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -651,7 +655,7 @@ cache_bf16(const CacheArgs c, const Split sp, int unit0) {
       uint32_t v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        v[e] = pack_bf16x2(o[ht][4 * q4 + 2 * e] * inv, o[ht][4 * q4 + 2 * e + 1] * inv);
+        v[e] = pack_bf16x2(norm(o[ht][4 * q4 + 2 * e], inv), norm(o[ht][4 * q4 + 2 * e + 1], inv));
       const auto x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
       const auto y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
       if (in_tile < left) *(uint4*)(op + 32 * ht + 8 * (q4 + g)) = make_uint4(x[0], y[0], x[1], y[1]);
@@ -707,9 +711,9 @@ __device__ __forceinline__ void join_rows(const CacheArgs& c, const float* po, c
     const int head = hk * c.group + row_of.head(r);
     T* op = (T*)c.o + tok * c.o_ld + head * D + col;
     if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+      *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(norm(acc[0], inv), norm(acc[1], inv)), pack_bf16x2(norm(acc[2], inv), norm(acc[3], inv)));
     else
-      *reinterpret_cast<float4*>(op) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      *reinterpret_cast<float4*>(op) = make_float4(norm(acc[0], inv), norm(acc[1], inv), norm(acc[2], inv), norm(acc[3], inv));
     if (c.lse != nullptr && col == 0) c.lse[tok * c.heads + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
   }
 }
@@ -1159,7 +1163,7 @@ cache_few(const CacheArgs c, const Few f) {
         uint32_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          v[e] = pack_bf16x2(o[ht][4 * q4 + 2 * e] * inv, o[ht][4 * q4 + 2 * e + 1] * inv);
+          v[e] = pack_bf16x2(norm(o[ht][4 * q4 + 2 * e], inv), norm(o[ht][4 * q4 + 2 * e + 1], inv));
         const auto x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
         const auto y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
         if (r31 < left) *(uint4*)(op + 32 * ht + 8 * (q4 + g)) = make_uint4(x[0], y[0], x[1], y[1]);
@@ -1236,7 +1240,7 @@ cache_f32(const CacheArgs c, const Few f) {
           acc[2] = fmaf(y.z, e4[v], acc[2]);
           acc[3] = fmaf(y.w, e4[v], acc[3]);
         }
-        *reinterpret_cast<float4*>(dst + 4 * x) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        *reinterpret_cast<float4*>(dst + 4 * x) = make_float4(norm(acc[0], inv), norm(acc[1], inv), norm(acc[2], inv), norm(acc[3], inv));
       }
       if ((tid & 7) == 0) {
         if (!last.whole) *reinterpret_cast<float2*>(f.ml + at * 2) = make_float2(mt, lt);
@@ -1544,9 +1548,9 @@ line_join_row(const CacheArgs c, const Few f) {
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* op = (T*)c.o + tok * c.o_ld + head * D + col;
       if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+        *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf16x2(norm(x[0], inv), norm(x[1], inv)), pack_bf16x2(norm(x[2], inv), norm(x[3], inv)));
       else
-        *reinterpret_cast<float4*>(op) = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+        *reinterpret_cast<float4*>(op) = make_float4(norm(x[0], inv), norm(x[1], inv), norm(x[2], inv), norm(x[3], inv));
       if (c.lse != nullptr && lane == 0) c.lse[id] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
     }
   }

@@ -1091,3 +1091,30 @@ def test_a_short_chunk_in_a_padded_call_keeps_16_bits_of_the_weights(contexts, d
         check_fine(c, q[r], o[r], [n], True, 0, 0.01)
         check_cache_attention(c, q[r], o[r], None, [n], True, 0, 0.01, o[r], None)
         assert bool((o[:first] == 7.0).all()) and bool((o[first + n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new,old,heads,kvh", [([1], [9], 4, 2), ([1], [3000], 4, 4), ([5, 1], [40, 900], 6, 2), ([200], [150], 3, 3),
+                                               ([300, 2], [64, 700], 4, 4), ([900], [0], 16, 16)])
+def test_rows_without_a_weight_are_zeros_whatever_the_values(contexts, dtype, dim, new, old, heads, kvh):
+    """Scores that are all minus infinity: the rows are zeros and their normaliser minus infinity, also with values that are
+    not finite, in a cache whose first K/V head alone is so."""
+    dt, g = TYPES[dtype], gen(31)
+    c = Paged(dt, old, [a + b for a, b in zip(new, old)], 16, kvh, dim)
+    for s in range(len(new)):
+        c.put(s, 0, old[s] + new[s], g)
+    q, _ = rows_of((sum(new), heads, dim), dt, g)
+    q[:, :, 7] = q[:, :, 7].abs() + 0.5
+    clean = torch.empty_like(q)
+    contexts[dtype].cache_attention(c.c, q, clean, cu=offsets(new))
+    for s in range(len(new)):
+        j = torch.arange(old[s] + new[s], device="cuda")
+        p, t = c.where(s, j)
+        c.k[p, t, 0, 7] = -math.inf
+        c.v[p, t, 0] = torch.tensor([math.inf, math.nan, -math.inf, 1.0], device="cuda").to(dt)[(j[:, None] + torch.arange(dim, device="cuda")) % 4]
+    o, lse = torch.full_like(q, 7.0), torch.full((sum(new), heads), 7.0, device="cuda")
+    contexts[dtype].cache_attention(c.c, q, o, cu=offsets(new), lse=lse)
+    group = heads // kvh
+    assert bool((o[:, :group] == 0).all()) and bool((lse[:, :group] == -math.inf).all())
+    assert torch.equal(o[:, group:], clean[:, group:]) and bool(torch.isfinite(lse[:, group:]).all())
