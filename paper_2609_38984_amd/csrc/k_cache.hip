@@ -11,7 +11,8 @@
 // some row sees in part.
 //
 // What bounds it (kernels alone, on keys from memory): for chunks the instructions of a score (causal 10,160 x 24
-// heads of 64 373 us, 850 TFLOP/s: vector operations 64% of the time, MFMAs 40%, hardly side by side); for single
+// heads of 64 373 to 388 us by the clock, 820 to 850 TFLOP/s: vector operations 65% of the time, MFMAs 40%, hardly
+// side by side); for single
 // tokens the bytes of K and V (8 x 10,160 keys of 24 heads 92 us, 5.4 TB/s); in float32 the matrix unit
 // (causal 4,096 x 24 heads 443 us with the joining pass, 1.2 times its products at a large product's rate).
 #include "gemm_common.h"
